@@ -497,6 +497,103 @@ pipe_status pipe_ensemble_conv2d_q8(const pipe_layer_desc* desc, const pipe_conv
  */
 pipe_status pipe_lower_conv_input(const pipe_conv_geom* geom, const int8_t* d_xq, int8_t* d_rows, int64_t ld_rows, void* stream);
 
+/*
+ * 4-bit weights with group scales on 16-bit activations, and products grouped by expert.
+ *
+ * Beside the expansion above, whose scales belong to whole rows and whose activations are int8, this is the form in which
+ * checkpoints of large language models hold their projections: codes of 4 bits, one scale (and, asymmetric, one zero point) per
+ * group of g consecutive weights of a row, activations in bf16 or fp16.  A layer may be E layers of one shape, the experts of a
+ * sparse layer, of which every token meets a few.
+ *
+ * A layer of E experts [O, I] is three device arrays (any of them may come from elsewhere than pipe_group_quantize):
+ *   codes   uint8 [E, I/32, O, 16], 16-byte aligned: the 32 codes 32b .. 32b+31 of row o are the 16 bytes at (e, b, o); code
+ *           8w + 2i of them is nibble i and code 8w + 2i + 1 nibble i + 4 of the w-th little-endian 32-bit word, so that a shift
+ *           and a mask leave two neighbouring codes in the two halves of a register
+ *   scales  [E, I/g, O] in the type of the activations
+ *   zeros   uint8 [E, I/g, O], values 0..15, or NULL for a symmetric layer, whose zero point is 8 everywhere
+ * and stands for W_e[o, i] = scales[e, i/g, o] * (code[e, o, i] - zeros[e, i/g, o]).
+ */
+#define PIPE_DTYPE_BF16 0
+#define PIPE_DTYPE_FP16 1
+#define PIPE_DTYPE_FP32 2   /* source weights of pipe_group_quantize only */
+#define PIPE_MAX_EXPERTS 1024
+typedef struct pipe_group_desc {
+  int32_t experts;       /* E, 1..PIPE_MAX_EXPERTS (1: a plain layer) */
+  int32_t out_features;  /* O: rows of W */
+  int32_t in_features;   /* I: reduction length, a multiple of g */
+  int32_t group_size;    /* g: 32, 64 or 128 */
+  int32_t dtype;         /* activations, scales, bias and outputs: PIPE_DTYPE_BF16 or PIPE_DTYPE_FP16 */
+  int32_t asymmetric;    /* 0, or 1: the layer has zero points */
+} pipe_group_desc;
+
+typedef struct pipe_group_layout_t {
+  int32_t groups;        /* I / g */
+  uint64_t codes_bytes, scales_bytes, zeros_bytes;   /* sizes of the three arrays (zeros: 0 for a symmetric layer) */
+} pipe_group_layout_t;
+
+/* Validates `desc` (PIPE_ERR_INVALID_ARG: a field out of its range; PIPE_ERR_UNSUPPORTED: another group size;
+ * PIPE_ERR_SHAPE: g does not divide I) and fills `h_out`.  Pure host function. */
+pipe_status pipe_group_layout(const pipe_group_desc* desc, pipe_group_layout_t* h_out);
+
+/*
+ * Makes such a layer from weights d_W (E*O rows of I values of type w_dtype, row pitch ldw; expert e's rows follow expert e-1's).
+ * Per group, in binary32 with IEEE divisions, h() being the rounding to the layer's type and rne() to the nearest integer of the
+ * exact quotient, ties to even:
+ *   symmetric   s = h(max|w| / 7),                              code = clamp(rne(w / s), -7, 7) + 8
+ *   asymmetric  lo = min(w, 0), hi = max(w, 0), s = h((hi - lo) / 15), z = clamp(rne(-lo / s), 0, 15),
+ *               code = clamp(rne(w / s) + z, 0, 15)
+ * A group whose s is zero has codes equal to its zero point (8; asymmetric 0).
+ * d_values (NULL, or float [E*O, I] pitch ldv): receives s * (code - z), which binary32 holds exactly: the weights that the layer
+ * stands for, from which a caller forms the residual that the next order of an expansion quantizes.
+ * A NaN or Inf among the weights, or a scale beyond the range of fp16, sets PIPE_ERR_NONFINITE in the device status word.
+ * d_W and d_values need the alignment of their type (16-byte aligned rows are faster); d_codes 16 bytes.
+ */
+pipe_status pipe_group_quantize(const pipe_group_desc* desc, const void* d_W, int32_t w_dtype, int64_t ldw, void* d_codes,
+                                void* d_scales, uint8_t* d_zeros, float* d_values, int64_t ldv, void* stream);
+
+/*
+ * y[t, o] = h(sigma(sum_i x[t, i] W[o, i] + bias[o])) for a layer of one expert: products with a vector for one token, with a
+ * matrix for more.  sums and sigma (PIPE_ACT_*) in binary32.  Codes and activations are multiplied as they are, the scale
+ * is applied to a group's binary32 sum.
+ * d_x: [T, I] pitch ldx, 16-byte aligned, ldx a multiple of 8.  d_bias: [O] or NULL.  d_y: [T, O] pitch ldy.
+ * T = 0 is a no-op.  d_y must not overlap the inputs.
+ */
+pipe_status pipe_group_linear(const pipe_group_desc* desc, const void* d_codes, const void* d_scales, const uint8_t* d_zeros,
+                              const void* d_x, int64_t T, int64_t ldx, const void* d_bias, int32_t activation, void* d_y,
+                              int64_t ldy, void* stream);
+
+/*
+ * Deals a router's choice to the experts: d_choice int32 [T, k] (dense) names the k experts of every token.  The T*k places of
+ * the choice, those of expert 0 first, then those of expert 1 and so on, each expert's in ascending order of t*k + j, are
+ * numbered as slots:
+ *   d_offsets int32 [E + 1]: the slots of expert e are d_offsets[e] .. d_offsets[e+1] - 1
+ *   d_rows    int32 [T*k]:   the token of every slot (entries from d_offsets[E] on are left as they were)
+ *   d_slots   int32 [T, k]:  the slot of every place, -1 for a choice outside [0, E), which gets none
+ * No atomics decide an order: equal inputs give equal outputs.  T*k < 2^31, 1 <= E <= PIPE_MAX_EXPERTS.  One launch, no workspace.
+ */
+pipe_status pipe_expert_rows(const int32_t* d_choice, int64_t T, int32_t k, int32_t experts, int32_t* d_offsets, int32_t* d_rows,
+                             int32_t* d_slots, void* stream);
+
+/*
+ * One launch of all experts, each on its own rows:  for d_offsets[e] <= s < d_offsets[e+1]
+ *     y[s, o] = h(sigma(sum_i x[r, i] W_e[o, i] + bias[e, o])),   r = d_rows[s], or s itself where d_rows is NULL.
+ * Ragged sizes, empty experts among them, are read on the device; nothing is copied to the host.  d_x: [T, I] pitch ldx (16-byte
+ * aligned, ldx a multiple of 8); d_rows: int32 [N] or NULL; d_offsets: int32 [E+1] ascending; d_bias: [E, O] or NULL; d_y: [N, O]
+ * pitch ldy, of which the rows behind d_offsets[E] are left as they were.  N: the rows that d_y and d_rows have room for.  Offsets
+ * are taken as clamped to [0, N], and a row index outside [0, T) reads as a row of zeros.  Arithmetic as in pipe_group_linear.
+ */
+pipe_status pipe_expert_linear(const pipe_group_desc* desc, const void* d_codes, const void* d_scales, const uint8_t* d_zeros,
+                               const void* d_x, int64_t T, int64_t ldx, const int32_t* d_rows, const int32_t* d_offsets, int64_t N,
+                               const void* d_bias, int32_t activation, void* d_y, int64_t ldy, void* stream);
+
+/*
+ * The experts' outputs of every token joined: out[t, o] = h(sum_j weights[t, j] * y[slots[t, j], o]), j ascending, in binary32.
+ * A slot outside [0, N) contributes nothing; a token without slots gets zeros.  d_y: [N, O] pitch ldy; d_slots: int32 [T, k] dense;
+ * d_weights: float [T, k] dense; d_out: [T, O] pitch ldo; dtype: PIPE_DTYPE_BF16 or PIPE_DTYPE_FP16, of d_y and d_out.
+ */
+pipe_status pipe_expert_combine(const void* d_y, int64_t N, int64_t ldy, const int32_t* d_slots, const float* d_weights, int64_t T,
+                                int32_t k, int32_t O, int32_t dtype, void* d_out, int64_t ldo, void* stream);
+
 /* Number of kernels the library has launched in this process (all calls, all streams). */
 uint64_t pipe_launch_count(void);
 

@@ -38,6 +38,7 @@ EXPORTS = ["pipe_keep_groups_from_gamma", "pipe_default_branches", "pipe_layout"
            "pipe_quantize_act", "pipe_quantize_act_ex", "pipe_ensemble_forward_zp", "pipe_expanded_linear", "pipe_expanded_conv2d", "pipe_ensemble_forward",
            "pipe_ensemble_forward_q8", "pipe_expanded_conv2d_q8", "pipe_ensemble_conv2d", "pipe_ensemble_conv2d_q8",
            "pipe_lower_conv_input",
+           "pipe_group_layout", "pipe_group_quantize", "pipe_group_linear", "pipe_expert_rows", "pipe_expert_linear", "pipe_expert_combine",
            "pipe_launch_count", "pipe_poll_status", "pipe_status_string",
            # include/pipe_diag.h: tests and measurements only
            "pipe_diag_select_kernel", "pipe_diag_mma_i8_rate", "pipe_diag_bounded_wait"]
@@ -70,6 +71,15 @@ class LayerLayout(C.Structure):
                 ("decode_split_all", C.c_int32),
                 ("blob_bytes", C.c_uint64), ("expand_ws_bytes", C.c_uint64),
                 ("quantize_ws_bytes", C.c_uint64)]
+
+
+class GroupDesc(C.Structure):
+    _fields_ = [("experts", C.c_int32), ("out_features", C.c_int32), ("in_features", C.c_int32), ("group_size", C.c_int32),
+                ("dtype", C.c_int32), ("asymmetric", C.c_int32)]
+
+
+class GroupLayout(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("codes_bytes", C.c_uint64), ("scales_bytes", C.c_uint64), ("zeros_bytes", C.c_uint64)]
 
 
 class PipeError(RuntimeError):
@@ -112,6 +122,12 @@ def lib() -> C.CDLL:
         L.pipe_ensemble_conv2d.argtypes = [C.POINTER(LayerDesc), C.POINTER(ConvGeom), p, p, p, p, p, i64, i32, p, p]
         L.pipe_ensemble_conv2d_q8.argtypes = [C.POINTER(LayerDesc), C.POINTER(ConvGeom), p, p, p, p, i32, p, p, i64, p, p]
         L.pipe_lower_conv_input.argtypes = [C.POINTER(ConvGeom), p, p, i64, p]
+        L.pipe_group_layout.argtypes = [C.POINTER(GroupDesc), C.POINTER(GroupLayout)]
+        L.pipe_group_quantize.argtypes = [C.POINTER(GroupDesc), p, i32, i64, p, p, p, p, i64, p]
+        L.pipe_group_linear.argtypes = [C.POINTER(GroupDesc), p, p, p, p, i64, i64, p, i32, p, i64, p]
+        L.pipe_expert_rows.argtypes = [p, i64, i32, i32, p, p, p, p]
+        L.pipe_expert_linear.argtypes = [C.POINTER(GroupDesc), p, p, p, p, i64, i64, p, p, i64, p, i32, p, i64, p]
+        L.pipe_expert_combine.argtypes = [p, i64, i64, p, p, i64, i32, i32, i32, p, i64, p]
         L.pipe_diag_select_kernel.argtypes = [i32]
         L.pipe_diag_mma_i8_rate.argtypes = [i32, i64, i32, C.POINTER(C.c_double), p]
         L.pipe_diag_bounded_wait.argtypes = [i64, p]
@@ -425,6 +441,140 @@ def pipe_ensemble_forward_q8(desc: LayerDesc, blob: torch.Tensor, xq_m, sx_m, ou
     yp = PA(*[_dp(t) for t in yq_m])
     _check(lib().pipe_ensemble_forward_q8(C.byref(desc), _dp(blob), xp, T, ldxq, sp, _dp(bias), int(relu), op, yp,
                                           ldyq, _dp(partials), _stream_ptr(stream)), "pipe_ensemble_forward_q8")
+
+
+# ---- 4-bit weights with group scales, products grouped by expert -----------------------------------------------------------------
+DTYPE_BF16, DTYPE_FP16, DTYPE_FP32 = 0, 1, 2
+MAX_EXPERTS = 1024
+_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_FP16, torch.float32: DTYPE_FP32}
+
+
+def make_group_desc(O: int, I: int, g: int, dtype=torch.bfloat16, asymmetric: bool = False, experts: int = 1) -> GroupDesc:
+    if dtype not in _DTYPES:
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"make_group_desc: dtype {dtype}")
+    return GroupDesc(int(experts), int(O), int(I), int(g), _DTYPES[dtype], 1 if asymmetric else 0)
+
+
+def pipe_group_layout(desc: GroupDesc) -> GroupLayout:
+    out = GroupLayout()
+    _check(lib().pipe_group_layout(C.byref(desc), C.byref(out)), "pipe_group_layout")
+    return out
+
+
+def _wants(where: str, ok: bool, what: str) -> None:
+    if not ok:
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: {what}")
+
+
+def _on_current(where: str, first: torch.Tensor, *others) -> None:
+    """Every tensor lies on the current device: the library launches there, on that device's stream."""
+    dev = first.get_device()
+    if dev < 0 or dev != _current_device() or any(t is not None and t.get_device() != dev for t in others):
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: all tensors have to be on the current device")
+
+
+def _rows_of(where: str, t: torch.Tensor, cols: int) -> int:
+    """Row pitch of a [rows, cols] matrix whose rows are contiguous."""
+    if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: a matrix of shape {tuple(t.shape)} and strides {t.stride()}, {cols} contiguous columns are needed")
+    return t.stride(0) if t.shape[0] > 1 else max(cols + 7 & ~7, t.stride(0) & ~7)
+
+
+def _group_arrays(where: str, desc: GroupDesc, codes, scales, zeros, *others) -> torch.dtype:
+    """Checks the three arrays of a layer against the descriptor; the layer's torch type."""
+    E, O, I, g = desc.experts, desc.out_features, desc.in_features, desc.group_size
+    h = torch.bfloat16 if desc.dtype == DTYPE_BF16 else torch.float16
+    if codes.dtype != torch.uint8 or scales.dtype != h or codes.numel() * 2 != E * O * I or scales.numel() * g != E * O * I \
+            or not codes.is_contiguous() or not scales.is_contiguous():
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: codes / scales are not the descriptor's arrays")
+    if (zeros is not None) != bool(desc.asymmetric) or \
+            (zeros is not None and (zeros.dtype != torch.uint8 or zeros.numel() * g != E * O * I or not zeros.is_contiguous())):
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: zeros are not the descriptor's array")
+    _on_current(where, codes, scales, zeros, *others)
+    return h
+
+
+def pipe_group_quantize(desc: GroupDesc, W: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor | None = None,
+                        values: torch.Tensor | None = None, stream=None) -> None:
+    """W: cuda float32 / bfloat16 / float16 [E, O, I] or [E*O, I]; codes, scales, zeros: the layer's arrays (see alloc_group);
+    values: float32 of W's shape, or None."""
+    where = "pipe_group_quantize"
+    _group_arrays(where, desc, codes, scales, zeros, W, values)
+    rows, I = desc.experts * desc.out_features, desc.in_features
+    _wants(where, W.dtype in _DTYPES and W.numel() == rows * I, "W is not the descriptor's weights")
+    W = W.view(rows, I) if W.dim() != 2 else W
+    ldv = 0
+    if values is not None:
+        _wants(where, values.dtype == torch.float32 and values.numel() == rows * I, "values have another shape or type")
+        values = values.view(rows, I) if values.dim() != 2 else values
+        _wants(where, I == 1 or values.stride(1) == 1, "values: rows are not contiguous")
+        ldv = values.stride(0) if rows > 1 else max(I, values.stride(0))
+    _wants(where, I == 1 or W.stride(1) == 1, "W: rows are not contiguous")
+    _check(lib().pipe_group_quantize(C.byref(desc), W.data_ptr(), _DTYPES[W.dtype], W.stride(0) if rows > 1 else max(I, W.stride(0)),
+                                     codes.data_ptr(), scales.data_ptr(), _dp(zeros), _dp(values), ldv, _stream_ptr(stream)), where)
+
+
+def pipe_group_linear(desc: GroupDesc, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor | None, x: torch.Tensor,
+                      y: torch.Tensor, bias: torch.Tensor | None = None, activation: int = ACT_IDENTITY, stream=None) -> None:
+    """x: cuda [T, I], y: cuda [T, O], bias: [O] (or [1, O]), all in the layer's type."""
+    where = "pipe_group_linear"
+    h = _group_arrays(where, desc, codes, scales, zeros, x, y, bias)
+    _wants(where, x.dtype == h and y.dtype == h and x.shape[0] == y.shape[0], "x and y differ in rows or from the layer's type")
+    _wants(where, bias is None or (bias.dtype == h and bias.numel() == desc.out_features and bias.is_contiguous()), "bias")
+    _check(lib().pipe_group_linear(C.byref(desc), codes.data_ptr(), scales.data_ptr(), _dp(zeros), x.data_ptr(), x.shape[0],
+                                   _rows_of(where, x, desc.in_features), _dp(bias), activation, y.data_ptr(),
+                                   _rows_of(where, y, desc.out_features), _stream_ptr(stream)), where)
+
+
+def pipe_expert_rows(choice: torch.Tensor, experts: int, offsets: torch.Tensor, rows: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
+    """choice: cuda int32 [T, k]; offsets: int32 [experts + 1]; rows: int32 [T*k]; slots: int32 [T, k]."""
+    where = "pipe_expert_rows"
+    _on_current(where, choice, offsets, rows, slots)
+    _wants(where, choice.dim() == 2 and all(t.dtype == torch.int32 and t.is_contiguous() for t in (choice, offsets, rows, slots)),
+           "int32 tensors with contiguous entries are needed")
+    T, k = choice.shape
+    _wants(where, offsets.numel() == experts + 1 and rows.numel() == T * k and slots.numel() == T * k, "sizes do not match the choice")
+    _check(lib().pipe_expert_rows(choice.data_ptr(), T, k, experts, offsets.data_ptr(), rows.data_ptr(), slots.data_ptr(),
+                                  _stream_ptr(stream)), where)
+
+
+def pipe_expert_linear(desc: GroupDesc, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor | None, x: torch.Tensor,
+                       offsets: torch.Tensor, y: torch.Tensor, rows: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                       activation: int = ACT_IDENTITY, stream=None) -> None:
+    """x: cuda [T, I]; offsets: int32 [E + 1]; rows: int32 [N] or None; y: [N, O]; bias: [E, O] or None."""
+    where = "pipe_expert_linear"
+    h = _group_arrays(where, desc, codes, scales, zeros, x, y, bias, offsets, rows)
+    N = y.shape[0]
+    _wants(where, x.dtype == h and y.dtype == h, "x or y has another type than the layer")
+    _wants(where, offsets.dtype == torch.int32 and offsets.numel() == desc.experts + 1 and offsets.is_contiguous(), "offsets")
+    _wants(where, rows is None or (rows.dtype == torch.int32 and rows.numel() == N and rows.is_contiguous()), "rows")
+    _wants(where, bias is None or (bias.dtype == h and bias.numel() == desc.experts * desc.out_features and bias.is_contiguous()), "bias")
+    _check(lib().pipe_expert_linear(C.byref(desc), codes.data_ptr(), scales.data_ptr(), _dp(zeros), x.data_ptr(), x.shape[0],
+                                    _rows_of(where, x, desc.in_features), _dp(rows), offsets.data_ptr(), N, _dp(bias), activation,
+                                    y.data_ptr(), _rows_of(where, y, desc.out_features), _stream_ptr(stream)), where)
+
+
+def pipe_expert_combine(y: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    """y: cuda [N, O]; slots: int32 [T, k]; weights: float32 [T, k]; out: [T, O] of y's type."""
+    where = "pipe_expert_combine"
+    _on_current(where, y, slots, weights, out)
+    _wants(where, y.dtype == out.dtype and y.dtype in _DTYPES and slots.dtype == torch.int32 and weights.dtype == torch.float32, "types")
+    _wants(where, slots.dim() == 2 and weights.shape == slots.shape and slots.is_contiguous() and weights.is_contiguous() and
+           out.shape[0] == slots.shape[0], "slots, weights and out do not belong together")
+    T, k = slots.shape
+    O = y.shape[1]
+    _check(lib().pipe_expert_combine(y.data_ptr(), y.shape[0], _rows_of(where, y, O), slots.data_ptr(), weights.data_ptr(), T, k, O,
+                                     _DTYPES[y.dtype], out.data_ptr(), _rows_of(where, out, O), _stream_ptr(stream)), where)
+
+
+def alloc_group(desc: GroupDesc, device="cuda"):
+    """codes, scales and zeros (None for a symmetric layer) of a layer, unset."""
+    lay = pipe_group_layout(desc)
+    E, O, I = desc.experts, desc.out_features, desc.in_features
+    h = torch.bfloat16 if desc.dtype == DTYPE_BF16 else torch.float16
+    codes = torch.empty((E, I // 32, O, 16), dtype=torch.uint8, device=device)
+    scales = torch.empty((E, lay.groups, O), dtype=h, device=device)
+    return codes, scales, torch.empty((E, lay.groups, O), dtype=torch.uint8, device=device) if desc.asymmetric else None
 
 
 def pipe_diag_select_kernel(which: int) -> None:

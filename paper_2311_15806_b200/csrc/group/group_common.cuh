@@ -1,0 +1,176 @@
+// What the kernels of the 4-bit layers with group scales share (formats and entry points: include/pipe.h).
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "pipe_common.cuh"
+
+namespace pipe {
+namespace grp {
+
+// One call of pipe_group_linear (offsets = nullptr: one expert that owns all N rows) or pipe_expert_linear.
+struct Call {
+  int E, O, I, g;
+  int KB;                 // I / 32: runs of 32 codes, the rows of 16 bytes of the code array
+  const uint8_t* codes;   // [E, KB, O, 16]
+  const void* scales;     // [E, I/g, O]
+  const uint8_t* zeros;   // the same shape, or nullptr
+  const void* x;          // [T, I] pitch ldx
+  int64_t T, ldx;
+  const int32_t* rows;    // [N] or nullptr
+  const int32_t* offsets; // [E + 1] or nullptr
+  int64_t N;
+  const void* bias;       // [E, O] or nullptr
+  int act;
+  void* y;                // [N, O] pitch ldy
+  int64_t ldy;
+  int* status;
+};
+
+// CTAs of a cluster: rank, count, the barrier of all their threads, and reads of another one's shared memory.
+__device__ __forceinline__ int cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return static_cast<int>(r);
+}
+__device__ __forceinline__ int cluster_ctas() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return static_cast<int>(r);
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_address(const void* own, int rank) {
+  uint32_t d;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(own))), "r"(rank));
+  return d;
+}
+__device__ __forceinline__ float cluster_load(const float* own, int rank) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_address(own, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ int cluster_load(const int32_t* own, int rank) {
+  int v;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(cluster_address(own, rank)) : "memory");
+  return v;
+}
+
+// The two element types: packed arithmetic on pairs, and the number whose low mantissa bits a 4-bit code can be or-ed into
+// (128 + u in bf16, 1024 + u in fp16: both exact, as is the difference of two of them).
+struct Bf16 {
+  using T = __nv_bfloat16;
+  static constexpr uint32_t kBase = 0x43004300u;
+  static __device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+  }
+  static __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+  }
+  static __device__ __forceinline__ float to_float(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
+  static __device__ __forceinline__ uint16_t from_float(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
+  static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  }
+};
+struct Fp16 {
+  using T = __half;
+  static constexpr uint32_t kBase = 0x64006400u;
+  static __device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+  }
+  static __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+  }
+  static __device__ __forceinline__ float to_float(uint16_t v) { return __half2float(__ushort_as_half(v)); }
+  static __device__ __forceinline__ uint16_t from_float(float v) { return __half_as_ushort(__float2half_rn(v)); }
+  static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  }
+};
+
+// Pair i (codes 2i, 2i + 1) of a word, each on top of the base.
+template <class H>
+__device__ __forceinline__ uint32_t code_pair(uint32_t w, int i) {
+  uint32_t d;   // (shifted & mask) | base in one three-input operation
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(w >> (4 * i)), "r"(0x000F000Fu), "r"(H::kBase));
+  return d;
+}
+// The zero point z (8 for a symmetric layer) on top of the base, in both halves.
+template <class H>
+__device__ __forceinline__ uint32_t zero_pair(uint32_t z) {
+  return H::kBase | z | (z << 16);
+}
+
+// Row tiles of `per` rows dealt to units: unit u is tile `tile` of expert e, whose rows are [lo, hi).  Every lane of the calling
+// warp gets the answer; false: there are fewer units.  Offsets are taken as clamped to [0, N] and ascending, whatever they hold.
+struct Unit {
+  int e;
+  int64_t lo, hi;   // the tile's rows
+};
+__device__ __forceinline__ bool find_unit(const Call& c, int64_t u, int per, Unit& out) {
+  if (!c.offsets) {
+    out.e = 0;
+    out.lo = u * per;
+    out.hi = out.lo + per < c.N ? out.lo + per : c.N;
+    return out.lo < c.N;
+  }
+  const int lane = threadIdx.x & 31;
+  int64_t before = 0;
+  for (int e0 = 0; e0 < c.E; e0 += 32) {
+    const int e = e0 + lane;
+    int64_t lo = 0, hi = 0;
+    if (e < c.E) {
+      lo = __ldcg(c.offsets + e);
+      hi = __ldcg(c.offsets + e + 1);
+      lo = lo < 0 ? 0 : (lo > c.N ? c.N : lo);
+      hi = hi < lo ? lo : (hi > c.N ? c.N : hi);
+    }
+    const int mine = static_cast<int>((hi - lo + per - 1) / per);
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += v;
+    }
+    const int total = __shfl_sync(0xffffffffu, upto, 31);
+    if (u < before + total) {
+      const int at = static_cast<int>(u - before);
+      const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
+      const int src = __ffs(past) - 1;
+      const int tile = at - __shfl_sync(0xffffffffu, upto - mine, src);
+      lo = __shfl_sync(0xffffffffu, lo, src);
+      hi = __shfl_sync(0xffffffffu, hi, src);
+      out.e = e0 + src;
+      out.lo = lo + static_cast<int64_t>(tile) * per;
+      out.hi = out.lo + per < hi ? out.lo + per : hi;
+      return true;
+    }
+    before += total;
+  }
+  return false;
+}
+// The most units that N rows on E experts can make: every expert with rows has at most one tile that is not full.
+inline int64_t most_units(const Call& c, int per) {
+  if (!c.offsets) return ceil_div<int64_t>(c.N, per);
+  return (c.N < c.E ? c.N : static_cast<int64_t>(c.E)) + c.N / per;
+}
+
+pipe_status linear_small(const Call& c, bool bf16, cudaStream_t stream);
+
+}  // namespace grp
+}  // namespace pipe

@@ -1,0 +1,94 @@
+// Entry points of the 4-bit layers with group scales: checks of arguments and the choice of a kernel.
+#include "group_common.cuh"
+
+namespace pipe {
+namespace grp {
+
+static pipe_status check_desc(const pipe_group_desc* d) {
+  if (!d) return PIPE_ERR_INVALID_ARG;
+  if (d->experts < 1 || d->experts > PIPE_MAX_EXPERTS || d->out_features < 1 || d->in_features < 1) return PIPE_ERR_INVALID_ARG;
+  if (d->dtype != PIPE_DTYPE_BF16 && d->dtype != PIPE_DTYPE_FP16) return PIPE_ERR_INVALID_ARG;
+  if (d->asymmetric != 0 && d->asymmetric != 1) return PIPE_ERR_INVALID_ARG;
+  if (d->group_size < 1) return PIPE_ERR_INVALID_ARG;
+  if (d->group_size != 32 && d->group_size != 64 && d->group_size != 128) return PIPE_ERR_UNSUPPORTED;
+  if (d->in_features % d->group_size) return PIPE_ERR_SHAPE;
+  return PIPE_OK;
+}
+
+static bool misaligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
+// What both products check alike; fills the call but for its rows.
+static pipe_status check_product(const pipe_group_desc* desc, const void* codes, const void* scales, const uint8_t* zeros, const void* x,
+                                 int64_t T, int64_t ldx, const void* bias, int32_t act, int64_t N, void* y, int64_t ldy, Call* c) {
+  const pipe_status st = check_desc(desc);
+  if (st != PIPE_OK) return st;
+  if (T < 0 || N < 0 || T >= (int64_t{1} << 31) || N >= (int64_t{1} << 31)) return PIPE_ERR_INVALID_ARG;
+  if (act < PIPE_ACT_IDENTITY || act > PIPE_ACT_SIGMOID) return PIPE_ERR_INVALID_ARG;
+  if (!codes || !scales || (zeros != nullptr) != (desc->asymmetric != 0)) return PIPE_ERR_INVALID_ARG;
+  if ((T > 0 && !x) || (N > 0 && !y)) return PIPE_ERR_INVALID_ARG;
+  if (ldx < desc->in_features || ldy < desc->out_features) return PIPE_ERR_INVALID_ARG;
+  if (misaligned(codes, 16) || misaligned(scales, 2) || misaligned(x, 16) || ldx % 8 || misaligned(bias, 2) || misaligned(y, 2))
+    return PIPE_ERR_ALIGNMENT;
+  c->E = desc->experts; c->O = desc->out_features; c->I = desc->in_features; c->g = desc->group_size;
+  c->KB = c->I / 32;
+  c->codes = static_cast<const uint8_t*>(codes);
+  c->scales = scales;
+  c->zeros = zeros;
+  c->x = x; c->T = T; c->ldx = ldx;
+  c->rows = nullptr; c->offsets = nullptr;
+  c->N = N;
+  c->bias = bias;
+  c->act = act;
+  c->y = y; c->ldy = ldy;
+  c->status = nullptr;
+  return PIPE_OK;
+}
+
+static pipe_status product(Call& c, bool bf16, cudaStream_t stream) {
+  if (c.N == 0) return PIPE_OK;
+  c.status = device_status_word();
+  if (!c.status) return PIPE_ERR_CUDA;
+  const pipe_status st = linear_small(c, bf16, stream);
+  if (st == PIPE_OK) take_expansion_mark(stream);
+  return st;
+}
+
+}  // namespace grp
+}  // namespace pipe
+
+using namespace pipe;
+
+extern "C" pipe_status pipe_group_layout(const pipe_group_desc* desc, pipe_group_layout_t* h_out) {
+  const pipe_status st = grp::check_desc(desc);
+  if (st != PIPE_OK) return st;
+  if (!h_out) return PIPE_ERR_INVALID_ARG;
+  const uint64_t rows = static_cast<uint64_t>(desc->experts) * desc->out_features;
+  h_out->groups = desc->in_features / desc->group_size;
+  h_out->codes_bytes = rows * desc->in_features / 2;
+  h_out->scales_bytes = rows * h_out->groups * 2;
+  h_out->zeros_bytes = desc->asymmetric ? rows * h_out->groups : 0;
+  return PIPE_OK;
+}
+
+extern "C" pipe_status pipe_group_linear(const pipe_group_desc* desc, const void* d_codes, const void* d_scales, const uint8_t* d_zeros,
+                                         const void* d_x, int64_t T, int64_t ldx, const void* d_bias, int32_t activation, void* d_y,
+                                         int64_t ldy, void* stream) {
+  grp::Call c;
+  const pipe_status st = grp::check_product(desc, d_codes, d_scales, d_zeros, d_x, T, ldx, d_bias, activation, T, d_y, ldy, &c);
+  if (st != PIPE_OK) return st;
+  if (c.E != 1) return PIPE_ERR_SHAPE;
+  return grp::product(c, desc->dtype == PIPE_DTYPE_BF16, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" pipe_status pipe_expert_linear(const pipe_group_desc* desc, const void* d_codes, const void* d_scales, const uint8_t* d_zeros,
+                                          const void* d_x, int64_t T, int64_t ldx, const int32_t* d_rows, const int32_t* d_offsets,
+                                          int64_t N, const void* d_bias, int32_t activation, void* d_y, int64_t ldy, void* stream) {
+  grp::Call c;
+  const pipe_status st = grp::check_product(desc, d_codes, d_scales, d_zeros, d_x, T, ldx, d_bias, activation, N, d_y, ldy, &c);
+  if (st != PIPE_OK) return st;
+  if (!d_offsets) return PIPE_ERR_INVALID_ARG;
+  if (grp::misaligned(d_offsets, 4) || grp::misaligned(d_rows, 4)) return PIPE_ERR_ALIGNMENT;
+  c.rows = d_rows;
+  c.offsets = d_offsets;
+  return grp::product(c, desc->dtype == PIPE_DTYPE_BF16, static_cast<cudaStream_t>(stream));
+}
