@@ -553,8 +553,9 @@ pipe_status pipe_group_quantize(const pipe_group_desc* desc, const void* d_W, in
 
 /*
  * y[t, o] = h(sigma(sum_i x[t, i] W[o, i] + bias[o])) for a layer of one expert: products with a vector for one token, with a
- * matrix for more.  sums and sigma (PIPE_ACT_*) in binary32.  Codes and activations are multiplied as they are, the scale
- * is applied to a group's binary32 sum.
+ * matrix for more.  sums and sigma (PIPE_ACT_*) in binary32.  Up to 16 tokens codes and activations are multiplied as they are
+ * and the scale is applied to a group's binary32 sum; beyond that, on the tensor cores' operands, s * (code - z) is first
+ * rounded to the layer's type (half a step of it at most, like the activations themselves).
  * d_x: [T, I] pitch ldx, 16-byte aligned, ldx a multiple of 8.  d_bias: [O] or NULL.  d_y: [T, O] pitch ldy.
  * T = 0 is a no-op.  d_y must not overlap the inputs.
  */
@@ -580,7 +581,8 @@ pipe_status pipe_expert_rows(const int32_t* d_choice, int64_t T, int32_t k, int3
  * Ragged sizes, empty experts among them, are read on the device; nothing is copied to the host.  d_x: [T, I] pitch ldx (16-byte
  * aligned, ldx a multiple of 8); d_rows: int32 [N] or NULL; d_offsets: int32 [E+1] ascending; d_bias: [E, O] or NULL; d_y: [N, O]
  * pitch ldy, of which the rows behind d_offsets[E] are left as they were.  N: the rows that d_y and d_rows have room for.  Offsets
- * are taken as clamped to [0, N], and a row index outside [0, T) reads as a row of zeros.  Arithmetic as in pipe_group_linear.
+ * are taken as clamped to [0, N], and a row index outside [0, T) reads as a row of zeros.  Arithmetic as in pipe_group_linear,
+ * with N / E (rounded up) in the place of the tokens.
  */
 pipe_status pipe_expert_linear(const pipe_group_desc* desc, const void* d_codes, const void* d_scales, const uint8_t* d_zeros,
                                const void* d_x, int64_t T, int64_t ldx, const int32_t* d_rows, const int32_t* d_offsets, int64_t N,

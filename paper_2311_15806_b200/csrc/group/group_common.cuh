@@ -171,6 +171,7 @@ inline int64_t most_units(const Call& c, int per) {
 }
 
 pipe_status linear_small(const Call& c, bool bf16, cudaStream_t stream);
+pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream);
 
 }  // namespace grp
 }  // namespace pipe

@@ -48,7 +48,10 @@ static pipe_status product(Call& c, bool bf16, cudaStream_t stream) {
   if (c.N == 0) return PIPE_OK;
   c.status = device_status_word();
   if (!c.status) return PIPE_ERR_CUDA;
-  const pipe_status st = linear_small(c, bf16, stream);
+  // Up to 16 rows (on experts: on average, rounded up) the codes' bytes are what counts; the small kernel holds 16 rows a unit.
+  const int64_t rows = c.offsets ? ceil_div<int64_t>(c.N, c.E) : c.N;
+  pipe_status st = rows > 16 ? linear_tc(c, bf16, stream) : PIPE_ERR_UNSUPPORTED;
+  if (st == PIPE_ERR_UNSUPPORTED) st = linear_small(c, bf16, stream);
   if (st == PIPE_OK) take_expansion_mark(stream);
   return st;
 }
