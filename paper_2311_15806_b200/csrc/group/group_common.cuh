@@ -75,6 +75,11 @@ struct Bf16 {
   }
   static __device__ __forceinline__ float to_float(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
   static __device__ __forceinline__ uint16_t from_float(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+  }
   static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -96,6 +101,11 @@ struct Fp16 {
   }
   static __device__ __forceinline__ float to_float(uint16_t v) { return __half2float(__ushort_as_half(v)); }
   static __device__ __forceinline__ uint16_t from_float(float v) { return __half_as_ushort(__float2half_rn(v)); }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+  }
   static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -114,6 +124,29 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t w, int i) {
 template <class H>
 __device__ __forceinline__ uint32_t zero_pair(uint32_t z) {
   return H::kBase | z | (z << 16);
+}
+
+// sigma of N sums, with SiLU and sigmoid on the approximate exponential and reciprocal (2^-22 and 2^-23 of their values, the
+// exponential's argument rounded: |v| 2^-24): far below half a step of a 16-bit output.  The kind is asked once for all of them:
+// asked per value, unrolled, it took a drain 85 cycles a value.
+template <int N>
+__device__ __forceinline__ void quick_activation(float (&v)[N], int kind) {
+  if (kind == PIPE_ACT_IDENTITY) return;
+  if (kind == PIPE_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = apply_activation(v[i], PIPE_ACT_RELU);
+  } else if (kind == PIPE_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = apply_activation(v[i], PIPE_ACT_GELU);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float e, r;
+      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v[i] * -1.44269504f));
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+      v[i] = kind == PIPE_ACT_SILU ? v[i] * r : r;
+    }
+  }
 }
 
 // Row tiles of `per` rows dealt to units: unit u is tile `tile` of expert e, whose rows are [lo, hi).  Every lane of the calling

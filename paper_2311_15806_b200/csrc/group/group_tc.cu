@@ -1,16 +1,20 @@
 // Products of a 4-bit layer with group scales with many rows, on the tensor cores (pipe_group_linear, pipe_expert_linear).
 //
 // The weights are the A operand: a tile is 128 output channels per CTA (256 over a pair of SMs, cta_group::2) by TN rows of
-// activations.  tcgen05.mma takes A from tensor memory, so the widened weights never pass through shared memory, whose bandwidth
-// the activations need: a thread owns one output channel, reads the 128 codes of a stage (four runs of 16 bytes), subtracts the
-// zero point exactly, multiplies by the scale -- one rounding to the layer's type, the type that the MMA takes its operands in;
-// it costs a product what the rounding of the activations costs it -- and stores 64 columns of tensor memory.  Activations come
-// by tensor copies (rows that are gathered: four rows per copy) in the 128-byte swizzle, codes by bulk copies, each on a ring.
-// Sums are binary32 in tensor memory.  Tiles of 256 rows have one accumulator, narrower ones two, so that the drain of a tile
-// overlaps the next one's products.
-//   warp 0  activations   warp 1  MMA issue, tensor memory   warp 2  codes   warp 3  idle
-//   warps 4-11  two groups that drain accumulators (bias, sigma, rounding, a turn in shared memory to rows of y)
-//   warps 12-19 two groups that widen weights, every other stage each
+// activations.  A thread owns one output channel, reads the 128 codes of a stage (four runs of 16 bytes), subtracts the zero point
+// exactly and multiplies by the scale -- one rounding to the layer's type, the type that the MMA takes its operands in; it costs a
+// product what the rounding of the activations costs it.  Where the widened weights go depends on what bounds the tile:
+//   a pair's tile (TN = 256) has 1024 cycles of products per stage, and its two accumulators take all of tensor memory; the weights
+//     go to shared memory, 128-byte swizzled (in tensor memory, with TN = 192 to make room, a store takes 1100 cycles to complete
+//     between the MMAs, and two slots do not cover that)
+//   one CTA's tile (TN <= 128) reads few activations per weight and would be bound by shared memory; there the weights go to
+//     tensor memory, four slots of 64 columns behind the two accumulators, and never pass through shared memory
+// Activations come by tensor copies in the 128-byte swizzle, codes by bulk copies, each on a ring.  Rows that are gathered come by
+// 16-byte asynchronous copies of two warps (a tensor copy that gathers four rows takes some 75 cycles of an SM, 48 of them a stage).
+// Sums are binary32 in tensor memory, in two accumulators, so that the drain of a tile overlaps the next one's products.
+//   warp 0  activations (gathered: and warp 3)   warp 1  MMA issue, tensor memory   warp 2  codes
+//   warps 4-7   drain accumulators (bias, sigma, rounding, a turn in shared memory to rows of y)
+//   warps 8-15  two groups that widen weights, every other stage each
 // Few tiles: the CTAs of a cluster share a tile's reduction axis and add their sums through distributed shared memory, in order.
 #include "group_common.cuh"
 #include "pipe_tc_common.cuh"
@@ -20,13 +24,13 @@ namespace grp {
 
 using namespace tcc;
 
-constexpr int kTThreads = 640;
+constexpr int kTThreads = 512;
 constexpr int kTStage = 128;         // reduction length of a stage
-constexpr int kTRing = 4;            // stages of activations and of widened weights (64 columns of tensor memory each)
+constexpr int kTMaxRing = 6;         // most stages of activations
 constexpr int kTMaxCodes = 12;       // most stages of codes
+constexpr int kTMaxSmem = 226 * 1024;   // dynamic shared memory (the rest of 227 KiB: barriers)
 constexpr int kTCodeBytes = 128 * kTStage / 2;
 constexpr int kTTurnBytes = 32 * 128 * 2;   // 32 rows of y by 128 channels
-constexpr uint32_t kTAcols = 256;    // tensor memory: accumulators in columns 0-255, widened weights in 256-511
 
 struct TcArgs {
   Call c;
@@ -35,8 +39,9 @@ struct TcArgs {
   int stages;      // ceil(I / 128)
   int split;       // CTAs that share a tile's reduction axis
   int code_depth;
+  int ring;        // stages of activations
   int wide_y;      // rows of y are 16-byte aligned
-  uint32_t off_codes, off_turn, off_table;   // shared memory behind the activations
+  uint32_t off_a, off_codes, off_turn, off_table;   // shared memory behind the activations
 };
 
 __device__ __forceinline__ void tma_pair_2d(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
@@ -45,30 +50,26 @@ __device__ __forceinline__ void tma_pair_2d(uint32_t dst, const CUtensorMap* map
       "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar)
       : "memory");
 }
-template <int CG>
-__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* map, int c0, int4 r, uint32_t bar) {
-  if constexpr (CG == 2)
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w), "r"(bar)
-        : "memory");
-  else
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w), "r"(bar)
-        : "memory");
+// 16 bytes from global to shared memory, past L1; `real` of them (16 or 0), zeros behind.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int real) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real) : "memory");
 }
+template <int N>
+__device__ __forceinline__ void copies_left() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+// A from tensor memory (one CTA), from shared memory (a pair).
 template <int CG>
-__device__ __forceinline__ void mma_f16_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
   if constexpr (CG == 2)
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
         : "memory");
   else
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(static_cast<uint32_t>(a)), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
         : "memory");
 }
 template <int CG>
@@ -84,11 +85,11 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 __device__ __forceinline__ void arrive_lead(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[16]) {
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[4][4]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
-      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
-      "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      "r"(v[0][0]), "r"(v[0][1]), "r"(v[0][2]), "r"(v[0][3]), "r"(v[1][0]), "r"(v[1][1]), "r"(v[1][2]), "r"(v[1][3]),
+      "r"(v[2][0]), "r"(v[2][1]), "r"(v[2][2]), "r"(v[2][3]), "r"(v[3][0]), "r"(v[3][1]), "r"(v[3][2]), "r"(v[3][3])
       : "memory");
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16]) {
@@ -102,7 +103,36 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16]) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[i]);
 }
-__device__ __forceinline__ void group_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
+// 16 lanes by 32 columns: register 4 j + 2 h + i is lane (of the 16) l/4 + 8 h, column 8 j + 2 (l % 4) + i.
+__device__ __forceinline__ void tmem_ld_16x32(uint32_t addr, float (&v)[16]) {
+  uint32_t u[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]),
+        "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+      : "r"(addr)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[i]);
+}
+// Four 8 x 8 blocks of pairs, turned: lane l names the 16 bytes that take column l % 8 of block l / 8.
+__device__ __forceinline__ void turn_store(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+__device__ __forceinline__ void drain_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
+// Eight neighbouring outputs of a row of y, `room` of them inside the layer.
+__device__ __forceinline__ void store_y8(uint16_t* y, const uint4& w, int wide, int room) {
+  if (wide && room >= 8) {
+    *reinterpret_cast<uint4*>(y) = w;
+  } else {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < room) y[k] = static_cast<uint16_t>(u[k >> 1] >> (16 * (k & 1)));
+  }
+}
 
 // Tile t of the launch: its expert, its rows, its first channel.
 struct Tile {
@@ -127,10 +157,15 @@ __device__ __forceinline__ Tile tile_of(const TcArgs& p, const int32_t* first, i
   return r;
 }
 
-template <class H, int CG>
+// KPG: runs of 32 codes per group.  Slots of widened weights: kSlots of 64 columns of tensor memory, or of 32 KiB of shared memory.
+template <int CG>
+constexpr int kSlots = CG == 2 ? 2 : 4;
+constexpr int kTSlotBytes = 128 * kTStage * 2;
+
+template <class H, int CG, int KPG>
 __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_constant__ TcArgs p, const __grid_constant__ CUtensorMap xmap) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bars[3 * kTRing + 2 * kTMaxCodes + 4];
+  __shared__ uint64_t bars[3 * kTMaxRing + 2 * kTMaxCodes + 4];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_s;
   const Call& c = p.c;
@@ -139,7 +174,7 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
   uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
   int32_t* table = reinterpret_cast<int32_t*>(gen + p.off_table);
   const uint32_t bar0 = smem_u32(bars);
-  const uint32_t x_full = bar0, a_full = bar0 + 8 * kTRing, done = bar0 + 16 * kTRing, d_full = bar0 + 24 * kTRing, d_empty = d_full + 16,
+  const uint32_t x_full = bar0, a_full = bar0 + 8 * kTMaxRing, done = bar0 + 16 * kTMaxRing, d_full = bar0 + 24 * kTMaxRing, d_empty = d_full + 16,
                  c_full = d_empty + 16, c_empty = c_full + 8 * kTMaxCodes;
   volatile int* abort_flag = &abort_s;
   const int crank = cluster_rank();
@@ -149,12 +184,13 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
   const int st0 = static_cast<int>(static_cast<int64_t>(p.stages) * part / p.split), st1 = static_cast<int>(static_cast<int64_t>(p.stages) * (part + 1) / p.split);
   const int own_rows = p.TN / CG;                       // activation rows in this CTA's shared memory
   const uint32_t x_bytes = static_cast<uint32_t>(own_rows) * 256u;
-  const int bufs = p.TN <= 128 ? 2 : 1;
+  constexpr uint32_t kAcol = 256;   // one CTA: tensor memory has the accumulators in columns 0-255, widened weights behind
+  const uint32_t ring = p.ring;
 
   if (threadIdx.x == 0) {
     abort_s = 0;
-    for (int s = 0; s < kTRing; ++s) {
-      mbar_init(x_full + 8 * s, 1);
+    for (int s = 0; s < kTMaxRing; ++s) {
+      mbar_init(x_full + 8 * s, c.rows ? 2 * CG : 1);
       mbar_init(a_full + 8 * s, 4 * CG);
       mbar_init(done + 8 * s, 1);
     }
@@ -164,7 +200,7 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(d_full + 8 * b, 1);
-      mbar_init(d_empty + 8 * b, 8 * CG);
+      mbar_init(d_empty + 8 * b, 4 * CG);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -218,46 +254,98 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
   const int most = p.split > 1 ? teams : 0x7fffffff;   // (a cluster that shares the axis does one tile)
   const int tiles = static_cast<int>(all < most ? all : most);
 
-  if (warp == 0) {
+  if (warp == 0 && !c.rows) {
     // ---- activations
+    RingPos rp{0, 0};
     uint32_t it = 0;
     const uint32_t lead = CG == 2 ? cluster_address(bars, 0) : bar0;   // the first CTA's barriers
     bool ok = true;
     for (int64_t t = team; ok && t < tiles; t += teams) {
       const Tile tl = tile_of(p, table, static_cast<int>(t));
       const int row0 = tl.lo + rank * own_rows;
-      for (int st = st0; st < st1; ++st, ++it) {
-        const uint32_t s = it % kTRing, use = it / kTRing;
-        if (!mbar_wait(done + 8 * s, (use & 1) ^ 1, abort_flag, c.status)) { ok = false; break; }
-        const uint32_t full = lead + 8 * s, dst = base + s * x_bytes;
-        if (lane == 0 && rank == 0) mbar_expect_tx(x_full + 8 * s, CG * x_bytes);
+      for (int st = st0; st < st1; ++st, ++it, rp.advance(1, ring)) {
+        if (!mbar_wait(done + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
+        if (lane == 0 && rank == 0) mbar_expect_tx(x_full + 8 * rp.slot, CG * x_bytes);
         __syncwarp();
-        if (!c.rows) {
-          if (lane < 2) {
-            const int col = st * kTStage + 64 * lane;
-            if (CG == 2) tma_pair_2d(dst + lane * (x_bytes / 2), &xmap, col, row0, full);
-            else tma_load_2d(dst + lane * (x_bytes / 2), &xmap, col, row0, full);
-          }
-        } else {
-          for (int q = lane; q < own_rows / 4; q += 32) {
-            int r[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int at = row0 + 4 * q + i;
-              r[i] = at < tl.hi ? __ldcg(c.rows + at) : 0;
-              if (r[i] < 0 || r[i] >= c.T) r[i] = static_cast<int>(c.T);   // outside: zeros
-            }
-            const int4 rr = make_int4(r[0], r[1], r[2], r[3]);
-            tma_gather4<CG>(dst + q * 512, &xmap, st * kTStage, rr, full);
-            tma_gather4<CG>(dst + x_bytes / 2 + q * 512, &xmap, st * kTStage + 64, rr, full);
-          }
+        if (lane < 2) {
+          const uint32_t dst = base + rp.slot * x_bytes + lane * (x_bytes / 2);
+          const int col = st * kTStage + 64 * lane;
+          if (CG == 2) tma_pair_2d(dst, &xmap, col, row0, lead + 8 * rp.slot);
+          else tma_load_2d(dst, &xmap, col, row0, lead + 8 * rp.slot);
         }
         __syncwarp();
       }
     }
-    if (rank == 0 && *abort_flag) drain_ring(x_full, it, kTRing, 20000000ll);
+    if (rank == 0 && *abort_flag) drain_ring(x_full, it, p.ring, 20000000ll);
+  } else if ((warp == 0 || warp == 3) && c.rows) {
+    // ---- activations, gathered: this warp's half of the rows, four rows by 128 bytes per copy instruction.  A stage is handed on
+    // before the one after the next is asked for.
+    constexpr int kMost = 128 / 2 / 4;
+    const int half = own_rows / 2, mine = half / 4;   // copies of this warp per 64 columns
+    const int first = (warp ? half : 0) + (lane >> 3);
+    const uint32_t lead = cluster_address(bars, CG == 2 ? 0 : crank);
+    const uint32_t place = static_cast<uint32_t>(first * 128 + (((lane & 7) ^ (first & 7)) * 16));   // (+ 4 rows: the other half of the atom)
+    RingPos rp{0, 0}, out{0, 0};
+    uint32_t it = 0;
+    bool ok = true;
+    auto hand_on = [&]() {   // the copies of the oldest stage have landed: visible to the tensor core
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) arrive_lead(lead + 8 * out.slot);
+      out.advance(1, ring);
+    };
+    for (int64_t t = team; ok && t < tiles; t += teams) {
+      const Tile tl = tile_of(p, table, static_cast<int>(t));
+      const uint16_t* src[kMost];   // rows behind the tile's: its last one, whose sums are not stored
+      uint32_t none = 0;            // rows whose index lies outside: zeros
+#pragma unroll
+      for (int i = 0; i < kMost; ++i) {
+        const int at = tl.lo + rank * own_rows + first + 4 * i;
+        int64_t r = __ldcg(c.rows + (at < tl.hi ? at : tl.hi - 1));
+        if (r < 0 || r >= c.T) {
+          none |= 1u << i;
+          r = 0;
+        }
+        src[i] = static_cast<const uint16_t*>(c.x) + r * c.ldx + 8 * (lane & 7) + st0 * kTStage;
+      }
+      const bool plain = !__any_sync(0xffffffffu, none != 0);
+      for (int st = st0; st < st1; ++st, ++it, rp.advance(1, ring)) {
+        if (it >= 2) {
+          copies_left<1>();
+          hand_on();
+        }
+        if (!mbar_wait(done + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
+        const uint32_t even = base + rp.slot * x_bytes + place, odd = even ^ 64u;
+        if (plain && (st + 1) * kTStage <= c.I) {
+#pragma unroll
+          for (int i = 0; i < kMost; ++i)
+            if (i < mine) {
+              copy16((i & 1 ? odd : even) + i * 512, src[i], 16);
+              copy16((i & 1 ? odd : even) + x_bytes / 2 + i * 512, src[i] + 64, 16);
+            }
+        } else {
+#pragma unroll 1
+          for (int h = 0; h < 2; ++h) {
+            const bool inside = st * kTStage + 64 * h + 8 * (lane & 7) < c.I;
+#pragma unroll
+            for (int i = 0; i < kMost; ++i)
+              if (i < mine) {
+                const bool real = inside && !((none >> i) & 1);
+                copy16((i & 1 ? odd : even) + h * (x_bytes / 2) + i * 512, real ? src[i] + 64 * h : static_cast<const uint16_t*>(c.x), real ? 16 : 0);
+              }
+          }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) src[i] += kTStage;
+      }
+    }
+    copies_left<0>();
+    if (ok)
+      for (uint32_t n = it >= 2 ? it - 2 : 0; n < it; ++n) hand_on();
   } else if (warp == 2) {
     // ---- codes
+    RingPos rp{0, 0};
     uint32_t it = 0;
     bool ok = true;
     for (int64_t t = team; ok && t < tiles; t += teams) {
@@ -265,16 +353,26 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
       const int o0 = (tl.m * CG + rank) * 128;
       const int rows = c.O - o0 < 128 ? (c.O > o0 ? c.O - o0 : 0) : 128;
       const uint8_t* src = c.codes + (static_cast<int64_t>(tl.e) * c.KB * c.O + o0) * 16;
-      for (int st = st0; st < st1; ++st, ++it) {
-        const uint32_t s = it % p.code_depth, use = it / p.code_depth;
-        if (!mbar_wait(c_empty + 8 * s, (use & 1) ^ 1, abort_flag, c.status)) { ok = false; break; }
+      // this lane's piece of the stage's scales (lanes 0-19, five to a group) or zero points (lanes 20-31, three to a group)
+      const bool is_zero = lane >= 20;
+      const int part_group = is_zero ? (lane - 20) / 3 : lane / 5, part_byte = 64 * (is_zero ? (lane - 20) % 3 : lane % 5);
+      const int run_bytes = is_zero ? rows : 2 * rows;
+      const uint8_t* meta = nullptr;
+      if (rows > 0 && part_group < 4 / KPG && (!is_zero || c.zeros)) {
+        const int64_t at = (static_cast<int64_t>(tl.e) * (c.KB / KPG) + part_group) * c.O + o0;
+        meta = (is_zero ? c.zeros + at : static_cast<const uint8_t*>(c.scales) + 2 * at) + (part_byte < run_bytes ? part_byte : run_bytes - 1);
+      }
+      for (int st = st0; st < st1; ++st, ++it, rp.advance(1, p.code_depth)) {
+        if (!mbar_wait(c_empty + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
         const int runs = c.KB - 4 * st < 4 ? c.KB - 4 * st : 4;
-        if (lane == 0) mbar_expect_tx(c_full + 8 * s, static_cast<uint32_t>(runs * rows * 16));
+        // scales and zero points are read by the threads that use them, one stage ahead: from L2, then
+        if (meta && part_group * KPG < runs) prefetch_l2(meta + static_cast<int64_t>(st) * (4 / KPG) * c.O * (is_zero ? 1 : 2));
+        if (lane == 0) mbar_expect_tx(c_full + 8 * rp.slot, static_cast<uint32_t>(runs * rows * 16));
         __syncwarp();
         if (lane < runs && rows > 0) {
-          const uint32_t dst = base + p.off_codes + s * kTCodeBytes + lane * 2048;
+          const uint32_t dst = base + p.off_codes + rp.slot * kTCodeBytes + lane * 2048;
           asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-                       "l"(src + static_cast<int64_t>(4 * st + lane) * c.O * 16), "r"(rows * 16), "r"(c_full + 8 * s)
+                       "l"(src + static_cast<int64_t>(4 * st + lane) * c.O * 16), "r"(rows * 16), "r"(c_full + 8 * rp.slot)
                        : "memory");
         }
         __syncwarp();
@@ -286,24 +384,29 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
     if (rank == 0) {
       const uint32_t type = H::kBase == Bf16::kBase ? 1u : 0u;
       const uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | (static_cast<uint32_t>(p.TN >> 3) << 17) | (static_cast<uint32_t>(128 * CG >> 4) << 24);
+      RingPos rp{0, 0};
       uint32_t it = 0, n = 0;
       bool ok = true;
       for (int64_t t = team; ok && t < tiles; t += teams, ++n) {
-        const uint32_t buf = n % bufs, use = n / bufs;
+        const uint32_t buf = n & 1, use = n >> 1;
         if (!mbar_wait<true>(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status)) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t d = tmem + buf * 128;
-        for (int st = st0; st < st1; ++st, ++it) {
-          const uint32_t s = it % kTRing, ph = (it / kTRing) & 1;
-          if (!mbar_wait<CG == 2>(x_full + 8 * s, ph, abort_flag, c.status) || !mbar_wait<true>(a_full + 8 * s, ph, abort_flag, c.status)) { ok = false; break; }
+        const uint32_t d = tmem + buf * p.TN;
+        for (int st = st0; st < st1; ++st, ++it, rp.advance(1, ring)) {
+          if (!mbar_wait<true>(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status) || !mbar_wait<true>(a_full + 8 * rp.slot, rp.phase, abort_flag, c.status)) {
+            ok = false;
+            break;
+          }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           if (lane == 0) {
-            const uint32_t a = tmem + kTAcols + s * 64;
-            const uint32_t x = base + s * x_bytes;
+            const uint32_t slot = it & (kSlots<CG> - 1);
+            const uint32_t a = CG == 2 ? base + p.off_a + slot * kTSlotBytes : tmem + kAcol + slot * 64;
+            const uint32_t x = base + rp.slot * x_bytes;
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-              mma_f16_ta<CG>(d, a + 8 * k, smem_desc_sw128(x + (k >> 2) * (x_bytes / 2) + (k & 3) * 32), idesc, st > st0 || k > 0);
-            commit<CG>(done + 8 * s);
+              mma_f16<CG>(d, CG == 2 ? smem_desc_sw128(a + (k >> 2) * (kTSlotBytes / 2) + (k & 3) * 32) : a + 8 * k,
+                          smem_desc_sw128(x + (k >> 2) * (x_bytes / 2) + (k & 3) * 32), idesc, st > st0 || k > 0);
+            commit<CG>(done + 8 * rp.slot);
           }
           __syncwarp();
         }
@@ -311,130 +414,172 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
         __syncwarp();
       }
     }
-  } else if (warp >= 12) {
-    // ---- weights: a thread's channel is its lane of tensor memory
-    const int wg = (warp - 12) >> 2, row = (warp & 3) * 32 + lane;
-    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t lead_a = cluster_address(bars, CG == 2 ? 0 : crank) + 8 * kTRing;
-    const int kpg = c.g >> 5, groups = c.KB / kpg;
-    uint32_t it = 0;
-    bool ok = true;
-    for (int64_t t = team; ok && t < tiles; t += teams) {
+  } else if (warp >= 8) {
+    // ---- weights: a thread's channel is a row of the tile (one CTA: its lane of tensor memory)
+    const uint32_t wg = (warp - 8) >> 2;
+    const int row = (warp & 3) * 32 + lane;
+    const uint32_t lead_a = cluster_address(bars, CG == 2 ? 0 : crank) + 8 * kTMaxRing;
+    const int groups = c.KB / KPG, nst = st1 - st0;
+    const uint32_t total = team < tiles ? static_cast<uint32_t>((tiles - team + teams - 1) / teams) * nst : 0;
+    // the stage whose scales and zero points are fetched next
+    int64_t t = team;
+    int st = st0 + static_cast<int>(wg);
+    const uint16_t* scales = nullptr;
+    const uint8_t* zeros = nullptr;
+    bool here = false;
+    auto open_tile = [&]() {
       const Tile tl = tile_of(p, table, static_cast<int>(t));
       const int o = (tl.m * CG + rank) * 128 + row;
-      const bool here = o < c.O;
-      const int64_t at0 = static_cast<int64_t>(tl.e) * groups * c.O + (here ? o : 0);
-      const uint16_t* scales = static_cast<const uint16_t*>(c.scales) + at0;
-      const uint8_t* zeros = c.zeros ? c.zeros + at0 : nullptr;
-      // scales and zero points of the four runs of a stage (read one of this group's stages ahead)
-      uint32_t sc[4], zp[4];
-      auto fetch = [&](int st) {
+      here = o < c.O;
+      const int64_t at = static_cast<int64_t>(tl.e) * groups * c.O + (here ? o : c.O - 1);
+      scales = static_cast<const uint16_t*>(c.scales) + at;
+      zeros = c.zeros + (c.zeros ? at : 0);
+    };
+    // scales and zero points of a stage's groups; beyond the layer those of its last channel and group, which are not used
+    uint32_t sc[4 / KPG], zp[4 / KPG];
+    auto fetch = [&]() {
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const int kb = 4 * st + b;
-          if (b % kpg == 0) {
-            sc[b] = 0;
-            zp[b] = 8;
-            if (here && st < st1 && kb < c.KB) {
-              const int64_t at = static_cast<int64_t>(kb / kpg) * c.O;
-              sc[b] = __ldcg(scales + at);
-              if (zeros) zp[b] = __ldcg(zeros + at);
-            }
-          } else {
-            sc[b] = sc[b - 1];
-            zp[b] = zp[b - 1];
-          }
+      for (int f = 0; f < 4 / KPG; ++f) {
+        const int group = st * (4 / KPG) + f;
+        const int64_t at = static_cast<int64_t>(group < groups ? group : groups - 1) * c.O;
+        sc[f] = __ldcg(scales + at);
+        if (c.zeros) zp[f] = __ldcg(zeros + at);
+      }
+    };
+    auto settle = [&]() {   // a stage number beyond the tile's is one of the next tile's
+      if (st >= st1) {
+        do {
+          st -= nst;
+          t += teams;
+        } while (st >= st1);
+        if (t < tiles) open_tile();
+      }
+    };
+    if (wg < total) {
+      settle();
+      if (t == team) open_tile();
+      fetch();
+    }
+    // positions of stage it: in the rings of activations (whose barriers are used) and codes; `past`: of stage it - kSlots
+    RingPos rp{0, 0}, cp{0, 0}, past{0, 0};
+    rp.advance(wg, ring);
+    cp.advance(wg, p.code_depth);
+    past.advance(wg, ring);
+    for (uint32_t it = wg; it < total; it += 2) {
+      const int left = c.KB - 4 * st;   // runs of this stage
+      uint32_t s2[4 / KPG], z2[4 / KPG];
+#pragma unroll
+      for (int f = 0; f < 4 / KPG; ++f) {
+        s2[f] = here ? sc[f] * 0x10001u : 0u;
+        z2[f] = zero_pair<H>(c.zeros ? zp[f] : 8u);
+      }
+      if (it + 2 < total) {
+        st += 2;
+        settle();
+        fetch();
+      }
+      if (!mbar_wait(c_full + 8 * cp.slot, cp.phase, abort_flag, c.status)) break;
+      const uint4* src = reinterpret_cast<const uint4*>(gen + p.off_codes + cp.slot * kTCodeBytes) + row;
+      uint4 q[4];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) q[b] = b < left ? src[b * 128] : make_uint4(0, 0, 0, 0);
+      auto widen = [&](int b, int word, uint32_t (&v)[4]) {   // 8 codes of run b
+        const uint32_t w = word == 0 ? q[b].x : (word == 1 ? q[b].y : (word == 2 ? q[b].z : q[b].w));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = H::mul2(H::sub2(code_pair<H>(w, i), z2[b / KPG]), s2[b / KPG]);
+          if (b > 0 && b >= left) v[i] = 0;   // behind the reduction axis
         }
       };
-      int st = st0 + static_cast<int>((it ^ static_cast<uint32_t>(wg)) & 1);
-      it += st - st0;
-      fetch(st);
-      for (; st < st1; st += 2, it += 2) {
-        const uint32_t cs = it % p.code_depth, s = it % kTRing, use = it / kTRing;
-        uint32_t s2[4], z2[4];
+      uint32_t v[4][4][4];   // all of it, before the slot is free: what follows the products of the slot's last stage is the store alone
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          s2[b] = sc[b] | (sc[b] << 16);
-          z2[b] = zero_pair<H>(zp[b]);
-        }
-        fetch(st + 2);
-        if (!mbar_wait(c_full + 8 * cs, (it / p.code_depth) & 1, abort_flag, c.status)) { ok = false; break; }
-        const uint4* src = reinterpret_cast<const uint4*>(gen + p.off_codes + cs * kTCodeBytes) + row;
-        uint4 q[4];
+      for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) q[b] = src[b * 128];
-        if (!mbar_wait(done + 8 * s, (use & 1) ^ 1, abort_flag, c.status)) { ok = false; break; }
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        for (int word = 0; word < 4; ++word) widen(b, word, v[b][word]);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(c_empty + 8 * cp.slot);
+      if (it >= static_cast<uint32_t>(kSlots<CG>)) {
+        if (!mbar_wait(done + 8 * past.slot, past.phase, abort_flag, c.status)) break;
+        past.advance(2, ring);
+      }
+      if constexpr (CG == 2) {
+        uint8_t* to = gen + p.off_a + (it & (kSlots<CG> - 1)) * kTSlotBytes + row * 128;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          uint32_t v[16];
-          const uint32_t w[4] = {q[b].x, q[b].y, q[b].z, q[b].w};
+        for (int b = 0; b < 4; ++b)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = H::mul2(H::sub2(code_pair<H>(w[i >> 2], i & 3), z2[b]), s2[b]);
-          if (4 * st + b >= c.KB) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = 0;
+          for (int word = 0; word < 4; ++word) {
+            const int piece = (4 * (b & 1) + word) ^ (row & 7);
+            *reinterpret_cast<uint4*>(to + (b >> 1) * (kTSlotBytes / 2) + piece * 16) = make_uint4(v[b][word][0], v[b][word][1], v[b][word][2], v[b][word][3]);
           }
-          tmem_st16(tmem + lane_base + kTAcols + s * 64 + b * 16, v);
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(c_empty + 8 * cs);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // visible to the tensor core
+      } else {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t to = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kAcol + (it & (kSlots<CG> - 1)) * 64;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) tmem_st16(to + b * 16, v[b]);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) arrive_lead(lead_a + 8 * s);
       }
-      it -= st - st1;   // the stage count at the tile's end
+      __syncwarp();
+      if (lane == 0) arrive_lead(lead_a + 8 * rp.slot);
+      rp.advance(2, ring);
+      cp.advance(2, p.code_depth);
     }
   } else if (warp >= 4 && p.split == 1) {
     // ---- drain
-    const int wg = (warp - 4) >> 2, row = (warp & 3) * 32 + lane, tid = threadIdx.x - 128 - 128 * wg;
-    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const int q = warp & 3, tid = threadIdx.x - 128;
+    const uint32_t from = tmem + (static_cast<uint32_t>(q * 32) << 16);
     const uint32_t lead_e = cluster_address(bars, CG == 2 ? 0 : crank) + (d_empty - bar0);
-    uint8_t* turn = gen + p.off_turn + wg * 2 * kTTurnBytes;
+    uint8_t* turn = gen + p.off_turn;
+    const int piece = tid & 15, r0 = tid >> 4;
     uint32_t n = 0, chunk = 0;
     for (int64_t t = team; t < tiles; t += teams, ++n) {
       const Tile tl = tile_of(p, table, static_cast<int>(t));
-      const int o0 = (tl.m * CG + rank) * 128, o = o0 + row;
-      const uint32_t buf = n % bufs, use = n / bufs;
-      const float bias = c.bias && o < c.O ? H::to_float(__ldcg(static_cast<const uint16_t*>(c.bias) + static_cast<int64_t>(tl.e) * c.O + o)) : 0.f;
+      const int o0 = (tl.m * CG + rank) * 128;
+      const uint32_t buf = n & 1, use = n >> 1;
+      float bias[4];   // of channels 32 q + lane / 4 + 8 h
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const int o = o0 + 32 * q + 8 * h + (lane >> 2);
+        bias[h] = c.bias && o < c.O ? H::to_float(__ldcg(static_cast<const uint16_t*>(c.bias) + static_cast<int64_t>(tl.e) * c.O + o)) : 0.f;
+      }
+      const int col = o0 + 8 * piece;
+      uint16_t* y = static_cast<uint16_t*>(c.y) + (static_cast<int64_t>(tl.lo) + r0) * c.ldy + col;
       if (!mbar_wait<false, 64>(d_full + 8 * buf, use & 1, abort_flag, c.status)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      for (int n0 = 32 * wg; n0 < p.TN; n0 += 64, ++chunk) {
-        if (tl.lo + n0 >= tl.hi) break;   // (the same for all warps of the group)
+      const int count = tl.hi - tl.lo;   // rows of y, 32 at a time
+      for (int n0 = 0; n0 < count; n0 += 32, ++chunk) {
         uint8_t* to = turn + (chunk & 1) * kTTurnBytes;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float v[16];
-          tmem_ld16(tmem + lane_base + buf * 128 + n0 + 16 * h, v);
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            *reinterpret_cast<uint16_t*>(to + (16 * h + i) * 256 + row * 2) = H::from_float(apply_activation(v[i] + bias, c.act));
+        float v[2][16];   // 16 channels each
+        tmem_ld_16x32(from + buf * p.TN + n0, v[0]);
+        tmem_ld_16x32(from + (16u << 16) + buf * p.TN + n0, v[1]);
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        if (n0 + 32 >= count) {   // the accumulator is read
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) arrive_lead(lead_e + 8 * buf);
         }
-        group_sync(1 + wg);
-        const int col = (tid & 15) * 8;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = (tid >> 4) + 8 * i;
-          const int64_t at = static_cast<int64_t>(tl.lo + n0 + r);
-          if (at < tl.hi && o0 + col < c.O) {
-            const uint4 q = *reinterpret_cast<const uint4*>(to + r * 256 + col * 2);
-            uint16_t* y = static_cast<uint16_t*>(c.y) + at * c.ldy + o0 + col;
-            if (p.wide_y && o0 + col + 8 <= c.O) {
-              *reinterpret_cast<uint4*>(y) = q;
-            } else {
-              const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+        for (int g = 0; g < 2; ++g) {
 #pragma unroll
-              for (int k = 0; k < 8; ++k)
-                if (o0 + col + k < c.O) y[k] = static_cast<uint16_t>(u[k >> 1] >> (16 * (k & 1)));
-            }
+          for (int i = 0; i < 16; ++i) v[g][i] += bias[2 * g + ((i >> 1) & 1)];
+          quick_activation(v[g], c.act);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {   // 8 channels: four blocks of 8 rows; a row's 16-byte pieces lie permuted by its number
+            const int at = (4 * q + 2 * g + h) ^ (lane & 7);
+            turn_store(smem_u32(to) + lane * 256 + at * 16, H::pack(v[g][2 * h], v[g][2 * h + 1]), H::pack(v[g][4 + 2 * h], v[g][5 + 2 * h]),
+                       H::pack(v[g][8 + 2 * h], v[g][9 + 2 * h]), H::pack(v[g][12 + 2 * h], v[g][13 + 2 * h]));
           }
         }
+        drain_sync();
+        uint4 w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const uint4*>(to + (r0 + 8 * i) * 256 + ((piece ^ (r0 & 7)) * 16));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (n0 + r0 + 8 * i < count && col < c.O) store_y8(y + static_cast<int64_t>(8 * i) * c.ldy, w[i], p.wide_y, c.O - col);
+        y += 32 * c.ldy;
       }
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) arrive_lead(lead_e + 8 * buf);
     }
   }
   if (CG == 1 && p.split > 1) {
@@ -444,12 +589,12 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
     const bool work = team < tiles;
     const Tile tl = work ? tile_of(p, table, team) : Tile{};
     bool ok = work;
-    if (work && warp >= 4 && warp < 12) {
-      const int wg = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
+    if (work && warp >= 4 && warp < 8) {
+      const int row = (warp & 3) * 32 + lane;
       ok = mbar_wait<false, 64>(d_full, 0, abort_flag, c.status);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       if (ok)
-        for (int n0 = 16 * wg; n0 < p.TN; n0 += 32) {
+        for (int n0 = 0; n0 < p.TN; n0 += 16) {
           float v[16];
           tmem_ld16(tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + n0, v);
           asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
@@ -478,22 +623,14 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
             for (int j = 0; j < 4; ++j) v[k + j] += w[j];
           }
         }
-        uint32_t u[4];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const int o = o0 + col + k;
           if (c.bias && o < c.O) v[k] += H::to_float(__ldcg(static_cast<const uint16_t*>(c.bias) + static_cast<int64_t>(tl.e) * c.O + o));
-          const uint32_t h = H::from_float(apply_activation(v[k], c.act));
-          u[k >> 1] = k & 1 ? u[k >> 1] | (h << 16) : h;
         }
-        uint16_t* y = static_cast<uint16_t*>(c.y) + at * c.ldy + o0 + col;
-        if (p.wide_y && o0 + col + 8 <= c.O) {
-          *reinterpret_cast<uint4*>(y) = make_uint4(u[0], u[1], u[2], u[3]);
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            if (o0 + col + k < c.O) y[k] = static_cast<uint16_t>(u[k >> 1] >> (16 * (k & 1)));
-        }
+        quick_activation(v, c.act);
+        store_y8(static_cast<uint16_t*>(c.y) + at * c.ldy + o0 + col,
+                 make_uint4(H::pack(v[0], v[1]), H::pack(v[2], v[3]), H::pack(v[4], v[5]), H::pack(v[6], v[7])), p.wide_y, c.O - o0 - col);
       }
     }
     cluster_sync();   // no CTA leaves while another reads its sums
@@ -506,6 +643,11 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
     if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
+}
+
+template <class H, int CG>
+static auto tc_kernel(int g) {
+  return g == 32 ? group_tc_kernel<H, CG, 1> : (g == 64 ? group_tc_kernel<H, CG, 2> : group_tc_kernel<H, CG, 4>);
 }
 
 static bool make_x_map(CUtensorMap* map, const Call& c, int box_rows) {
@@ -524,9 +666,9 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   TcArgs p;
   p.c = c;
   const int64_t rows = c.offsets ? ceil_div<int64_t>(c.N, c.E) : c.N;
-  // 256 rows are a pair's tile: one CTA alone has no room for four stages of them
   const int cg = rows > 128 && c.O > 128 ? 2 : 1;
   p.TN = rows <= 32 ? 32 : (rows <= 64 ? 64 : (cg == 1 ? 128 : 256));
+  p.ring = cg == 1 ? 4 : 3;
   p.stages = ceil_div(c.I, kTStage);
   const int64_t units = most_units(c, p.TN);
   p.mtiles = ceil_div(c.O, 128 * cg);
@@ -537,19 +679,19 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   int64_t teams = p.split > 1 ? tiles : kPlanSMs / cg;
   if (teams > tiles) teams = tiles;
   p.wide_y = !(reinterpret_cast<uintptr_t>(c.y) & 15) && c.ldy % 8 == 0;
-  const int x_bytes = kTRing * (p.TN / cg) * 256;
+  const int x_bytes = p.ring * (p.TN / cg) * 256, a_bytes = cg == 2 ? 2 * kTSlotBytes : 0, turn = p.split > 1 ? 0 : 2 * kTTurnBytes;
   const int table = (3 * c.E + 1) * 4;
-  p.off_codes = x_bytes;
-  const int turn = p.split > 1 ? 0 : 4 * kTTurnBytes;
-  const int room = 220 * 1024 - 1024 - x_bytes - turn - table;
+  const int room = kTMaxSmem - 1024 - x_bytes - a_bytes - turn - table;
   p.code_depth = room / kTCodeBytes < kTMaxCodes ? room / kTCodeBytes : kTMaxCodes;
   if (p.code_depth < 2) return PIPE_ERR_UNSUPPORTED;
+  p.off_a = x_bytes;
+  p.off_codes = p.off_a + a_bytes;
   p.off_turn = p.off_codes + p.code_depth * kTCodeBytes;
   p.off_table = p.off_turn + turn;
   const int smem = 1024 + static_cast<int>(p.off_table) + table;
   CUtensorMap map;
-  if (!make_x_map(&map, c, c.rows ? 1 : p.TN / cg)) return PIPE_ERR_CUDA;
-  void (*k)(TcArgs, CUtensorMap) = bf16 ? (cg == 2 ? group_tc_kernel<Bf16, 2> : group_tc_kernel<Bf16, 1>) : (cg == 2 ? group_tc_kernel<Fp16, 2> : group_tc_kernel<Fp16, 1>);
+  if (!make_x_map(&map, c, p.TN / cg)) return PIPE_ERR_CUDA;
+  void (*k)(TcArgs, CUtensorMap) = bf16 ? (cg == 2 ? tc_kernel<Bf16, 2>(c.g) : tc_kernel<Bf16, 1>(c.g)) : (cg == 2 ? tc_kernel<Fp16, 2>(c.g) : tc_kernel<Fp16, 1>(c.g));
   if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return PIPE_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
