@@ -10,7 +10,11 @@
 //   one CTA's tile (TN <= 128) reads few activations per weight and would be bound by shared memory; there the weights go to
 //     tensor memory, four slots of 64 columns behind the two accumulators, and never pass through shared memory
 // Activations come by tensor copies in the 128-byte swizzle, codes by bulk copies, each on a ring.  Rows that are gathered come by
-// 16-byte asynchronous copies of two warps (a tensor copy that gathers four rows takes some 75 cycles of an SM, 48 of them a stage).
+// 16-byte asynchronous copies of two warps (a tensor copy that gathers four rows takes some 75 cycles of an SM, 64 of them a stage).
+// The fence that makes ordinary writes visible to the tensor core waits for everything the thread has in flight, so the threads
+// that fence have nothing else in flight: scales and zero points come with the codes (read by the widening threads themselves, one
+// stage ahead, they cost 1400 cycles a stage), and gathered rows are fenced by the warp that issues the MMAs, the pair's second
+// CTA's by the same warp there, which has nothing to issue.
 // Sums are binary32 in tensor memory, in two accumulators, so that the drain of a tile overlaps the next one's products.
 //   warp 0  activations (gathered: and warp 3)   warp 1  MMA issue, tensor memory   warp 2  codes
 //   warps 4-7   drain accumulators (bias, sigma, rounding, a turn in shared memory to rows of y)
@@ -29,7 +33,9 @@ constexpr int kTStage = 128;         // reduction length of a stage
 constexpr int kTMaxRing = 6;         // most stages of activations
 constexpr int kTMaxCodes = 12;       // most stages of codes
 constexpr int kTMaxSmem = 226 * 1024;   // dynamic shared memory (the rest of 227 KiB: barriers)
-constexpr int kTCodeBytes = 128 * kTStage / 2;
+constexpr int kTCodeBytes = 128 * kTStage / 2;            // of a stage
+constexpr int kTMetaBytes = 4 * 128 * 3;                  // its scales and zero points: at most four groups of 128 channels
+constexpr int kTCodeSlot = kTCodeBytes + kTMetaBytes;
 constexpr int kTTurnBytes = 32 * 128 * 2;   // 32 rows of y by 128 channels
 
 struct TcArgs {
@@ -41,6 +47,7 @@ struct TcArgs {
   int code_depth;
   int ring;        // stages of activations
   int wide_y;      // rows of y are 16-byte aligned
+  int wide_meta;   // scales of four channels are 8-byte, zero points 4-byte aligned
   uint32_t off_a, off_codes, off_turn, off_table;   // shared memory behind the activations
 };
 
@@ -54,10 +61,15 @@ __device__ __forceinline__ void tma_pair_2d(uint32_t dst, const CUtensorMap* map
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, int real) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real) : "memory");
 }
-template <int N>
-__device__ __forceinline__ void copies_left() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+template <int BYTES>   // 8 or 4
+__device__ __forceinline__ void copy_small(uint32_t dst, const void* src, bool real) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(real ? BYTES : 0) : "memory");
 }
+// An arrival on the barrier once this thread's copies so far have landed (one of the arrivals that the barrier is set to).
+__device__ __forceinline__ void arrive_behind_copies(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // A from tensor memory (one CTA), from shared memory (a pair).
 template <int CG>
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
@@ -119,7 +131,6 @@ __device__ __forceinline__ void tmem_ld_16x32(uint32_t addr, float (&v)[16]) {
 __device__ __forceinline__ void turn_store(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 __device__ __forceinline__ void drain_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 // Eight neighbouring outputs of a row of y, `room` of them inside the layer.
@@ -165,7 +176,7 @@ constexpr int kTSlotBytes = 128 * kTStage * 2;
 template <class H, int CG, int KPG>
 __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_constant__ TcArgs p, const __grid_constant__ CUtensorMap xmap) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bars[3 * kTMaxRing + 2 * kTMaxCodes + 4];
+  __shared__ uint64_t bars[4 * kTMaxRing + 2 * kTMaxCodes + 4];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_s;
   const Call& c = p.c;
@@ -175,7 +186,7 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
   int32_t* table = reinterpret_cast<int32_t*>(gen + p.off_table);
   const uint32_t bar0 = smem_u32(bars);
   const uint32_t x_full = bar0, a_full = bar0 + 8 * kTMaxRing, done = bar0 + 16 * kTMaxRing, d_full = bar0 + 24 * kTMaxRing, d_empty = d_full + 16,
-                 c_full = d_empty + 16, c_empty = c_full + 8 * kTMaxCodes;
+                 c_full = d_empty + 16, c_empty = c_full + 8 * kTMaxCodes, x_peer = c_empty + 8 * kTMaxCodes;
   volatile int* abort_flag = &abort_s;
   const int crank = cluster_rank();
   const int rank = CG == 2 ? crank : 0;                 // within the pair
@@ -190,12 +201,13 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
   if (threadIdx.x == 0) {
     abort_s = 0;
     for (int s = 0; s < kTMaxRing; ++s) {
-      mbar_init(x_full + 8 * s, c.rows ? 2 * CG : 1);
+      mbar_init(x_full + 8 * s, c.rows ? 64 : 1);
+      mbar_init(x_peer + 8 * s, 1);
       mbar_init(a_full + 8 * s, 4 * CG);
       mbar_init(done + 8 * s, 1);
     }
     for (int s = 0; s < kTMaxCodes; ++s) {
-      mbar_init(c_full + 8 * s, 1);
+      mbar_init(c_full + 8 * s, 33);
       mbar_init(c_empty + 8 * s, 4);
     }
     for (int b = 0; b < 2; ++b) {
@@ -278,22 +290,13 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
     }
     if (rank == 0 && *abort_flag) drain_ring(x_full, it, p.ring, 20000000ll);
   } else if ((warp == 0 || warp == 3) && c.rows) {
-    // ---- activations, gathered: this warp's half of the rows, four rows by 128 bytes per copy instruction.  A stage is handed on
-    // before the one after the next is asked for.
+    // ---- activations, gathered: this warp's half of the rows, four rows by 128 bytes per copy instruction
     constexpr int kMost = 128 / 2 / 4;
     const int half = own_rows / 2, mine = half / 4;   // copies of this warp per 64 columns
     const int first = (warp ? half : 0) + (lane >> 3);
-    const uint32_t lead = cluster_address(bars, CG == 2 ? 0 : crank);
     const uint32_t place = static_cast<uint32_t>(first * 128 + (((lane & 7) ^ (first & 7)) * 16));   // (+ 4 rows: the other half of the atom)
-    RingPos rp{0, 0}, out{0, 0};
-    uint32_t it = 0;
+    RingPos rp{0, 0};
     bool ok = true;
-    auto hand_on = [&]() {   // the copies of the oldest stage have landed: visible to the tensor core
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) arrive_lead(lead + 8 * out.slot);
-      out.advance(1, ring);
-    };
     for (int64_t t = team; ok && t < tiles; t += teams) {
       const Tile tl = tile_of(p, table, static_cast<int>(t));
       const uint16_t* src[kMost];   // rows behind the tile's: its last one, whose sums are not stored
@@ -309,11 +312,7 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
         src[i] = static_cast<const uint16_t*>(c.x) + r * c.ldx + 8 * (lane & 7) + st0 * kTStage;
       }
       const bool plain = !__any_sync(0xffffffffu, none != 0);
-      for (int st = st0; st < st1; ++st, ++it, rp.advance(1, ring)) {
-        if (it >= 2) {
-          copies_left<1>();
-          hand_on();
-        }
+      for (int st = st0; st < st1; ++st, rp.advance(1, ring)) {
         if (!mbar_wait(done + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
         const uint32_t even = base + rp.slot * x_bytes + place, odd = even ^ 64u;
         if (plain && (st + 1) * kTStage <= c.I) {
@@ -335,14 +334,12 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
               }
           }
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        arrive_behind_copies(x_full + 8 * rp.slot);
 #pragma unroll
         for (int i = 0; i < kMost; ++i) src[i] += kTStage;
       }
     }
-    copies_left<0>();
-    if (ok)
-      for (uint32_t n = it >= 2 ? it - 2 : 0; n < it; ++n) hand_on();
+    copies_done();
   } else if (warp == 2) {
     // ---- codes
     RingPos rp{0, 0};
@@ -353,31 +350,48 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
       const int o0 = (tl.m * CG + rank) * 128;
       const int rows = c.O - o0 < 128 ? (c.O > o0 ? c.O - o0 : 0) : 128;
       const uint8_t* src = c.codes + (static_cast<int64_t>(tl.e) * c.KB * c.O + o0) * 16;
-      // this lane's piece of the stage's scales (lanes 0-19, five to a group) or zero points (lanes 20-31, three to a group)
-      const bool is_zero = lane >= 20;
-      const int part_group = is_zero ? (lane - 20) / 3 : lane / 5, part_byte = 64 * (is_zero ? (lane - 20) % 3 : lane % 5);
-      const int run_bytes = is_zero ? rows : 2 * rows;
-      const uint8_t* meta = nullptr;
-      if (rows > 0 && part_group < 4 / KPG && (!is_zero || c.zeros)) {
-        const int64_t at = (static_cast<int64_t>(tl.e) * (c.KB / KPG) + part_group) * c.O + o0;
-        meta = (is_zero ? c.zeros + at : static_cast<const uint8_t*>(c.scales) + 2 * at) + (part_byte < run_bytes ? part_byte : run_bytes - 1);
-      }
+      // scales and zero points: this lane's four channels
+      const int groups = c.KB / KPG, o4 = o0 + 4 * lane;
+      const int64_t meta0 = static_cast<int64_t>(tl.e) * groups * c.O;
+      const uint16_t* scales = static_cast<const uint16_t*>(c.scales) + meta0;
+      const uint8_t* zeros = c.zeros + (c.zeros ? meta0 : 0);
       for (int st = st0; st < st1; ++st, ++it, rp.advance(1, p.code_depth)) {
         if (!mbar_wait(c_empty + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
         const int runs = c.KB - 4 * st < 4 ? c.KB - 4 * st : 4;
-        // scales and zero points are read by the threads that use them, one stage ahead: from L2, then
-        if (meta && part_group * KPG < runs) prefetch_l2(meta + static_cast<int64_t>(st) * (4 / KPG) * c.O * (is_zero ? 1 : 2));
+        const uint32_t at = p.off_codes + rp.slot * kTCodeSlot;
         if (lane == 0) mbar_expect_tx(c_full + 8 * rp.slot, static_cast<uint32_t>(runs * rows * 16));
         __syncwarp();
         if (lane < runs && rows > 0) {
-          const uint32_t dst = base + p.off_codes + rp.slot * kTCodeBytes + lane * 2048;
+          const uint32_t dst = base + at + lane * 2048;
           asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                        "l"(src + static_cast<int64_t>(4 * st + lane) * c.O * 16), "r"(rows * 16), "r"(c_full + 8 * rp.slot)
                        : "memory");
         }
         __syncwarp();
+        // (a scale of zero behind the layer's channels and groups: what is widened there is zero, whatever its codes)
+#pragma unroll
+        for (int f = 0; f < 4 / KPG; ++f) {
+          const int group = st * (4 / KPG) + f;
+          const int64_t from = static_cast<int64_t>(group) * c.O + o4;
+          const uint32_t to_s = at + kTCodeBytes + f * 256 + lane * 8, to_z = at + kTCodeBytes + 1024 + f * 128 + lane * 4;
+          if (p.wide_meta) {
+            const bool real = group < groups && o4 < c.O;
+            copy_small<8>(base + to_s, real ? scales + from : scales, real);
+            if (c.zeros) copy_small<4>(base + to_z, real ? zeros + from : zeros, real);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const bool real = group < groups && o4 + i < c.O;
+              *reinterpret_cast<uint16_t*>(gen + to_s + 2 * i) = real ? __ldcg(scales + from + i) : 0;
+              if (c.zeros) gen[to_z + i] = real ? __ldcg(zeros + from + i) : 0;
+            }
+          }
+        }
+        if (p.wide_meta) arrive_behind_copies(c_full + 8 * rp.slot);
+        else mbar_arrive(c_full + 8 * rp.slot);
       }
     }
+    copies_done();
     if (*abort_flag) drain_ring(c_full, it, p.code_depth, 20000000ll);
   } else if (warp == 1) {
     // ---- MMA
@@ -393,10 +407,12 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + buf * p.TN;
         for (int st = st0; st < st1; ++st, ++it, rp.advance(1, ring)) {
-          if (!mbar_wait<true>(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status) || !mbar_wait<true>(a_full + 8 * rp.slot, rp.phase, abort_flag, c.status)) {
+          if (!mbar_wait<true>(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status) ||
+              (CG == 2 && c.rows && !mbar_wait<true>(x_peer + 8 * rp.slot, rp.phase, abort_flag, c.status)) || !mbar_wait<true>(a_full + 8 * rp.slot, rp.phase, abort_flag, c.status)) {
             ok = false;
             break;
           }
+          if (c.rows) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           if (lane == 0) {
             const uint32_t slot = it & (kSlots<CG> - 1);
@@ -413,89 +429,51 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
         if (ok && lane == 0) commit<CG>(d_full + 8 * buf);
         __syncwarp();
       }
+    } else if (c.rows) {
+      // the pair's second CTA: its gathered rows, made visible to the tensor core, are reported to the first
+      const uint32_t lead = cluster_address(bars, 0) + (x_peer - bar0);
+      RingPos rp{0, 0};
+      bool ok = true;
+      for (int64_t t = team; ok && t < tiles; t += teams)
+        for (int st = st0; st < st1; ++st, rp.advance(1, ring)) {
+          if (!mbar_wait(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status)) { ok = false; break; }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) arrive_lead(lead + 8 * rp.slot);
+        }
     }
   } else if (warp >= 8) {
     // ---- weights: a thread's channel is a row of the tile (one CTA: its lane of tensor memory)
     const uint32_t wg = (warp - 8) >> 2;
     const int row = (warp & 3) * 32 + lane;
     const uint32_t lead_a = cluster_address(bars, CG == 2 ? 0 : crank) + 8 * kTMaxRing;
-    const int groups = c.KB / KPG, nst = st1 - st0;
-    const uint32_t total = team < tiles ? static_cast<uint32_t>((tiles - team + teams - 1) / teams) * nst : 0;
-    // the stage whose scales and zero points are fetched next
-    int64_t t = team;
-    int st = st0 + static_cast<int>(wg);
-    const uint16_t* scales = nullptr;
-    const uint8_t* zeros = nullptr;
-    bool here = false;
-    auto open_tile = [&]() {
-      const Tile tl = tile_of(p, table, static_cast<int>(t));
-      const int o = (tl.m * CG + rank) * 128 + row;
-      here = o < c.O;
-      const int64_t at = static_cast<int64_t>(tl.e) * groups * c.O + (here ? o : c.O - 1);
-      scales = static_cast<const uint16_t*>(c.scales) + at;
-      zeros = c.zeros + (c.zeros ? at : 0);
-    };
-    // scales and zero points of a stage's groups; beyond the layer those of its last channel and group, which are not used
-    uint32_t sc[4 / KPG], zp[4 / KPG];
-    auto fetch = [&]() {
-#pragma unroll
-      for (int f = 0; f < 4 / KPG; ++f) {
-        const int group = st * (4 / KPG) + f;
-        const int64_t at = static_cast<int64_t>(group < groups ? group : groups - 1) * c.O;
-        sc[f] = __ldcg(scales + at);
-        if (c.zeros) zp[f] = __ldcg(zeros + at);
-      }
-    };
-    auto settle = [&]() {   // a stage number beyond the tile's is one of the next tile's
-      if (st >= st1) {
-        do {
-          st -= nst;
-          t += teams;
-        } while (st >= st1);
-        if (t < tiles) open_tile();
-      }
-    };
-    if (wg < total) {
-      settle();
-      if (t == team) open_tile();
-      fetch();
-    }
+    const uint32_t total = team < tiles ? static_cast<uint32_t>((tiles - team + teams - 1) / teams) * (st1 - st0) : 0;
     // positions of stage it: in the rings of activations (whose barriers are used) and codes; `past`: of stage it - kSlots
     RingPos rp{0, 0}, cp{0, 0}, past{0, 0};
     rp.advance(wg, ring);
     cp.advance(wg, p.code_depth);
     past.advance(wg, ring);
     for (uint32_t it = wg; it < total; it += 2) {
-      const int left = c.KB - 4 * st;   // runs of this stage
+      if (!mbar_wait(c_full + 8 * cp.slot, cp.phase, abort_flag, c.status)) break;
+      const uint8_t* at = gen + p.off_codes + cp.slot * kTCodeSlot;
+      uint4 q[4];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) q[b] = reinterpret_cast<const uint4*>(at)[b * 128 + row];
       uint32_t s2[4 / KPG], z2[4 / KPG];
 #pragma unroll
       for (int f = 0; f < 4 / KPG; ++f) {
-        s2[f] = here ? sc[f] * 0x10001u : 0u;
-        z2[f] = zero_pair<H>(c.zeros ? zp[f] : 8u);
+        s2[f] = *reinterpret_cast<const uint16_t*>(at + kTCodeBytes + f * 256 + row * 2) * 0x10001u;
+        z2[f] = zero_pair<H>(c.zeros ? at[kTCodeBytes + 1024 + f * 128 + row] : 8u);
       }
-      if (it + 2 < total) {
-        st += 2;
-        settle();
-        fetch();
-      }
-      if (!mbar_wait(c_full + 8 * cp.slot, cp.phase, abort_flag, c.status)) break;
-      const uint4* src = reinterpret_cast<const uint4*>(gen + p.off_codes + cp.slot * kTCodeBytes) + row;
-      uint4 q[4];
-#pragma unroll
-      for (int b = 0; b < 4; ++b) q[b] = b < left ? src[b * 128] : make_uint4(0, 0, 0, 0);
-      auto widen = [&](int b, int word, uint32_t (&v)[4]) {   // 8 codes of run b
-        const uint32_t w = word == 0 ? q[b].x : (word == 1 ? q[b].y : (word == 2 ? q[b].z : q[b].w));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[i] = H::mul2(H::sub2(code_pair<H>(w, i), z2[b / KPG]), s2[b / KPG]);
-          if (b > 0 && b >= left) v[i] = 0;   // behind the reduction axis
-        }
-      };
       uint32_t v[4][4][4];   // all of it, before the slot is free: what follows the products of the slot's last stage is the store alone
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int word = 0; word < 4; ++word) widen(b, word, v[b][word]);
+        for (int word = 0; word < 4; ++word) {
+          const uint32_t w = word == 0 ? q[b].x : (word == 1 ? q[b].y : (word == 2 ? q[b].z : q[b].w));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[b][word][i] = H::mul2(H::sub2(code_pair<H>(w, i), z2[b / KPG]), s2[b / KPG]);
+        }
       __syncwarp();
       if (lane == 0) mbar_arrive(c_empty + 8 * cp.slot);
       if (it >= static_cast<uint32_t>(kSlots<CG>)) {
@@ -679,14 +657,15 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   int64_t teams = p.split > 1 ? tiles : kPlanSMs / cg;
   if (teams > tiles) teams = tiles;
   p.wide_y = !(reinterpret_cast<uintptr_t>(c.y) & 15) && c.ldy % 8 == 0;
+  p.wide_meta = c.O % 4 == 0 && !(reinterpret_cast<uintptr_t>(c.scales) & 7) && !(reinterpret_cast<uintptr_t>(c.zeros) & 3);
   const int x_bytes = p.ring * (p.TN / cg) * 256, a_bytes = cg == 2 ? 2 * kTSlotBytes : 0, turn = p.split > 1 ? 0 : 2 * kTTurnBytes;
   const int table = (3 * c.E + 1) * 4;
   const int room = kTMaxSmem - 1024 - x_bytes - a_bytes - turn - table;
-  p.code_depth = room / kTCodeBytes < kTMaxCodes ? room / kTCodeBytes : kTMaxCodes;
+  p.code_depth = room / kTCodeSlot < kTMaxCodes ? room / kTCodeSlot : kTMaxCodes;
   if (p.code_depth < 2) return PIPE_ERR_UNSUPPORTED;
   p.off_a = x_bytes;
   p.off_codes = p.off_a + a_bytes;
-  p.off_turn = p.off_codes + p.code_depth * kTCodeBytes;
+  p.off_turn = p.off_codes + p.code_depth * kTCodeSlot;
   p.off_table = p.off_turn + turn;
   const int smem = 1024 + static_cast<int>(p.off_table) + table;
   CUtensorMap map;
