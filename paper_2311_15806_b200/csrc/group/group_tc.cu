@@ -93,9 +93,11 @@ __device__ __forceinline__ void commit(uint32_t bar) {
   else
     mma_commit(bar);
 }
-// Arrival on a barrier of the pair's first CTA (an address of the cluster's window).
+// Arrival on a barrier of the pair's first CTA (an address of the cluster's window).  Release at CTA scope is enough: what it
+// reports is read by this SM's own tensor core, to which the fences before the arrival have made it visible.  (At cluster scope the
+// arrival waits some 2000 cycles for everything that the thread has written.)
 __device__ __forceinline__ void arrive_lead(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[4][4]) {
   asm volatile(
