@@ -176,7 +176,8 @@ constexpr int kSlots = CG == 2 ? 2 : 4;
 constexpr int kTSlotBytes = 128 * kTStage * 2;
 
 template <class H, int CG, int KPG>
-__global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_constant__ TcArgs p, const __grid_constant__ CUtensorMap xmap) {
+__global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_constant__ TcArgs p, const __grid_constant__ CUtensorMap xmap,
+                                                                     const __grid_constant__ CUtensorMap cmap) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bars[4 * kTMaxRing + 2 * kTMaxCodes + 4];
   __shared__ uint32_t tmem_slot;
@@ -350,47 +351,40 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
     for (int64_t t = team; ok && t < tiles; t += teams) {
       const Tile tl = tile_of(p, table, static_cast<int>(t));
       const int o0 = (tl.m * CG + rank) * 128;
-      const int rows = c.O - o0 < 128 ? (c.O > o0 ? c.O - o0 : 0) : 128;
-      const uint8_t* src = c.codes + (static_cast<int64_t>(tl.e) * c.KB * c.O + o0) * 16;
-      // scales and zero points: this lane's four channels
       const int groups = c.KB / KPG, o4 = o0 + 4 * lane;
-      const int64_t meta0 = static_cast<int64_t>(tl.e) * groups * c.O;
+      const int64_t meta0 = (static_cast<int64_t>(tl.e) * groups + st0 * (4 / KPG)) * c.O + o4;   // scales and zero points: this lane's four channels
       const uint16_t* scales = static_cast<const uint16_t*>(c.scales) + meta0;
       const uint8_t* zeros = c.zeros + (c.zeros ? meta0 : 0);
       for (int st = st0; st < st1; ++st, ++it, rp.advance(1, p.code_depth)) {
         if (!mbar_wait(c_empty + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
-        const int runs = c.KB - 4 * st < 4 ? c.KB - 4 * st : 4;
-        const uint32_t at = p.off_codes + rp.slot * kTCodeSlot;
-        if (lane == 0) mbar_expect_tx(c_full + 8 * rp.slot, static_cast<uint32_t>(runs * rows * 16));
-        __syncwarp();
-        if (lane < runs && rows > 0) {
-          const uint32_t dst = base + at + lane * 2048;
-          asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-                       "l"(src + static_cast<int64_t>(4 * st + lane) * c.O * 16), "r"(rows * 16), "r"(c_full + 8 * rp.slot)
-                       : "memory");
+        const uint32_t at = p.off_codes + rp.slot * kTCodeSlot, to_s = at + kTCodeBytes + lane * 8, to_z = at + kTCodeBytes + 1024 + lane * 4;
+        if (lane == 0) {
+          mbar_expect_tx(c_full + 8 * rp.slot, kTCodeBytes);
+          tma_load_2d(base + at, &cmap, 2 * o0, tl.e * c.KB + 4 * st, c_full + 8 * rp.slot);
         }
         __syncwarp();
         // (a scale of zero behind the layer's channels and groups: what is widened there is zero, whatever its codes)
+        if (p.wide_meta) {
 #pragma unroll
-        for (int f = 0; f < 4 / KPG; ++f) {
-          const int group = st * (4 / KPG) + f;
-          const int64_t from = static_cast<int64_t>(group) * c.O + o4;
-          const uint32_t to_s = at + kTCodeBytes + f * 256 + lane * 8, to_z = at + kTCodeBytes + 1024 + f * 128 + lane * 4;
-          if (p.wide_meta) {
-            const bool real = group < groups && o4 < c.O;
-            copy_small<8>(base + to_s, real ? scales + from : scales, real);
-            if (c.zeros) copy_small<4>(base + to_z, real ? zeros + from : zeros, real);
-          } else {
+          for (int f = 0; f < 4 / KPG; ++f) {
+            const bool real = st * (4 / KPG) + f < groups && o4 < c.O;
+            copy_small<8>(base + to_s + f * 256, real ? scales + static_cast<int64_t>(f) * c.O : c.scales, real);
+            if (c.zeros) copy_small<4>(base + to_z + f * 128, real ? zeros + static_cast<int64_t>(f) * c.O : c.zeros, real);
+          }
+          arrive_behind_copies(c_full + 8 * rp.slot);
+        } else {
+#pragma unroll 1
+          for (int f = 0; f < 4 / KPG; ++f)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const bool real = group < groups && o4 + i < c.O;
-              *reinterpret_cast<uint16_t*>(gen + to_s + 2 * i) = real ? __ldcg(scales + from + i) : 0;
-              if (c.zeros) gen[to_z + i] = real ? __ldcg(zeros + from + i) : 0;
+              const bool real = st * (4 / KPG) + f < groups && o4 + i < c.O;
+              *reinterpret_cast<uint16_t*>(gen + to_s + f * 256 + 2 * i) = real ? __ldcg(scales + static_cast<int64_t>(f) * c.O + i) : 0;
+              if (c.zeros) gen[to_z + f * 128 + i] = real ? __ldcg(zeros + static_cast<int64_t>(f) * c.O + i) : 0;
             }
-          }
+          mbar_arrive(c_full + 8 * rp.slot);
         }
-        if (p.wide_meta) arrive_behind_copies(c_full + 8 * rp.slot);
-        else mbar_arrive(c_full + 8 * rp.slot);
+        scales += (4 / KPG) * static_cast<int64_t>(c.O);
+        if (c.zeros) zeros += (4 / KPG) * static_cast<int64_t>(c.O);
       }
     }
     copies_done();
@@ -630,15 +624,14 @@ static auto tc_kernel(int g) {
   return g == 32 ? group_tc_kernel<H, CG, 1> : (g == 64 ? group_tc_kernel<H, CG, 2> : group_tc_kernel<H, CG, 4>);
 }
 
-static bool make_x_map(CUtensorMap* map, const Call& c, int box_rows) {
+static bool encode_2d(CUtensorMap* map, CUtensorMapDataType type, const void* base, uint64_t cols, uint64_t rows, uint64_t pitch_bytes, int box_cols,
+                      int box_rows, CUtensorMapSwizzle swizzle) {
   EncodeFn fn = encode_fn();
   if (!fn) return false;
-  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(c.I), static_cast<cuuint64_t>(c.T > 0 ? c.T : 1)};
-  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(c.ldx) * 2};
-  const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)};
-  const cuuint32_t estr[2] = {1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(c.x), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint64_t dims[2] = {cols, rows}, strides[1] = {pitch_bytes};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
+  return fn(map, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
@@ -670,9 +663,14 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   p.off_turn = p.off_codes + p.code_depth * kTCodeSlot;
   p.off_table = p.off_turn + turn;
   const int smem = 1024 + static_cast<int>(p.off_table) + table;
-  CUtensorMap map;
-  if (!make_x_map(&map, c, p.TN / cg)) return PIPE_ERR_CUDA;
-  void (*k)(TcArgs, CUtensorMap) = bf16 ? (cg == 2 ? tc_kernel<Bf16, 2>(c.g) : tc_kernel<Bf16, 1>(c.g)) : (cg == 2 ? tc_kernel<Fp16, 2>(c.g) : tc_kernel<Fp16, 1>(c.g));
+  // activations: boxes of 64 columns; codes: rows of O runs of 16 bytes, taken as 8-byte elements, a stage's four runs of 128 channels in
+  // one box (behind the layer's channels zeros; behind an expert's last run the next one's, which meet scales of zero)
+  CUtensorMap xmap, cmap;
+  if (!encode_2d(&xmap, CU_TENSOR_MAP_DATA_TYPE_UINT16, c.x, c.I, c.T, static_cast<uint64_t>(c.ldx) * 2, 64, p.TN / cg, CU_TENSOR_MAP_SWIZZLE_128B) ||
+      !encode_2d(&cmap, CU_TENSOR_MAP_DATA_TYPE_FLOAT64, c.codes, static_cast<uint64_t>(c.O) * 2, static_cast<uint64_t>(c.E) * c.KB,
+                 static_cast<uint64_t>(c.O) * 16, 256, 4, CU_TENSOR_MAP_SWIZZLE_NONE))
+    return PIPE_ERR_CUDA;
+  void (*k)(TcArgs, CUtensorMap, CUtensorMap) = bf16 ? (cg == 2 ? tc_kernel<Bf16, 2>(c.g) : tc_kernel<Bf16, 1>(c.g)) : (cg == 2 ? tc_kernel<Fp16, 2>(c.g) : tc_kernel<Fp16, 1>(c.g));
   if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return PIPE_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
@@ -687,7 +685,7 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  if (cudaLaunchKernelEx(&cfg, k, p, map) != cudaSuccess) return PIPE_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, k, p, xmap, cmap) != cudaSuccess) return PIPE_ERR_CUDA;
   count_launch(1);
   return launch_status();
 }
