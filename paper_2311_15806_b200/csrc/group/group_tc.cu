@@ -3,12 +3,9 @@
 // The weights are the A operand: a tile is 128 output channels per CTA (256 over a pair of SMs, cta_group::2) by TN rows of
 // activations.  A thread owns one output channel, reads the 128 codes of a stage (four runs of 16 bytes), subtracts the zero point
 // exactly and multiplies by the scale -- one rounding to the layer's type, the type that the MMA takes its operands in; it costs a
-// product what the rounding of the activations costs it.  Where the widened weights go depends on what bounds the tile:
-//   a pair's tile (TN = 256) has 1024 cycles of products per stage, and its two accumulators take all of tensor memory; the weights
-//     go to shared memory, 128-byte swizzled (in tensor memory, with TN = 192 to make room, a store takes 1100 cycles to complete
-//     between the MMAs, and two slots do not cover that)
-//   one CTA's tile (TN <= 128) reads few activations per weight and would be bound by shared memory; there the weights go to
-//     tensor memory, four slots of 64 columns behind the two accumulators, and never pass through shared memory
+// product what the rounding of the activations costs it -- and stores them, 128-byte swizzled, as the tile's A operand.  (In tensor
+// memory, which tcgen05.mma takes A from as well, they need no shared-memory bandwidth, but there an MMA takes some 150 cycles
+// whatever its width: 1250 cycles a stage at TN = 128 against 875 of shared-memory traffic.)
 // Activations come by tensor copies in the 128-byte swizzle, codes by bulk copies, each on a ring.  Rows that are gathered come by
 // 16-byte asynchronous copies of two warps (a tensor copy that gathers four rows takes some 75 cycles of an SM, 64 of them a stage).
 // The fence that makes ordinary writes visible to the tensor core waits for everything the thread has in flight, so the threads
@@ -35,6 +32,7 @@ constexpr int kTMaxCodes = 12;       // most stages of codes
 constexpr int kTMaxSmem = 226 * 1024;   // dynamic shared memory (the rest of 227 KiB: barriers)
 constexpr int kTCodeBytes = 128 * kTStage / 2;            // of a stage
 constexpr int kTMetaBytes = 4 * 128 * 3;                  // its scales and zero points: at most four groups of 128 channels
+constexpr int kTSlotBytes = 128 * kTStage * 2;            // widened weights of a stage
 constexpr int kTCodeSlot = kTCodeBytes + kTMetaBytes;
 constexpr int kTTurnBytes = 32 * 128 * 2;   // 32 rows of y by 128 channels
 
@@ -46,6 +44,7 @@ struct TcArgs {
   int split;       // CTAs that share a tile's reduction axis
   int code_depth;
   int ring;        // stages of activations
+  int slots;       // stages of widened weights, at most `ring`
   int wide_y;      // rows of y are 16-byte aligned
   int wide_meta;   // scales of four channels are 8-byte, zero points 4-byte aligned
   uint32_t off_a, off_codes, off_turn, off_table;   // shared memory behind the activations
@@ -70,7 +69,6 @@ __device__ __forceinline__ void arrive_behind_copies(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-// A from tensor memory (one CTA), from shared memory (a pair).
 template <int CG>
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
   if constexpr (CG == 2)
@@ -81,7 +79,7 @@ __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint
   else
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(static_cast<uint32_t>(a)), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
         : "memory");
 }
 template <int CG>
@@ -98,13 +96,6 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 // arrival waits some 2000 cycles for everything that the thread has written.)
 __device__ __forceinline__ void arrive_lead(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[4][4]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
-      "r"(v[0][0]), "r"(v[0][1]), "r"(v[0][2]), "r"(v[0][3]), "r"(v[1][0]), "r"(v[1][1]), "r"(v[1][2]), "r"(v[1][3]),
-      "r"(v[2][0]), "r"(v[2][1]), "r"(v[2][2]), "r"(v[2][3]), "r"(v[3][0]), "r"(v[3][1]), "r"(v[3][2]), "r"(v[3][3])
-      : "memory");
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16]) {
   uint32_t u[16];
@@ -170,11 +161,7 @@ __device__ __forceinline__ Tile tile_of(const TcArgs& p, const int32_t* first, i
   return r;
 }
 
-// KPG: runs of 32 codes per group.  Slots of widened weights: kSlots of 64 columns of tensor memory, or of 32 KiB of shared memory.
-template <int CG>
-constexpr int kSlots = CG == 2 ? 2 : 4;
-constexpr int kTSlotBytes = 128 * kTStage * 2;
-
+// KPG: runs of 32 codes per group.
 template <class H, int CG, int KPG>
 __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_constant__ TcArgs p, const __grid_constant__ CUtensorMap xmap,
                                                                      const __grid_constant__ CUtensorMap cmap) {
@@ -198,7 +185,6 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
   const int st0 = static_cast<int>(static_cast<int64_t>(p.stages) * part / p.split), st1 = static_cast<int>(static_cast<int64_t>(p.stages) * (part + 1) / p.split);
   const int own_rows = p.TN / CG;                       // activation rows in this CTA's shared memory
   const uint32_t x_bytes = static_cast<uint32_t>(own_rows) * 256u;
-  constexpr uint32_t kAcol = 256;   // one CTA: tensor memory has the accumulators in columns 0-255, widened weights behind
   const uint32_t ring = p.ring;
 
   if (threadIdx.x == 0) {
@@ -394,15 +380,15 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
     if (rank == 0) {
       const uint32_t type = H::kBase == Bf16::kBase ? 1u : 0u;
       const uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | (static_cast<uint32_t>(p.TN >> 3) << 17) | (static_cast<uint32_t>(128 * CG >> 4) << 24);
-      RingPos rp{0, 0};
-      uint32_t it = 0, n = 0;
+      RingPos rp{0, 0}, wp{0, 0};
+      uint32_t n = 0;
       bool ok = true;
       for (int64_t t = team; ok && t < tiles; t += teams, ++n) {
         const uint32_t buf = n & 1, use = n >> 1;
         if (!mbar_wait<true>(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status)) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + buf * p.TN;
-        for (int st = st0; st < st1; ++st, ++it, rp.advance(1, ring)) {
+        for (int st = st0; st < st1; ++st, rp.advance(1, ring), wp.advance(1, p.slots)) {
           if (!mbar_wait<true>(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status) ||
               (CG == 2 && c.rows && !mbar_wait<true>(x_peer + 8 * rp.slot, rp.phase, abort_flag, c.status)) || !mbar_wait<true>(a_full + 8 * rp.slot, rp.phase, abort_flag, c.status)) {
             ok = false;
@@ -411,12 +397,11 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
           if (c.rows) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           if (lane == 0) {
-            const uint32_t slot = it & (kSlots<CG> - 1);
-            const uint32_t a = CG == 2 ? base + p.off_a + slot * kTSlotBytes : tmem + kAcol + slot * 64;
+            const uint32_t a = base + p.off_a + wp.slot * kTSlotBytes;
             const uint32_t x = base + rp.slot * x_bytes;
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-              mma_f16<CG>(d, CG == 2 ? smem_desc_sw128(a + (k >> 2) * (kTSlotBytes / 2) + (k & 3) * 32) : a + 8 * k,
+              mma_f16<CG>(d, smem_desc_sw128(a + (k >> 2) * (kTSlotBytes / 2) + (k & 3) * 32),
                           smem_desc_sw128(x + (k >> 2) * (x_bytes / 2) + (k & 3) * 32), idesc, st > st0 || k > 0);
             commit<CG>(done + 8 * rp.slot);
           }
@@ -439,16 +424,17 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
         }
     }
   } else if (warp >= 8) {
-    // ---- weights: a thread's channel is a row of the tile (one CTA: its lane of tensor memory)
+    // ---- weights: a thread's channel is a row of the tile
     const uint32_t wg = (warp - 8) >> 2;
     const int row = (warp & 3) * 32 + lane;
     const uint32_t lead_a = cluster_address(bars, CG == 2 ? 0 : crank) + 8 * kTMaxRing;
     const uint32_t total = team < tiles ? static_cast<uint32_t>((tiles - team + teams - 1) / teams) * (st1 - st0) : 0;
-    // positions of stage it: in the rings of activations (whose barriers are used) and codes; `past`: of stage it - kSlots
-    RingPos rp{0, 0}, cp{0, 0}, past{0, 0};
+    // positions of stage it in the rings of activations (whose barriers are used), codes and widened weights; past: of stage it - slots
+    RingPos rp{0, 0}, cp{0, 0}, wp{0, 0}, past{0, 0};
     rp.advance(wg, ring);
     cp.advance(wg, p.code_depth);
-    past.advance(wg, ring);
+    wp.advance(wg, p.slots);
+    past.advance((p.slots & 1) ^ wg, ring);   // (the first stage of this group that waits: slots + this)
     for (uint32_t it = wg; it < total; it += 2) {
       if (!mbar_wait(c_full + 8 * cp.slot, cp.phase, abort_flag, c.status)) break;
       const uint8_t* at = gen + p.off_codes + cp.slot * kTCodeSlot;
@@ -472,32 +458,24 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
         }
       __syncwarp();
       if (lane == 0) mbar_arrive(c_empty + 8 * cp.slot);
-      if (it >= static_cast<uint32_t>(kSlots<CG>)) {
+      if (it >= static_cast<uint32_t>(p.slots)) {
         if (!mbar_wait(done + 8 * past.slot, past.phase, abort_flag, c.status)) break;
         past.advance(2, ring);
       }
-      if constexpr (CG == 2) {
-        uint8_t* to = gen + p.off_a + (it & (kSlots<CG> - 1)) * kTSlotBytes + row * 128;
+      uint8_t* to = gen + p.off_a + wp.slot * kTSlotBytes + row * 128;
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+      for (int b = 0; b < 4; ++b)
 #pragma unroll
-          for (int word = 0; word < 4; ++word) {
-            const int piece = (4 * (b & 1) + word) ^ (row & 7);
-            *reinterpret_cast<uint4*>(to + (b >> 1) * (kTSlotBytes / 2) + piece * 16) = make_uint4(v[b][word][0], v[b][word][1], v[b][word][2], v[b][word][3]);
-          }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // visible to the tensor core
-      } else {
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t to = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kAcol + (it & (kSlots<CG> - 1)) * 64;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) tmem_st16(to + b * 16, v[b]);
-        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      }
+        for (int word = 0; word < 4; ++word) {
+          const int piece = (4 * (b & 1) + word) ^ (row & 7);
+          *reinterpret_cast<uint4*>(to + (b >> 1) * (kTSlotBytes / 2) + piece * 16) = make_uint4(v[b][word][0], v[b][word][1], v[b][word][2], v[b][word][3]);
+        }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // visible to the tensor core
       __syncwarp();
       if (lane == 0) arrive_lead(lead_a + 8 * rp.slot);
       rp.advance(2, ring);
       cp.advance(2, p.code_depth);
+      wp.advance(2, p.slots);
     }
   } else if (warp >= 4 && p.split == 1) {
     // ---- drain
@@ -639,13 +617,13 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   TcArgs p;
   p.c = c;
   const int64_t rows = c.offsets ? ceil_div<int64_t>(c.N, c.E) : c.N;
-  const int cg = rows > 128 && c.O > 128 ? 2 : 1;
-  p.TN = rows <= 32 ? 32 : (rows <= 64 ? 64 : (cg == 1 ? 128 : 256));
-  p.ring = cg == 1 ? 4 : 3;
-  p.stages = ceil_div(c.I, kTStage);
+  p.TN = rows <= 32 ? 32 : (rows <= 64 ? 64 : (rows <= 128 || c.O <= 128 ? 128 : 256));
   const int64_t units = most_units(c, p.TN);
+  const int cg = c.O > 128 && units * ceil_div(c.O, 128) > kPlanSMs ? 2 : 1;
+  if (cg == 1 && p.TN == 256) p.TN = 128;
+  p.stages = ceil_div(c.I, kTStage);
   p.mtiles = ceil_div(c.O, 128 * cg);
-  const int64_t tiles = units * p.mtiles;
+  const int64_t tiles = most_units(c, p.TN) * p.mtiles;
   p.split = 1;
   if (cg == 1)
     while (p.split < 8 && tiles * p.split * 2 <= kPlanSMs && p.stages >= 4 * p.split) p.split *= 2;
@@ -653,7 +631,10 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   if (teams > tiles) teams = tiles;
   p.wide_y = !(reinterpret_cast<uintptr_t>(c.y) & 15) && c.ldy % 8 == 0;
   p.wide_meta = c.O % 4 == 0 && !(reinterpret_cast<uintptr_t>(c.scales) & 7) && !(reinterpret_cast<uintptr_t>(c.zeros) & 3);
-  const int x_bytes = p.ring * (p.TN / cg) * 256, a_bytes = cg == 2 ? 2 * kTSlotBytes : 0, turn = p.split > 1 ? 0 : 2 * kTTurnBytes;
+  const int own = p.TN / cg;
+  p.ring = own >= 128 ? 3 : 4;
+  p.slots = own >= 128 ? 2 : 3;
+  const int x_bytes = p.ring * own * 256, a_bytes = p.slots * kTSlotBytes, turn = p.split > 1 ? 0 : 2 * kTTurnBytes;
   const int table = (3 * c.E + 1) * 4;
   const int room = kTMaxSmem - 1024 - x_bytes - a_bytes - turn - table;
   p.code_depth = room / kTCodeSlot < kTMaxCodes ? room / kTCodeSlot : kTMaxCodes;

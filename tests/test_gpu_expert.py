@@ -109,6 +109,16 @@ def test_experts_over_layer_sizes(O, I, g, counts):
     _expert(3, O, I, g, "fp16", True, counts, 29, False, True, B.ACT_RELU, O + 1, ldx=I + 8, ldy=O + 3)
 
 
+@pytest.mark.parametrize("gather", [False, True])
+@pytest.mark.parametrize("E,O,mean", [(64, 401, 20), (64, 400, 40), (32, 514, 100), (12, 1100, 300), (9, 2051, 260)])
+def test_experts_with_more_tiles_than_sms(E, O, mean, gather):
+    """Enough tiles for pairs of SMs and for several tiles each, at every tile width; experts without rows among them."""
+    gen = _gen(E + O)
+    counts = [0 if e % 7 == 3 else int(v) for e, v in enumerate(torch.randint(1, 2 * mean, (E,), generator=gen))]
+    _expert(E, O, 160, 32, "bf16", O % 2 == 0, counts, 333, gather, True, B.ACT_SILU, O)
+    _expert(E, O, 256, 128, "fp16", O % 2 == 1, counts, 333, gather, False, B.ACT_IDENTITY, O + 1)
+
+
 def test_more_experts_than_a_warp_looks_at():
     gen = _gen(3)
     counts = torch.randint(0, 3, (1024,), generator=gen).tolist()

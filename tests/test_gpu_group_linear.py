@@ -154,6 +154,12 @@ def test_linear_long_reduction_and_many_channels(T):
     _linear(11008, 128, 128, T, "bf16", True, False, B.ACT_IDENTITY, 4)
 
 
+@pytest.mark.parametrize("O,I,g,T", [(11008, 256, 64, 700), (2500, 640, 128, 2049), (130, 96, 32, 20001), (5003, 352, 32, 1000)])
+def test_linear_with_more_tiles_than_sms(O, I, g, T):
+    _linear(O, I, g, T, "bf16", False, True, B.ACT_IDENTITY, O)
+    _linear(O, I, g, T, "fp16", True, False, B.ACT_SIGMOID, O + 1)
+
+
 @pytest.mark.parametrize("T", [4, 100])
 def test_a_token_that_is_not_finite_stays_alone(T):
     gen = _gen(9)
