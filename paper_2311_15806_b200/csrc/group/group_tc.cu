@@ -124,6 +124,13 @@ __device__ __forceinline__ void tmem_ld_16x32(uint32_t addr, float (&v)[16]) {
 __device__ __forceinline__ void turn_store(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
+// One lane of a converged warp, in the form that the compiler knows as one thread of a uniform warp: asked by its lane number
+// instead, the thread that issues the MMAs takes 1150 cycles for a stage of any width.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t pred;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(pred));
+  return pred != 0;
+}
 __device__ __forceinline__ void drain_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 // Eight neighbouring outputs of a row of y, `room` of them inside the layer.
@@ -266,13 +273,15 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
       const int row0 = tl.lo + rank * own_rows;
       for (int st = st0; st < st1; ++st, ++it, rp.advance(1, ring)) {
         if (!mbar_wait(done + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
-        if (lane == 0 && rank == 0) mbar_expect_tx(x_full + 8 * rp.slot, CG * x_bytes);
-        __syncwarp();
-        if (lane < 2) {
-          const uint32_t dst = base + rp.slot * x_bytes + lane * (x_bytes / 2);
-          const int col = st * kTStage + 64 * lane;
-          if (CG == 2) tma_pair_2d(dst, &xmap, col, row0, lead + 8 * rp.slot);
-          else tma_load_2d(dst, &xmap, col, row0, lead + 8 * rp.slot);
+        if (elect_one()) {
+          if (rank == 0) mbar_expect_tx(x_full + 8 * rp.slot, CG * x_bytes);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t dst = base + rp.slot * x_bytes + h * (x_bytes / 2);
+            const int col = st * kTStage + 64 * h;
+            if (CG == 2) tma_pair_2d(dst, &xmap, col, row0, lead + 8 * rp.slot);
+            else tma_load_2d(dst, &xmap, col, row0, lead + 8 * rp.slot);
+          }
         }
         __syncwarp();
       }
@@ -344,7 +353,7 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
       for (int st = st0; st < st1; ++st, ++it, rp.advance(1, p.code_depth)) {
         if (!mbar_wait(c_empty + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
         const uint32_t at = p.off_codes + rp.slot * kTCodeSlot, to_s = at + kTCodeBytes + lane * 8, to_z = at + kTCodeBytes + 1024 + lane * 4;
-        if (lane == 0) {
+        if (elect_one()) {
           mbar_expect_tx(c_full + 8 * rp.slot, kTCodeBytes);
           tma_load_2d(base + at, &cmap, 2 * o0, tl.e * c.KB + 4 * st, c_full + 8 * rp.slot);
         }
@@ -385,18 +394,18 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
       bool ok = true;
       for (int64_t t = team; ok && t < tiles; t += teams, ++n) {
         const uint32_t buf = n & 1, use = n >> 1;
-        if (!mbar_wait<true>(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status)) break;
+        if (!mbar_wait(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status)) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + buf * p.TN;
         for (int st = st0; st < st1; ++st, rp.advance(1, ring), wp.advance(1, p.slots)) {
-          if (!mbar_wait<true>(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status) ||
-              (CG == 2 && c.rows && !mbar_wait<true>(x_peer + 8 * rp.slot, rp.phase, abort_flag, c.status)) || !mbar_wait<true>(a_full + 8 * rp.slot, rp.phase, abort_flag, c.status)) {
+          if (!mbar_wait(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status) ||
+              (CG == 2 && c.rows && !mbar_wait(x_peer + 8 * rp.slot, rp.phase, abort_flag, c.status)) || !mbar_wait(a_full + 8 * rp.slot, rp.phase, abort_flag, c.status)) {
             ok = false;
             break;
           }
           if (c.rows) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          if (lane == 0) {
+          if (elect_one()) {
             const uint32_t a = base + p.off_a + wp.slot * kTSlotBytes;
             const uint32_t x = base + rp.slot * x_bytes;
 #pragma unroll
@@ -407,7 +416,7 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
           }
           __syncwarp();
         }
-        if (ok && lane == 0) commit<CG>(d_full + 8 * buf);
+        if (ok && elect_one()) commit<CG>(d_full + 8 * buf);
         __syncwarp();
       }
     } else if (c.rows) {
