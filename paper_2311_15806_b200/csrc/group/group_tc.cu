@@ -3,9 +3,12 @@
 // The weights are the A operand: a tile is 128 output channels per CTA (256 over a pair of SMs, cta_group::2) by TN rows of
 // activations.  A thread owns one output channel, reads the 128 codes of a stage (four runs of 16 bytes), subtracts the zero point
 // exactly and multiplies by the scale -- one rounding to the layer's type, the type that the MMA takes its operands in; it costs a
-// product what the rounding of the activations costs it -- and stores them, 128-byte swizzled, as the tile's A operand.  (In tensor
-// memory, which tcgen05.mma takes A from as well, they need no shared-memory bandwidth, but there an MMA takes some 150 cycles
-// whatever its width: 1250 cycles a stage at TN = 128 against 875 of shared-memory traffic.)
+// product what the rounding of the activations costs it.  Where the widened weights go depends on the tile's width:
+//   TN = 256 (a pair's) has 1024 cycles of products per stage, and its two accumulators take all of tensor memory; the weights go to
+//     shared memory, 128-byte swizzled, by two groups of four warps
+//   TN <= 128 has half of that or less, and its 112 KB of shared-memory traffic a stage would be the bound; there the weights go to
+//     tensor memory, which tcgen05.mma takes A from as well: four slots of 64 columns behind the two accumulators, one to each of four
+//     groups of warps
 // Activations come by tensor copies in the 128-byte swizzle, codes by bulk copies, each on a ring.  Rows that are gathered come by
 // 16-byte asynchronous copies of two warps (a tensor copy that gathers four rows takes some 75 cycles of an SM, 64 of them a stage).
 // The fence that makes ordinary writes visible to the tensor core waits for everything the thread has in flight, so the threads
@@ -15,7 +18,7 @@
 // Sums are binary32 in tensor memory, in two accumulators, so that the drain of a tile overlaps the next one's products.
 //   warp 0  activations (gathered: and warp 3)   warp 1  MMA issue, tensor memory   warp 2  codes
 //   warps 4-7   drain accumulators (bias, sigma, rounding, a turn in shared memory to rows of y)
-//   warps 8-15  two groups that widen weights, every other stage each
+//   warps 8-    groups that widen weights, stages in turn
 // Few tiles: the CTAs of a cluster share a tile's reduction axis and add their sums through distributed shared memory, in order.
 #include "group_common.cuh"
 #include "pipe_tc_common.cuh"
@@ -25,7 +28,11 @@ namespace grp {
 
 using namespace tcc;
 
-constexpr int kTThreads = 512;
+template <bool TA>
+constexpr int kTWideners = TA ? 4 : 2;   // groups of four warps; TA: widened weights in tensor memory
+template <bool TA>
+constexpr int kTThreads = 256 + 128 * kTWideners<TA>;
+constexpr uint32_t kTAcol = 256;         // their columns
 constexpr int kTStage = 128;         // reduction length of a stage
 constexpr int kTMaxRing = 6;         // most stages of activations
 constexpr int kTMaxCodes = 12;       // most stages of codes
@@ -43,8 +50,7 @@ struct TcArgs {
   int stages;      // ceil(I / 128)
   int split;       // CTAs that share a tile's reduction axis
   int code_depth;
-  int ring;        // stages of activations
-  int slots;       // stages of widened weights, at most `ring`
+  int ring;        // stages of activations, at least the groups of wideners
   int wide_y;      // rows of y are 16-byte aligned
   int wide_meta;   // scales of four channels are 8-byte, zero points 4-byte aligned
   uint32_t off_a, off_codes, off_turn, off_table;   // shared memory behind the activations
@@ -69,12 +75,22 @@ __device__ __forceinline__ void arrive_behind_copies(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-template <int CG>
+template <int CG, bool TA>   // a: columns of tensor memory (TA) or a descriptor
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-  if constexpr (CG == 2)
+  if constexpr (CG == 2 && TA)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(static_cast<uint32_t>(a)), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
+        : "memory");
+  else if constexpr (CG == 2)
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
+        : "memory");
+  else if constexpr (TA)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(static_cast<uint32_t>(a)), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
         : "memory");
   else
     asm volatile(
@@ -96,6 +112,13 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 // arrival waits some 2000 cycles for everything that the thread has written.)
 __device__ __forceinline__ void arrive_lead(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[4][4]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
+      "r"(v[0][0]), "r"(v[0][1]), "r"(v[0][2]), "r"(v[0][3]), "r"(v[1][0]), "r"(v[1][1]), "r"(v[1][2]), "r"(v[1][3]),
+      "r"(v[2][0]), "r"(v[2][1]), "r"(v[2][2]), "r"(v[2][3]), "r"(v[3][0]), "r"(v[3][1]), "r"(v[3][2]), "r"(v[3][3])
+      : "memory");
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16]) {
   uint32_t u[16];
@@ -169,8 +192,8 @@ __device__ __forceinline__ Tile tile_of(const TcArgs& p, const int32_t* first, i
 }
 
 // KPG: runs of 32 codes per group.
-template <class H, int CG, int KPG>
-__global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_constant__ TcArgs p, const __grid_constant__ CUtensorMap xmap,
+template <class H, int CG, int KPG, bool TA>
+__global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid_constant__ TcArgs p, const __grid_constant__ CUtensorMap xmap,
                                                                      const __grid_constant__ CUtensorMap cmap) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bars[4 * kTMaxRing + 2 * kTMaxCodes + 4];
@@ -224,7 +247,7 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
   grid_wait();
   grid_release();
   // the units of every expert: rows (clamped as find_unit does), tiles, then a prefix over the experts
-  for (int e = threadIdx.x; e < c.E; e += kTThreads) {
+  for (int e = threadIdx.x; e < c.E; e += kTThreads<TA>) {
     int64_t lo = 0, hi = c.N;
     if (c.offsets) {
       lo = __ldcg(c.offsets + e);
@@ -359,8 +382,15 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
         }
         __syncwarp();
         // (a scale of zero behind the layer's channels and groups: what is widened there is zero, whatever its codes)
-        if (p.wide_meta) {
+        if (p.wide_meta && o0 + 128 <= c.O && (st + 1) * (4 / KPG) <= groups) {
 #pragma unroll
+          for (int f = 0; f < 4 / KPG; ++f) {
+            copy_small<8>(base + to_s + f * 256, scales + static_cast<int64_t>(f) * c.O, true);
+            if (c.zeros) copy_small<4>(base + to_z + f * 128, zeros + static_cast<int64_t>(f) * c.O, true);
+          }
+          arrive_behind_copies(c_full + 8 * rp.slot);
+        } else if (p.wide_meta) {
+#pragma unroll 1
           for (int f = 0; f < 4 / KPG; ++f) {
             const bool real = st * (4 / KPG) + f < groups && o4 < c.O;
             copy_small<8>(base + to_s + f * 256, real ? scales + static_cast<int64_t>(f) * c.O : c.scales, real);
@@ -397,7 +427,7 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
         if (!mbar_wait(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status)) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + buf * p.TN;
-        for (int st = st0; st < st1; ++st, rp.advance(1, ring), wp.advance(1, p.slots)) {
+        for (int st = st0; st < st1; ++st, rp.advance(1, ring), wp.advance(1, kTWideners<TA>)) {
           if (!mbar_wait(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status) ||
               (CG == 2 && c.rows && !mbar_wait(x_peer + 8 * rp.slot, rp.phase, abort_flag, c.status)) || !mbar_wait(a_full + 8 * rp.slot, rp.phase, abort_flag, c.status)) {
             ok = false;
@@ -406,12 +436,12 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
           if (c.rows) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           if (elect_one()) {
-            const uint32_t a = base + p.off_a + wp.slot * kTSlotBytes;
+            const uint32_t a = TA ? tmem + kTAcol + wp.slot * 64 : base + p.off_a + wp.slot * kTSlotBytes;
             const uint32_t x = base + rp.slot * x_bytes;
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-              mma_f16<CG>(d, smem_desc_sw128(a + (k >> 2) * (kTSlotBytes / 2) + (k & 3) * 32),
-                          smem_desc_sw128(x + (k >> 2) * (x_bytes / 2) + (k & 3) * 32), idesc, st > st0 || k > 0);
+              mma_f16<CG, TA>(d, TA ? a + 8 * k : smem_desc_sw128(a + (k >> 2) * (kTSlotBytes / 2) + (k & 3) * 32),
+                              smem_desc_sw128(x + (k >> 2) * (x_bytes / 2) + (k & 3) * 32), idesc, st > st0 || k > 0);
             commit<CG>(done + 8 * rp.slot);
           }
           __syncwarp();
@@ -434,17 +464,18 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
     }
   } else if (warp >= 8) {
     // ---- weights: a thread's channel is a row of the tile
+    constexpr uint32_t W = kTWideners<TA>;
     const uint32_t wg = (warp - 8) >> 2;
     const int row = (warp & 3) * 32 + lane;
     const uint32_t lead_a = cluster_address(bars, CG == 2 ? 0 : crank) + 8 * kTMaxRing;
     const uint32_t total = team < tiles ? static_cast<uint32_t>((tiles - team + teams - 1) / teams) * (st1 - st0) : 0;
-    // positions of stage it in the rings of activations (whose barriers are used), codes and widened weights; past: of stage it - slots
-    RingPos rp{0, 0}, cp{0, 0}, wp{0, 0}, past{0, 0};
+    // positions of stage it in the rings of activations (whose barriers are used) and codes; past: of the stage that had its slot
+    // before, W stages ago.  A group's slot is its number.
+    RingPos rp{0, 0}, cp{0, 0}, past{0, 0};
     rp.advance(wg, ring);
     cp.advance(wg, p.code_depth);
-    wp.advance(wg, p.slots);
-    past.advance((p.slots & 1) ^ wg, ring);   // (the first stage of this group that waits: slots + this)
-    for (uint32_t it = wg; it < total; it += 2) {
+    past.advance(wg, ring);
+    for (uint32_t it = wg; it < total; it += W) {
       if (!mbar_wait(c_full + 8 * cp.slot, cp.phase, abort_flag, c.status)) break;
       const uint8_t* at = gen + p.off_codes + cp.slot * kTCodeSlot;
       uint4 q[4];
@@ -456,35 +487,52 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
         s2[f] = *reinterpret_cast<const uint16_t*>(at + kTCodeBytes + f * 256 + row * 2) * 0x10001u;
         z2[f] = zero_pair<H>(c.zeros ? at[kTCodeBytes + 1024 + f * 128 + row] : 8u);
       }
-      uint32_t v[4][4][4];   // all of it, before the slot is free: what follows the products of the slot's last stage is the store alone
+      auto widen = [&](int b, uint32_t (&v)[4][4]) {   // the 32 codes of run b
+        const uint32_t w[4] = {q[b].x, q[b].y, q[b].z, q[b].w};
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
+        for (int i = 0; i < 16; ++i) v[i >> 2][i & 3] = H::mul2(H::sub2(code_pair<H>(w[i >> 2], i & 3), z2[b / KPG]), s2[b / KPG]);
+      };
+      auto slot_free = [&]() {   // the products of the slot's last stage are done
+        if (it < W) return true;
+        const bool ok = mbar_wait(done + 8 * past.slot, past.phase, abort_flag, c.status);
+        past.advance(W, ring);
+        return ok;
+      };
+      if constexpr (TA) {
+        if (!slot_free()) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t to = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kTAcol + wg * 64;
 #pragma unroll
-        for (int word = 0; word < 4; ++word) {
-          const uint32_t w = word == 0 ? q[b].x : (word == 1 ? q[b].y : (word == 2 ? q[b].z : q[b].w));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[b][word][i] = H::mul2(H::sub2(code_pair<H>(w, i), z2[b / KPG]), s2[b / KPG]);
+        for (int b = 0; b < 4; ++b) {
+          uint32_t v[4][4];
+          widen(b, v);
+          tmem_st16(to + b * 16, v);
         }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(c_empty + 8 * cp.slot);
-      if (it >= static_cast<uint32_t>(p.slots)) {
-        if (!mbar_wait(done + 8 * past.slot, past.phase, abort_flag, c.status)) break;
-        past.advance(2, ring);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(c_empty + 8 * cp.slot);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      } else {
+        uint32_t v[4][4][4];   // all of it, before the slot is free: what follows the products of the slot's last stage is the store alone
+#pragma unroll
+        for (int b = 0; b < 4; ++b) widen(b, v[b]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(c_empty + 8 * cp.slot);
+        if (!slot_free()) break;
+        uint8_t* to = gen + p.off_a + wg * kTSlotBytes + row * 128;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int word = 0; word < 4; ++word) {
+            const int piece = (4 * (b & 1) + word) ^ (row & 7);
+            *reinterpret_cast<uint4*>(to + (b >> 1) * (kTSlotBytes / 2) + piece * 16) = make_uint4(v[b][word][0], v[b][word][1], v[b][word][2], v[b][word][3]);
+          }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // visible to the tensor core
       }
-      uint8_t* to = gen + p.off_a + wp.slot * kTSlotBytes + row * 128;
-#pragma unroll
-      for (int b = 0; b < 4; ++b)
-#pragma unroll
-        for (int word = 0; word < 4; ++word) {
-          const int piece = (4 * (b & 1) + word) ^ (row & 7);
-          *reinterpret_cast<uint4*>(to + (b >> 1) * (kTSlotBytes / 2) + piece * 16) = make_uint4(v[b][word][0], v[b][word][1], v[b][word][2], v[b][word][3]);
-        }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // visible to the tensor core
       __syncwarp();
       if (lane == 0) arrive_lead(lead_a + 8 * rp.slot);
-      rp.advance(2, ring);
-      cp.advance(2, p.code_depth);
-      wp.advance(2, p.slots);
+      rp.advance(W, ring);
+      cp.advance(W, p.code_depth);
     }
   } else if (warp >= 4 && p.split == 1) {
     // ---- drain
@@ -567,7 +615,7 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
     cluster_sync();
     if (work) {
       const int o0 = tl.m * 128;
-      for (int i = crank * kTThreads + threadIdx.x; i < p.TN * 16; i += p.split * kTThreads) {
+      for (int i = crank * kTThreads<TA> + threadIdx.x; i < p.TN * 16; i += p.split * kTThreads<TA>) {
         const int r = i >> 4, col = (i & 15) * 8;
         const int64_t at = static_cast<int64_t>(tl.lo + r);
         if (at >= tl.hi || o0 + col >= c.O) continue;
@@ -606,9 +654,13 @@ __global__ void __launch_bounds__(kTThreads, 1) group_tc_kernel(const __grid_con
   }
 }
 
-template <class H, int CG>
+template <class H, int CG, bool TA>
 static auto tc_kernel(int g) {
-  return g == 32 ? group_tc_kernel<H, CG, 1> : (g == 64 ? group_tc_kernel<H, CG, 2> : group_tc_kernel<H, CG, 4>);
+  return g == 32 ? group_tc_kernel<H, CG, 1, TA> : (g == 64 ? group_tc_kernel<H, CG, 2, TA> : group_tc_kernel<H, CG, 4, TA>);
+}
+template <class H>
+static auto tc_kernel(int cg, bool ta, int g) {
+  return cg == 1 ? tc_kernel<H, 1, true>(g) : (ta ? tc_kernel<H, 2, true>(g) : tc_kernel<H, 2, false>(g));
 }
 
 static bool encode_2d(CUtensorMap* map, CUtensorMapDataType type, const void* base, uint64_t cols, uint64_t rows, uint64_t pitch_bytes, int box_cols,
@@ -641,13 +693,13 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   p.wide_y = !(reinterpret_cast<uintptr_t>(c.y) & 15) && c.ldy % 8 == 0;
   p.wide_meta = c.O % 4 == 0 && !(reinterpret_cast<uintptr_t>(c.scales) & 7) && !(reinterpret_cast<uintptr_t>(c.zeros) & 3);
   const int own = p.TN / cg;
-  p.ring = own >= 128 ? 3 : 4;
-  p.slots = own >= 128 ? 2 : 3;
-  const int x_bytes = p.ring * own * 256, a_bytes = p.slots * kTSlotBytes, turn = p.split > 1 ? 0 : 2 * kTTurnBytes;
+  const bool ta = p.TN <= 128;
+  p.ring = ta ? 4 : 3;
+  const int x_bytes = p.ring * own * 256, a_bytes = ta ? 0 : kTWideners<false> * kTSlotBytes, turn = p.split > 1 ? 0 : 2 * kTTurnBytes;
   const int table = (3 * c.E + 1) * 4;
   const int room = kTMaxSmem - 1024 - x_bytes - a_bytes - turn - table;
   p.code_depth = room / kTCodeSlot < kTMaxCodes ? room / kTCodeSlot : kTMaxCodes;
-  if (p.code_depth < 2) return PIPE_ERR_UNSUPPORTED;
+  if (p.code_depth < (ta ? kTWideners<true> : kTWideners<false>)) return PIPE_ERR_UNSUPPORTED;
   p.off_a = x_bytes;
   p.off_codes = p.off_a + a_bytes;
   p.off_turn = p.off_codes + p.code_depth * kTCodeSlot;
@@ -660,7 +712,7 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
       !encode_2d(&cmap, CU_TENSOR_MAP_DATA_TYPE_FLOAT64, c.codes, static_cast<uint64_t>(c.O) * 2, static_cast<uint64_t>(c.E) * c.KB,
                  static_cast<uint64_t>(c.O) * 16, 256, 4, CU_TENSOR_MAP_SWIZZLE_NONE))
     return PIPE_ERR_CUDA;
-  void (*k)(TcArgs, CUtensorMap, CUtensorMap) = bf16 ? (cg == 2 ? tc_kernel<Bf16, 2>(c.g) : tc_kernel<Bf16, 1>(c.g)) : (cg == 2 ? tc_kernel<Fp16, 2>(c.g) : tc_kernel<Fp16, 1>(c.g));
+  void (*k)(TcArgs, CUtensorMap, CUtensorMap) = bf16 ? tc_kernel<Bf16>(cg, ta, c.g) : tc_kernel<Fp16>(cg, ta, c.g);
   if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return PIPE_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
@@ -670,7 +722,7 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   attr[1].val.clusterDim.x = cg * p.split;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.gridDim = dim3(static_cast<unsigned>(teams * cg * p.split));
-  cfg.blockDim = dim3(kTThreads);
+  cfg.blockDim = dim3(ta ? kTThreads<true> : kTThreads<false>);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cfg.attrs = attr;
