@@ -11,10 +11,9 @@
 //     groups of warps
 // Activations come by tensor copies in the 128-byte swizzle, codes by bulk copies, each on a ring.  Rows that are gathered come by
 // 16-byte asynchronous copies of two warps (a tensor copy that gathers four rows takes some 75 cycles of an SM, 64 of them a stage).
-// The fence that makes ordinary writes visible to the tensor core waits for everything the thread has in flight, so the threads
-// that fence have nothing else in flight: scales and zero points come with the codes (read by the widening threads themselves, one
-// stage ahead, they cost 1400 cycles a stage), and gathered rows are fenced by the warp that issues the MMAs, the pair's second
-// CTA's by the same warp there, which has nothing to issue.
+// The fence that makes ordinary writes visible to the tensor core waits for everything the thread has in flight, so gathered rows
+// are fenced by the warp that issues the MMAs, the pair's second CTA's by the same warp there, which has nothing to issue.  Scales
+// and zero points are read by the threads that use them, a stage of theirs ahead.
 // Sums are binary32 in tensor memory, in two accumulators, so that the drain of a tile overlaps the next one's products.
 //   warp 0  activations (gathered: and warp 3)   warp 1  MMA issue, tensor memory   warp 2  codes
 //   warps 4-7   drain accumulators (bias, sigma, rounding, a turn in shared memory to rows of y)
@@ -38,9 +37,7 @@ constexpr int kTMaxRing = 6;         // most stages of activations
 constexpr int kTMaxCodes = 12;       // most stages of codes
 constexpr int kTMaxSmem = 226 * 1024;   // dynamic shared memory (the rest of 227 KiB: barriers)
 constexpr int kTCodeBytes = 128 * kTStage / 2;            // of a stage
-constexpr int kTMetaBytes = 4 * 128 * 3;                  // its scales and zero points: at most four groups of 128 channels
 constexpr int kTSlotBytes = 128 * kTStage * 2;            // widened weights of a stage
-constexpr int kTCodeSlot = kTCodeBytes + kTMetaBytes;
 constexpr int kTTurnBytes = 32 * 128 * 2;   // 32 rows of y by 128 channels
 
 struct TcArgs {
@@ -52,7 +49,6 @@ struct TcArgs {
   int code_depth;
   int ring;        // stages of activations, at least the groups of wideners
   int wide_y;      // rows of y are 16-byte aligned
-  int wide_meta;   // scales of four channels are 8-byte, zero points 4-byte aligned
   uint32_t off_a, off_codes, off_turn, off_table;   // shared memory behind the activations
 };
 
@@ -65,10 +61,6 @@ __device__ __forceinline__ void tma_pair_2d(uint32_t dst, const CUtensorMap* map
 // 16 bytes from global to shared memory, past L1; `real` of them (16 or 0), zeros behind.
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, int real) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real) : "memory");
-}
-template <int BYTES>   // 8 or 4
-__device__ __forceinline__ void copy_small(uint32_t dst, const void* src, bool real) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(real ? BYTES : 0) : "memory");
 }
 // An arrival on the barrier once this thread's copies so far have landed (one of the arrivals that the barrier is set to).
 __device__ __forceinline__ void arrive_behind_copies(uint32_t bar) {
@@ -143,6 +135,7 @@ __device__ __forceinline__ void tmem_ld_16x32(uint32_t addr, float (&v)[16]) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[i]);
 }
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 // Four 8 x 8 blocks of pairs, turned: lane l names the 16 bytes that take column l % 8 of block l / 8.
 __device__ __forceinline__ void turn_store(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -226,7 +219,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
       mbar_init(done + 8 * s, 1);
     }
     for (int s = 0; s < kTMaxCodes; ++s) {
-      mbar_init(c_full + 8 * s, 33);
+      mbar_init(c_full + 8 * s, 1);
       mbar_init(c_empty + 8 * s, 4);
     }
     for (int b = 0; b < 2; ++b) {
@@ -369,50 +362,25 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
     for (int64_t t = team; ok && t < tiles; t += teams) {
       const Tile tl = tile_of(p, table, static_cast<int>(t));
       const int o0 = (tl.m * CG + rank) * 128;
-      const int groups = c.KB / KPG, o4 = o0 + 4 * lane;
-      const int64_t meta0 = (static_cast<int64_t>(tl.e) * groups + st0 * (4 / KPG)) * c.O + o4;   // scales and zero points: this lane's four channels
-      const uint16_t* scales = static_cast<const uint16_t*>(c.scales) + meta0;
-      const uint8_t* zeros = c.zeros + (c.zeros ? meta0 : 0);
+      // scales and zero points on their way into L2: this lane's piece of a stage's scales (lanes 0-19, five to a group) or zero points
+      // (lanes 20-31, three to a group)
+      const int rows = c.O - o0 < 128 ? c.O - o0 : 128;
+      const bool is_zero = lane >= 20;
+      const int piece_group = is_zero ? (lane - 20) / 3 : lane / 5, piece_byte = 64 * (is_zero ? (lane - 20) % 3 : lane % 5);
+      const int run_bytes = is_zero ? rows : 2 * rows, groups = c.KB / KPG;
+      const bool mine = rows > 0 && piece_group < 4 / KPG && (!is_zero || c.zeros);
+      const int64_t meta0 = (static_cast<int64_t>(tl.e) * groups + piece_group) * c.O + o0;
+      const uint8_t* meta = (is_zero ? c.zeros + meta0 : static_cast<const uint8_t*>(c.scales) + 2 * meta0) + (piece_byte < run_bytes ? piece_byte : run_bytes - 1);
       for (int st = st0; st < st1; ++st, ++it, rp.advance(1, p.code_depth)) {
         if (!mbar_wait(c_empty + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
-        const uint32_t at = p.off_codes + rp.slot * kTCodeSlot, to_s = at + kTCodeBytes + lane * 8, to_z = at + kTCodeBytes + 1024 + lane * 4;
         if (elect_one()) {
           mbar_expect_tx(c_full + 8 * rp.slot, kTCodeBytes);
-          tma_load_2d(base + at, &cmap, 2 * o0, tl.e * c.KB + 4 * st, c_full + 8 * rp.slot);
+          tma_load_2d(base + p.off_codes + rp.slot * kTCodeBytes, &cmap, 2 * o0, tl.e * c.KB + 4 * st, c_full + 8 * rp.slot);
         }
+        if (mine && st * (4 / KPG) + piece_group < groups) prefetch_l2(meta + static_cast<int64_t>(st) * (4 / KPG) * c.O * (is_zero ? 1 : 2));
         __syncwarp();
-        // (a scale of zero behind the layer's channels and groups: what is widened there is zero, whatever its codes)
-        if (p.wide_meta && o0 + 128 <= c.O && (st + 1) * (4 / KPG) <= groups) {
-#pragma unroll
-          for (int f = 0; f < 4 / KPG; ++f) {
-            copy_small<8>(base + to_s + f * 256, scales + static_cast<int64_t>(f) * c.O, true);
-            if (c.zeros) copy_small<4>(base + to_z + f * 128, zeros + static_cast<int64_t>(f) * c.O, true);
-          }
-          arrive_behind_copies(c_full + 8 * rp.slot);
-        } else if (p.wide_meta) {
-#pragma unroll 1
-          for (int f = 0; f < 4 / KPG; ++f) {
-            const bool real = st * (4 / KPG) + f < groups && o4 < c.O;
-            copy_small<8>(base + to_s + f * 256, real ? scales + static_cast<int64_t>(f) * c.O : c.scales, real);
-            if (c.zeros) copy_small<4>(base + to_z + f * 128, real ? zeros + static_cast<int64_t>(f) * c.O : c.zeros, real);
-          }
-          arrive_behind_copies(c_full + 8 * rp.slot);
-        } else {
-#pragma unroll 1
-          for (int f = 0; f < 4 / KPG; ++f)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const bool real = st * (4 / KPG) + f < groups && o4 + i < c.O;
-              *reinterpret_cast<uint16_t*>(gen + to_s + f * 256 + 2 * i) = real ? __ldcg(scales + static_cast<int64_t>(f) * c.O + i) : 0;
-              if (c.zeros) gen[to_z + f * 128 + i] = real ? __ldcg(zeros + static_cast<int64_t>(f) * c.O + i) : 0;
-            }
-          mbar_arrive(c_full + 8 * rp.slot);
-        }
-        scales += (4 / KPG) * static_cast<int64_t>(c.O);
-        if (c.zeros) zeros += (4 / KPG) * static_cast<int64_t>(c.O);
       }
     }
-    copies_done();
     if (*abort_flag) drain_ring(c_full, it, p.code_depth, 20000000ll);
   } else if (warp == 1) {
     // ---- MMA
@@ -469,6 +437,42 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
     const int row = (warp & 3) * 32 + lane;
     const uint32_t lead_a = cluster_address(bars, CG == 2 ? 0 : crank) + 8 * kTMaxRing;
     const uint32_t total = team < tiles ? static_cast<uint32_t>((tiles - team + teams - 1) / teams) * (st1 - st0) : 0;
+    // the stage whose scales and zero points are fetched next
+    const int groups = c.KB / KPG, nst = st1 - st0;
+    int64_t t = team;
+    int st = st0 + static_cast<int>(wg);
+    int64_t meta = 0;   // of this channel in the first group of the tile's expert
+    bool here = false;
+    auto open_tile = [&]() {   // (a channel beyond the layer: the last one's, not used)
+      const Tile tl = tile_of(p, table, static_cast<int>(t));
+      const int o = (tl.m * CG + rank) * 128 + row;
+      here = o < c.O;
+      meta = static_cast<int64_t>(tl.e) * groups * c.O + (here ? o : c.O - 1);
+    };
+    uint32_t s2[4 / KPG], z2[4 / KPG], sc[4 / KPG], zp[4 / KPG];
+    auto fetch = [&]() {
+#pragma unroll
+      for (int f = 0; f < 4 / KPG; ++f) {
+        const int group = st * (4 / KPG) + f;   // (one beyond the axis: the last one's, which meet activations of zero; made zero themselves below)
+        const int64_t at = meta + static_cast<int64_t>(group < groups ? group : groups - 1) * c.O;
+        sc[f] = __ldcg(static_cast<const uint16_t*>(c.scales) + at);
+        if (c.zeros) zp[f] = __ldcg(c.zeros + at);
+      }
+    };
+    auto settle = [&]() {   // a stage number beyond the tile's is one of a later tile's
+      if (st >= st1) {
+        do {
+          st -= nst;
+          t += teams;
+        } while (st >= st1);
+        if (t < tiles) open_tile();
+      }
+    };
+    if (wg < total) {
+      settle();
+      if (t == team) open_tile();
+      fetch();
+    }
     // positions of stage it in the rings of activations (whose barriers are used) and codes; past: of the stage that had its slot
     // before, W stages ago.  A group's slot is its number.
     RingPos rp{0, 0}, cp{0, 0}, past{0, 0};
@@ -476,17 +480,22 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
     cp.advance(wg, p.code_depth);
     past.advance(wg, ring);
     for (uint32_t it = wg; it < total; it += W) {
+      // (zero where there is no such channel or group: what is widened there is zero, whatever its codes)
+#pragma unroll
+      for (int f = 0; f < 4 / KPG; ++f) {
+        s2[f] = here && st * (4 / KPG) + f < groups ? sc[f] * 0x10001u : 0u;
+        z2[f] = zero_pair<H>(c.zeros ? zp[f] : 8u);
+      }
+      if (it + W < total) {
+        st += W;
+        settle();
+        fetch();
+      }
       if (!mbar_wait(c_full + 8 * cp.slot, cp.phase, abort_flag, c.status)) break;
-      const uint8_t* at = gen + p.off_codes + cp.slot * kTCodeSlot;
+      const uint8_t* at = gen + p.off_codes + cp.slot * kTCodeBytes;
       uint4 q[4];
 #pragma unroll
       for (int b = 0; b < 4; ++b) q[b] = reinterpret_cast<const uint4*>(at)[b * 128 + row];
-      uint32_t s2[4 / KPG], z2[4 / KPG];
-#pragma unroll
-      for (int f = 0; f < 4 / KPG; ++f) {
-        s2[f] = *reinterpret_cast<const uint16_t*>(at + kTCodeBytes + f * 256 + row * 2) * 0x10001u;
-        z2[f] = zero_pair<H>(c.zeros ? at[kTCodeBytes + 1024 + f * 128 + row] : 8u);
-      }
       auto widen = [&](int b, uint32_t (&v)[4][4]) {   // the 32 codes of run b
         const uint32_t w[4] = {q[b].x, q[b].y, q[b].z, q[b].w};
 #pragma unroll
@@ -691,18 +700,17 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   int64_t teams = p.split > 1 ? tiles : kPlanSMs / cg;
   if (teams > tiles) teams = tiles;
   p.wide_y = !(reinterpret_cast<uintptr_t>(c.y) & 15) && c.ldy % 8 == 0;
-  p.wide_meta = c.O % 4 == 0 && !(reinterpret_cast<uintptr_t>(c.scales) & 7) && !(reinterpret_cast<uintptr_t>(c.zeros) & 3);
   const int own = p.TN / cg;
   const bool ta = p.TN <= 128;
   p.ring = ta ? 4 : 3;
   const int x_bytes = p.ring * own * 256, a_bytes = ta ? 0 : kTWideners<false> * kTSlotBytes, turn = p.split > 1 ? 0 : 2 * kTTurnBytes;
   const int table = (3 * c.E + 1) * 4;
   const int room = kTMaxSmem - 1024 - x_bytes - a_bytes - turn - table;
-  p.code_depth = room / kTCodeSlot < kTMaxCodes ? room / kTCodeSlot : kTMaxCodes;
+  p.code_depth = room / kTCodeBytes < kTMaxCodes ? room / kTCodeBytes : kTMaxCodes;
   if (p.code_depth < (ta ? kTWideners<true> : kTWideners<false>)) return PIPE_ERR_UNSUPPORTED;
   p.off_a = x_bytes;
   p.off_codes = p.off_a + a_bytes;
-  p.off_turn = p.off_codes + p.code_depth * kTCodeSlot;
+  p.off_turn = p.off_codes + p.code_depth * kTCodeBytes;
   p.off_table = p.off_turn + turn;
   const int smem = 1024 + static_cast<int>(p.off_table) + table;
   // activations: boxes of 64 columns; codes: rows of O runs of 16 bytes, taken as 8-byte elements, a stage's four runs of 128 channels in
