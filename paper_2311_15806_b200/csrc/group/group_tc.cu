@@ -165,6 +165,7 @@ __device__ __forceinline__ void store_y8(uint16_t* y, const uint4& w, int wide, 
 struct Tile {
   int e, m;
   int lo, hi;   // rows of y (N < 2^31)
+  int n;        // columns of its MMAs: the rows rounded up to 32
 };
 // first[e]: units before expert e, first[E] all of them; begin[e], end[e]: its rows.
 __device__ __forceinline__ Tile tile_of(const TcArgs& p, const int32_t* first, int t) {
@@ -181,6 +182,7 @@ __device__ __forceinline__ Tile tile_of(const TcArgs& p, const int32_t* first, i
   const int32_t *begin = first + p.c.E + 1, *end = begin + p.c.E;
   r.lo = begin[lo] + (u - first[lo]) * p.TN;
   r.hi = end[lo] - r.lo < p.TN ? end[lo] : r.lo + p.TN;
+  r.n = (r.hi - r.lo + 31) & ~31;
   return r;
 }
 
@@ -286,7 +288,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
     bool ok = true;
     for (int64_t t = team; ok && t < tiles; t += teams) {
       const Tile tl = tile_of(p, table, static_cast<int>(t));
-      const int row0 = tl.lo + rank * own_rows;
+      const int row0 = tl.lo + rank * (tl.n / CG);
       for (int st = st0; st < st1; ++st, ++it, rp.advance(1, ring)) {
         if (!mbar_wait(done + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
         if (elect_one()) {
@@ -306,18 +308,18 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
   } else if ((warp == 0 || warp == 3) && c.rows) {
     // ---- activations, gathered: this warp's half of the rows, four rows by 128 bytes per copy instruction
     constexpr int kMost = 128 / 2 / 4;
-    const int half = own_rows / 2, mine = half / 4;   // copies of this warp per 64 columns
-    const int first = (warp ? half : 0) + (lane >> 3);
-    const uint32_t place = static_cast<uint32_t>(first * 128 + (((lane & 7) ^ (first & 7)) * 16));   // (+ 4 rows: the other half of the atom)
     RingPos rp{0, 0};
     bool ok = true;
     for (int64_t t = team; ok && t < tiles; t += teams) {
       const Tile tl = tile_of(p, table, static_cast<int>(t));
+      const int half = tl.n / CG / 2, mine = half / 4;   // copies of this warp per 64 columns (half: a multiple of 8)
+      const int first = (warp ? half : 0) + (lane >> 3);
+      const uint32_t place = static_cast<uint32_t>(first * 128 + (((lane & 7) ^ (first & 7)) * 16));   // (+ 4 rows: the other half of the atom)
       const uint16_t* src[kMost];   // rows behind the tile's: its last one, whose sums are not stored
       uint32_t none = 0;            // rows whose index lies outside: zeros
 #pragma unroll
       for (int i = 0; i < kMost; ++i) {
-        const int at = tl.lo + rank * own_rows + first + 4 * i;
+        const int at = tl.lo + rank * (tl.n / CG) + first + 4 * i;
         int64_t r = __ldcg(c.rows + (at < tl.hi ? at : tl.hi - 1));
         if (r < 0 || r >= c.T) {
           none |= 1u << i;
@@ -383,17 +385,22 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
     }
     if (*abort_flag) drain_ring(c_full, it, p.code_depth, 20000000ll);
   } else if (warp == 1) {
-    // ---- MMA
+    // ---- MMA.  The whole warp runs the loop, one elected lane issues.  Of a descriptor only the low word changes (its address field,
+    // in 16-byte units, never carries out of it).
     if (rank == 0) {
       const uint32_t type = H::kBase == Bf16::kBase ? 1u : 0u;
-      const uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | (static_cast<uint32_t>(p.TN >> 3) << 17) | (static_cast<uint32_t>(128 * CG >> 4) << 24);
+      const uint32_t idesc0 = (1u << 4) | (type << 7) | (type << 10) | (static_cast<uint32_t>(128 * CG >> 4) << 24);
+      const uint64_t xdesc = smem_desc_sw128(base), adesc = smem_desc_sw128(base + p.off_a);
+      const uint32_t x_lo = static_cast<uint32_t>(xdesc), x_hi = static_cast<uint32_t>(xdesc >> 32);
+      const uint32_t a_lo = TA ? tmem + kTAcol : static_cast<uint32_t>(adesc), a_hi = TA ? 0u : static_cast<uint32_t>(adesc >> 32);
+      const uint32_t x_stage = x_bytes >> 4, x_half = x_bytes >> 5;
       RingPos rp{0, 0}, wp{0, 0};
       uint32_t n = 0;
       bool ok = true;
       for (int64_t t = team; ok && t < tiles; t += teams, ++n) {
         const uint32_t buf = n & 1, use = n >> 1;
+        const uint32_t idesc = idesc0 | (static_cast<uint32_t>(tile_of(p, table, static_cast<int>(t)).n >> 3) << 17);
         if (!mbar_wait(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status)) break;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + buf * p.TN;
         for (int st = st0; st < st1; ++st, rp.advance(1, ring), wp.advance(1, kTWideners<TA>)) {
           if (!mbar_wait(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status) ||
@@ -403,13 +410,14 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
           }
           if (c.rows) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t xl = x_lo + rp.slot * x_stage, al = a_lo + wp.slot * (TA ? 64u : kTSlotBytes >> 4);
           if (elect_one()) {
-            const uint32_t a = TA ? tmem + kTAcol + wp.slot * 64 : base + p.off_a + wp.slot * kTSlotBytes;
-            const uint32_t x = base + rp.slot * x_bytes;
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-              mma_f16<CG, TA>(d, TA ? a + 8 * k : smem_desc_sw128(a + (k >> 2) * (kTSlotBytes / 2) + (k & 3) * 32),
-                              smem_desc_sw128(x + (k >> 2) * (x_bytes / 2) + (k & 3) * 32), idesc, st > st0 || k > 0);
+            for (int k = 0; k < 8; ++k) {
+              const uint32_t ak = TA ? al + 8u * k : al + (k >> 2) * (kTSlotBytes >> 5) + 2u * (k & 3);
+              const uint32_t xk = xl + (k >> 2) * x_half + 2u * (k & 3);
+              mma_f16<CG, TA>(d, (static_cast<uint64_t>(a_hi) << 32) | ak, (static_cast<uint64_t>(x_hi) << 32) | xk, idesc, k > 0 || st > st0);
+            }
             commit<CG>(done + 8 * rp.slot);
           }
           __syncwarp();
@@ -691,6 +699,7 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   const int64_t units = most_units(c, p.TN);
   const int cg = c.O > 128 && units * ceil_div(c.O, 128) > kPlanSMs ? 2 : 1;
   if (cg == 1 && p.TN == 256) p.TN = 128;
+  if (!c.offsets) p.TN = static_cast<int>(round_up<int64_t>(ceil_div<int64_t>(c.N, ceil_div<int64_t>(c.N, p.TN)), 32));   // units of one size
   p.stages = ceil_div(c.I, kTStage);
   p.mtiles = ceil_div(c.O, 128 * cg);
   const int64_t tiles = most_units(c, p.TN) * p.mtiles;
