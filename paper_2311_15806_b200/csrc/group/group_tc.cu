@@ -66,6 +66,10 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, int real) 
 __device__ __forceinline__ void arrive_behind_copies(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
+template <int V>
+struct Int {
+  static constexpr int value = V;
+};
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 template <int CG, bool TA>   // a: columns of tensor memory (TA) or a descriptor
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
@@ -328,29 +332,53 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
         src[i] = static_cast<const uint16_t*>(c.x) + r * c.ldx + 8 * (lane & 7) + st0 * kTStage;
       }
       const bool plain = !__any_sync(0xffffffffu, none != 0);
-      for (int st = st0; st < st1; ++st, rp.advance(1, ring)) {
-        if (!mbar_wait(done + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
+      // a stage whose 128 columns from src + 128 * AHEAD on are all there, of FULL copies (0: `mine`) per 64 columns
+      auto whole_stage = [&](auto ahead, auto full) {
+        constexpr int AHEAD = decltype(ahead)::value, FULL = decltype(full)::value;
         const uint32_t even = base + rp.slot * x_bytes + place, odd = even ^ 64u;
-        if (plain && (st + 1) * kTStage <= c.I) {
+#pragma unroll
+        for (int i = 0; i < kMost; ++i)
+          if (FULL ? i < FULL : i < mine) {
+            copy16((i & 1 ? odd : even) + i * 512, src[i] + AHEAD * kTStage, 16);
+            copy16((i & 1 ? odd : even) + x_bytes / 2 + i * 512, src[i] + AHEAD * kTStage + 64, 16);
+          }
+      };
+      auto free_slot = [&]() { return mbar_wait(done + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status); };
+      auto hand_on = [&]() {
+        arrive_behind_copies(x_full + 8 * rp.slot);
+        rp.advance(1, ring);
+      };
+      int st = st0;
+      const int whole = plain ? (st1 * kTStage <= c.I ? st1 : st1 - 1) : st0;   // stages before this one have nothing to leave out
+      for (; ok && st + 2 <= whole; st += 2) {   // (two at a time: the rows' addresses are advanced once)
+        ok = free_slot();
+        if (!ok) break;
+        if (mine == kMost) whole_stage(Int<0>{}, Int<kMost>{});
+        else whole_stage(Int<0>{}, Int<0>{});
+        hand_on();
+        ok = free_slot();
+        if (!ok) break;
+        if (mine == kMost) whole_stage(Int<1>{}, Int<kMost>{});
+        else whole_stage(Int<1>{}, Int<0>{});
+        hand_on();
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) src[i] += 2 * kTStage;
+      }
+      for (; ok && st < st1; ++st) {
+        ok = free_slot();
+        if (!ok) break;
+        const uint32_t even = base + rp.slot * x_bytes + place, odd = even ^ 64u;
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          const bool inside = st * kTStage + 64 * h + 8 * (lane & 7) < c.I;
 #pragma unroll
           for (int i = 0; i < kMost; ++i)
             if (i < mine) {
-              copy16((i & 1 ? odd : even) + i * 512, src[i], 16);
-              copy16((i & 1 ? odd : even) + x_bytes / 2 + i * 512, src[i] + 64, 16);
+              const bool real = inside && !((none >> i) & 1);
+              copy16((i & 1 ? odd : even) + h * (x_bytes / 2) + i * 512, real ? src[i] + 64 * h : static_cast<const uint16_t*>(c.x), real ? 16 : 0);
             }
-        } else {
-#pragma unroll 1
-          for (int h = 0; h < 2; ++h) {
-            const bool inside = st * kTStage + 64 * h + 8 * (lane & 7) < c.I;
-#pragma unroll
-            for (int i = 0; i < kMost; ++i)
-              if (i < mine) {
-                const bool real = inside && !((none >> i) & 1);
-                copy16((i & 1 ? odd : even) + h * (x_bytes / 2) + i * 512, real ? src[i] + 64 * h : static_cast<const uint16_t*>(c.x), real ? 16 : 0);
-              }
-          }
         }
-        arrive_behind_copies(x_full + 8 * rp.slot);
+        hand_on();
 #pragma unroll
         for (int i = 0; i < kMost; ++i) src[i] += kTStage;
       }
