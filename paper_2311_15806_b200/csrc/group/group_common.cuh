@@ -63,9 +63,9 @@ __device__ __forceinline__ int cluster_load(const int32_t* own, int rank) {
 struct Bf16 {
   using T = __nv_bfloat16;
   static constexpr uint32_t kBase = 0x43004300u;
-  static __device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
+  static __device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {   // (one fused operation; an addition costs two)
     uint32_t d;
-    asm("sub.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(0x3F803F80u), "r"(b));
     return d;
   }
   static __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
@@ -89,9 +89,9 @@ struct Bf16 {
 struct Fp16 {
   using T = __half;
   static constexpr uint32_t kBase = 0x64006400u;
-  static __device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
+  static __device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {
     uint32_t d;
-    asm("sub.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    asm("add.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
   }
   static __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
@@ -120,10 +120,10 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t w, int i) {
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(w >> (4 * i)), "r"(0x000F000Fu), "r"(H::kBase));
   return d;
 }
-// The zero point z (8 for a symmetric layer) on top of the base, in both halves.
+// What takes the base and the zero point z (8 for a symmetric layer) away from a pair again: minus their sum, in both halves.
 template <class H>
 __device__ __forceinline__ uint32_t zero_pair(uint32_t z) {
-  return H::kBase | z | (z << 16);
+  return (H::kBase | 0x80008000u) | z | (z << 16);
 }
 
 // sigma of N sums, with SiLU and sigmoid on the approximate exponential and reciprocal (2^-22 and 2^-23 of their values, the
@@ -149,53 +149,60 @@ __device__ __forceinline__ void quick_activation(float (&v)[N], int kind) {
   }
 }
 
-// Row tiles of `per` rows dealt to units: unit u is tile `tile` of expert e, whose rows are [lo, hi).  Every lane of the calling
-// warp gets the answer; false: there are fewer units.  Offsets are taken as clamped to [0, N] and ascending, whatever they hold.
-struct Unit {
-  int e;
-  int64_t lo, hi;   // the tile's rows
-};
-__device__ __forceinline__ bool find_unit(const Call& c, int64_t u, int per, Unit& out) {
-  if (!c.offsets) {
-    out.e = 0;
-    out.lo = u * per;
-    out.hi = out.lo + per < c.N ? out.lo + per : c.N;
-    return out.lo < c.N;
-  }
-  const int lane = threadIdx.x & 31;
-  int64_t before = 0;
-  for (int e0 = 0; e0 < c.E; e0 += 32) {
-    const int e = e0 + lane;
-    int64_t lo = 0, hi = 0;
-    if (e < c.E) {
+// The rows cut into units of at most `per` rows of one expert, numbered expert by expert.  The table, unit_ints(E) integers of shared
+// memory: first[e], the units before expert e (first[E]: all of them), begin[e] and end[e], its rows.  Offsets are taken as clamped to
+// [0, N] and ascending, whatever they hold.
+__host__ __device__ inline int unit_ints(int E) { return 3 * E + 1; }
+template <int THREADS>
+__device__ __forceinline__ void build_units(const Call& c, int per, int32_t* table) {
+  for (int e = threadIdx.x; e < c.E; e += THREADS) {
+    int64_t lo = 0, hi = c.N;
+    if (c.offsets) {
       lo = __ldcg(c.offsets + e);
       hi = __ldcg(c.offsets + e + 1);
       lo = lo < 0 ? 0 : (lo > c.N ? c.N : lo);
       hi = hi < lo ? lo : (hi > c.N ? c.N : hi);
     }
-    const int mine = static_cast<int>((hi - lo + per - 1) / per);
-    int upto = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, upto, d);
-      if (lane >= d) upto += v;
-    }
-    const int total = __shfl_sync(0xffffffffu, upto, 31);
-    if (u < before + total) {
-      const int at = static_cast<int>(u - before);
-      const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
-      const int src = __ffs(past) - 1;
-      const int tile = at - __shfl_sync(0xffffffffu, upto - mine, src);
-      lo = __shfl_sync(0xffffffffu, lo, src);
-      hi = __shfl_sync(0xffffffffu, hi, src);
-      out.e = e0 + src;
-      out.lo = lo + static_cast<int64_t>(tile) * per;
-      out.hi = out.lo + per < hi ? out.lo + per : hi;
-      return true;
-    }
-    before += total;
+    table[c.E + 1 + e] = static_cast<int32_t>(lo);   // N < 2^31
+    table[2 * c.E + 1 + e] = static_cast<int32_t>(hi);
   }
-  return false;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    const int lane = threadIdx.x;
+    int before = 0;
+    for (int e0 = 0; e0 < c.E; e0 += 32) {
+      const int e = e0 + lane;
+      const int mine = e < c.E ? (table[2 * c.E + 1 + e] - table[c.E + 1 + e] + per - 1) / per : 0;
+      int upto = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += v;
+      }
+      if (e < c.E) table[e] = before + upto - mine;
+      before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (lane == 0) table[c.E] = before;
+  }
+  // (a barrier of the block follows)
+}
+struct Unit {
+  int e;
+  int lo, hi;   // its rows
+};
+__device__ __forceinline__ Unit unit_at(const int32_t* table, int E, int per, int u) {
+  int lo = 0, hi = E;   // the last e with first[e] <= u
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (table[mid] <= u) lo = mid;
+    else hi = mid;
+  }
+  Unit r;
+  r.e = lo;
+  const int end = table[2 * E + 1 + lo];
+  r.lo = table[E + 1 + lo] + (u - table[lo]) * per;
+  r.hi = end - r.lo < per ? end : r.lo + per;
+  return r;
 }
 // The most units that N rows on E experts can make: every expert with rows has at most one tile that is not full.
 inline int64_t most_units(const Call& c, int per) {

@@ -1,206 +1,316 @@
 // Products of a 4-bit layer with group scales with a few rows (pipe_group_linear, pipe_expert_linear).
 //
-// With a few rows the product is bound by reading the codes once.  The warp-level MMA m16n8k16 takes the weights as its 16-row and
-// the activations as its 8-column operand: the codes minus their zero point are small integers, exact in bf16 and fp16, so a
-// group's sum is formed in binary32 from exact operands and the scale enters once per group and output, in binary32 too.  A run of
-// 32 codes of a row is 16 bytes, 4 per lane of a quad: the lane's 8 codes are its operands of two MMAs, and the activations that
-// meet them are 8 neighbouring values of the row, 16 bytes.  A warp takes 16 * MT output channels and every step of 128 codes of
-// its share of the reduction axis; the warps of a CTA and the CTAs of a cluster share the axis and add their sums in a fixed
-// order, in shared memory and across it.
+// With a few rows the product is bound by reading the codes once, and by the instructions that widen them.  The warp-level MMA
+// m16n8k16 takes the weights as its 16-row and the activations as its 8-column operand: the codes minus their zero point are small
+// integers, exact in bf16 and fp16, so a group's sum is formed in binary32 from exact operands and the scale enters once per group
+// and output, in binary32 too.  A run of 32 codes of a row is 16 bytes, 4 per lane of a quad: the lane's 8 codes are its operands
+// of two MMAs, and the activations that meet them are 8 neighbouring values of the row, 16 bytes.
+// A CTA takes one tile of 16 * MT channels and one unit of rows; its four warps, and the CTAs of a cluster where there are few tiles,
+// share the reduction axis in steps of 128 codes.  A warp's activations are asked into L1, which the CTAs of an SM share, at once;
+// codes, scales and zero points of its next steps are in flight in registers (copies through shared memory cost more instructions
+// than the arithmetic).  Sums are added in a fixed order.
+#include <cstdlib>
+
 #include "group_common.cuh"
 
 namespace pipe {
 namespace grp {
 
-constexpr int kSWarps = 8;
+constexpr int kSWarps = 4;
+constexpr int kSThreads = 32 * kSWarps;
 
 struct SmallArgs {
   Call c;
-  int tiles;    // row tiles of the layer: ceil(O / (16 MT))
-  int steps;    // steps of 128 codes: ceil(I / 128)
+  int steps;      // steps of 128 codes: ceil(I / 128); 0 where there are no activations at all
+  int units;      // the most there can be
 };
 
-// NT: 8-column tiles (tokens of a unit: 8 NT); KPG: runs of 32 codes per group.
-template <class H, int MT, int NT, int KPG, bool ASYM>
-__global__ void __launch_bounds__(32 * kSWarps) group_small_kernel(SmallArgs p) {
-  constexpr int kM = 16 * MT, kN = 8 * NT;
-  constexpr int kFlush = 4 / KPG;            // groups of a step
-  __shared__ float part[kSWarps][kN][kM + 1];
+// Unit u of the rows cut into units of at most `per` rows of one expert: every lane of the calling warp gets the answer; false: there
+// are fewer units.  Offsets are taken as clamped to [0, N] and ascending, whatever they hold.
+__device__ __forceinline__ bool find_unit(const Call& c, int u, int per, Unit& out) {
+  if (!c.offsets) {
+    out.e = 0;
+    out.lo = u * per;
+    out.hi = out.lo + per < c.N ? out.lo + per : static_cast<int>(c.N);
+    return out.lo < c.N;
+  }
+  const int lane = threadIdx.x & 31, N = static_cast<int>(c.N);
+  int before = 0;
+  for (int e0 = 0; e0 < c.E; e0 += 32) {
+    const int e = e0 + lane;
+    int lo = 0, hi = 0;
+    if (e < c.E) {
+      lo = min(max(__ldcg(c.offsets + e), 0), N);
+      hi = min(max(__ldcg(c.offsets + e + 1), lo), N);
+    }
+    const int mine = (hi - lo + per - 1) / per;
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += v;
+    }
+    const int total = __shfl_sync(0xffffffffu, upto, 31);
+    if (u < before + total) {
+      const int src = __ffs(__ballot_sync(0xffffffffu, upto > u - before)) - 1;
+      const int tile = u - before - __shfl_sync(0xffffffffu, upto - mine, src);
+      out.e = e0 + src;
+      out.lo = __shfl_sync(0xffffffffu, lo, src) + tile * per;
+      out.hi = min(out.lo + per, __shfl_sync(0xffffffffu, hi, src));
+      return true;
+    }
+    before += total;
+  }
+  return false;
+}
+
+// NT: 8-column tiles (rows of a unit: 8 NT); KPG: runs of 32 codes per group.
+// TAIL: I is no multiple of 128, the last step has fewer runs.
+template <class H, int MT, int NT, int KPG, bool ASYM, bool TAIL>
+__global__ void __launch_bounds__(kSThreads, MT == 1 ? 5 : (NT == 1 ? 4 : 3)) group_small_kernel(SmallArgs p) {
+  constexpr int kM = 16 * MT, kN = 8 * NT, kP = kM + 4;   // kP: pitch of a row of sums (its writers then meet different banks)
+  constexpr int kGroups = 4 / KPG;                         // groups of a step
+  constexpr int kAhead = MT == 1 ? 4 : 2;                  // steps of codes in registers
+  constexpr int kMeta = 2;                                 // steps of scales and zero points
+  __shared__ float part[kSWarps * kN * kP];
   const Call& c = p.c;
   const int ctas = cluster_ctas(), rank = cluster_rank();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
-  const int64_t block = blockIdx.x / ctas;
-  const int tile = static_cast<int>(block % p.tiles);
-  const int o0 = tile * kM;
+  const uint32_t tile = ctas == 1 ? blockIdx.x : blockIdx.x / static_cast<uint32_t>(ctas);
+  const int o0 = static_cast<int>(tile) * kM;
   const int slices = ctas * kSWarps, slice = rank * kSWarps + warp;
-  const int step0 = static_cast<int>(static_cast<int64_t>(p.steps) * slice / slices), step1 = static_cast<int>(static_cast<int64_t>(p.steps) * (slice + 1) / slices);
+  const int step0 = static_cast<int>(static_cast<uint32_t>(p.steps) * slice / slices);   // (steps < 2^26, slices <= 32)
+  const int step1 = static_cast<int>(static_cast<uint32_t>(p.steps) * (slice + 1) / slices);
+  const int groups = c.KB / KPG;
+  const int64_t run_bytes = static_cast<int64_t>(c.O) * 16;
 
+  if (!c.offsets) {
+    // this warp's codes on their way into L2 before the wait (asking for a line that is still being written does no harm)
+    const int n = (step1 - step0) * 4 * 2 * MT;
+    for (int i = lane; i < n; i += 32) {
+      const int kb = 4 * step0 + i / (2 * MT), o = o0 + 8 * (i % (2 * MT));
+      if (kb < c.KB && o < c.O) asm volatile("prefetch.global.L2 [%0];" ::"l"(c.codes + kb * run_bytes + o * 16));
+    }
+  }
   grid_wait();
   grid_release();
-  Unit u;
-  if (!find_unit(c, block / p.tiles, kN, u)) return;   // (the same answer in every CTA of the cluster)
-
-  // rows of this lane's MMA operands; one beyond the layer reads the last one instead and is not stored
-  uint32_t row[2 * MT];
+  for (int un = blockIdx.y; un < p.units; un += gridDim.y) {
+    Unit u;
+    if (!find_unit(c, un, kN, u)) break;   // (the same answer in every CTA of the cluster)
+    const int count = u.hi - u.lo;
+    // This lane's rows of the MMA operands: channels o0 + gid + 8 m.  Of channels beyond the layer nothing is read: their sums, of
+    // whatever the registers hold, are not stored.  Rows of activations: behind the unit's last row it, not stored; in the place of one
+    // whose index lies outside some row, its sums made zero below.
+    bool real[2 * MT];
 #pragma unroll
-  for (int m = 0; m < 2 * MT; ++m) {
-    const int o = o0 + 16 * (m >> 1) + 8 * (m & 1) + gid;
-    row[m] = static_cast<uint32_t>(o < c.O ? o : c.O - 1);
-  }
-  const uint8_t* codes = c.codes + static_cast<int64_t>(u.e) * c.KB * c.O * 16 + 4 * tig;
-  const int groups = c.KB / KPG;
-  const uint16_t* scales = static_cast<const uint16_t*>(c.scales) + static_cast<int64_t>(u.e) * groups * c.O;
-  const uint8_t* zeros = ASYM ? c.zeros + static_cast<int64_t>(u.e) * groups * c.O : nullptr;
-  const uint16_t* x[NT];
+    for (int m = 0; m < 2 * MT; ++m) real[m] = o0 + 8 * m + gid < c.O;
+    const uint8_t* code[4];   // the four runs of the next step to be asked for
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int64_t s = u.lo + 8 * n + gid;
-    x[n] = nullptr;
-    if (s < u.hi) {
-      const int64_t r = c.rows ? __ldcg(c.rows + s) : s;
-      if (r >= 0 && r < c.T) x[n] = static_cast<const uint16_t*>(c.x) + r * c.ldx + 8 * tig;
+    for (int b = 0; b < 4; ++b) code[b] = c.codes + (static_cast<int64_t>(u.e) * c.KB + 4 * step0 + b) * run_bytes + (o0 + gid) * 16 + 4 * tig;
+    const int64_t meta0 = (static_cast<int64_t>(u.e) * groups + step0 * kGroups) * c.O + o0 + gid;
+    const uint16_t* scales = static_cast<const uint16_t*>(c.scales) + meta0;
+    const uint8_t* zeros = ASYM ? c.zeros + meta0 : nullptr;
+    const uint16_t* x[NT];
+    uint32_t inside[NT];   // bit 4 n: row n of the column tile exists
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int s = u.lo + min(8 * n + gid, count - 1);
+      int64_t r = c.rows ? __ldcg(c.rows + s) : s;
+      const bool ok = r >= 0 && r < c.T;
+      inside[n] = __ballot_sync(0xffffffffu, ok);
+      if (!ok) r = 0;
+      x[n] = static_cast<const uint16_t*>(c.x) + r * c.ldx + 128 * step0 + 8 * tig;
     }
-  }
+    uint32_t w[kAhead][4][2 * MT];
+    auto load = [&](int step, uint32_t (&d)[4][2 * MT]) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        if (!TAIL || 4 * step + b < c.KB) {
+#pragma unroll
+          for (int m = 0; m < 2 * MT; ++m)
+            if (real[m]) d[b][m] = __ldcg(reinterpret_cast<const uint32_t*>(code[b] + 128 * m));
+        }
+        code[b] += 4 * run_bytes;
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (step0 + i < step1) load(step0 + i, w[i]);
+    {   // this warp's share of the rows on their way into L1: four lanes have each row's address, eight of a row's lines are asked for at a time
+      const int lines = (min(c.I, 128 * step1) - 128 * step0 + 63) / 64;   // of 128 bytes
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        if (8 * n + gid < count)
+          for (int i = tig; i < lines; i += 4) asm volatile("prefetch.global.L1 [%0];" ::"l"(x[n] - 8 * tig + 64 * i));
+    }
 
-  float acc[MT][NT][4];
+    float acc[MT][NT][4];
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.f;
+        for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.f;
 
-  uint32_t w[2][4][2 * MT];
-  auto load = [&](int step, uint32_t (&d)[4][2 * MT]) {
+    uint32_t sc[kMeta][kGroups][2 * MT], zp[kMeta][kGroups][2 * MT];
+    auto fetch = [&](int step, uint32_t (&s)[kGroups][2 * MT], uint32_t (&z)[kGroups][2 * MT]) {
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int kb = 4 * step + b;
-      if (kb < c.KB) {
-        const uint8_t* run = codes + static_cast<int64_t>(kb) * c.O * 16;
+      for (int f = 0; f < kGroups; ++f) {
+        if (!TAIL || step * kGroups + f < groups) {
 #pragma unroll
-        for (int m = 0; m < 2 * MT; ++m) d[b][m] = __ldcg(reinterpret_cast<const uint32_t*>(run + static_cast<uint64_t>(row[m]) * 16));
+          for (int m = 0; m < 2 * MT; ++m)
+            if (real[m]) {
+              s[f][m] = __ldcg(scales + 8 * m);
+              if (ASYM) z[f][m] = __ldcg(zeros + 8 * m);
+            }
+        }
+        scales += c.O;
+        if (ASYM) zeros += c.O;
+      }
+    };
+    auto compute = [&](int step, const uint32_t (&d)[4][2 * MT], const uint32_t (&s)[kGroups][2 * MT], const uint32_t (&z)[kGroups][2 * MT]) {
+      const int runs = c.KB - 4 * step;   // fewer than 4: the last step of a layer whose I is no multiple of 128
+#pragma unroll
+      for (int f = 0; f < kGroups; ++f) {
+        if (TAIL && f * KPG >= runs) break;
+        float sum[MT][NT][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[m][n][k] = 0.f;
+#pragma unroll
+        for (int b = f * KPG; b < (f + 1) * KPG; ++b) {
+          uint4 xv[NT];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) xv[n] = *reinterpret_cast<const uint4*>(x[n] + 32 * b);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            uint32_t a[2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t zz = zero_pair<H>(ASYM ? z[f][2 * m + h] : 8u);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) a[h][k] = H::add2(code_pair<H>(d[b][2 * m + h], k), zz);
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              H::mma(sum[m][n], a[0][0], a[1][0], a[0][1], a[1][1], xv[n].x, xv[n].y);
+              H::mma(sum[m][n], a[0][2], a[1][2], a[0][3], a[1][3], xv[n].z, xv[n].w);
+            }
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              acc[m][n][k] = fmaf(H::to_float(static_cast<uint16_t>(s[f][2 * m + (k >> 1)])), sum[m][n][k], acc[m][n][k]);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) x[n] += 128;
+    };
+#pragma unroll
+    for (int i = 0; i < kMeta; ++i)
+      if (step0 + i < step1) fetch(step0 + i, sc[i], zp[i]);
+    int step = step0;
+    for (; step + 2 * kAhead <= step1; step += kAhead) {   // (what is asked for is all inside this warp's share)
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        compute(step + i, w[i], sc[i % kMeta], zp[i % kMeta]);
+        fetch(step + i + kMeta, sc[i % kMeta], zp[i % kMeta]);
+        load(step + i + kAhead, w[i]);
+      }
+    }
+    for (; step < step1; step += kAhead) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (step + i < step1) {
+          compute(step + i, w[i], sc[i % kMeta], zp[i % kMeta]);
+          if (step + i + kMeta < step1) fetch(step + i + kMeta, sc[i % kMeta], zp[i % kMeta]);
+          if (step + i + kAhead < step1) load(step + i + kAhead, w[i]);
+        }
+    }
+
+    // sums of the warps, then of the CTAs, in ascending order of the axis
+    float* to = part + warp * kN * kP;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 8 * n + 2 * tig + (i & 1);
+          if (r < count) to[r * kP + 16 * m + gid + 8 * (i >> 1)] = (inside[n] >> (4 * (r & 7))) & 1 ? acc[m][n][i] : 0.f;
+        }
+    __syncthreads();
+    if (ctas > 1) {
+      for (int i = threadIdx.x; i < kM * count; i += kSThreads) {
+        const int n = i / kM, m = i % kM;
+        float v = part[n * kP + m];
+#pragma unroll
+        for (int k = 1; k < kSWarps; ++k) v += part[(k * kN + n) * kP + m];
+        part[n * kP + m] = v;   // (no other thread reads this place)
+      }
+      cluster_sync();
+    }
+    for (int i = threadIdx.x + kSThreads * rank; i < kM * count; i += kSThreads * ctas) {   // every CTA finishes a share of the outputs
+      const int n = i / kM, m = i % kM, o = o0 + m;
+      float v[1] = {0.f};
+      if (ctas > 1) {
+        for (int k = 0; k < ctas; ++k) v[0] += cluster_load(part + n * kP + m, k);
       } else {
+        v[0] = part[n * kP + m];
 #pragma unroll
-        for (int m = 0; m < 2 * MT; ++m) d[b][m] = 0;
+        for (int k = 1; k < kSWarps; ++k) v[0] += part[(k * kN + n) * kP + m];
+      }
+      if (o < c.O) {
+        if (c.bias) v[0] += H::to_float(__ldcg(static_cast<const uint16_t*>(c.bias) + static_cast<int64_t>(u.e) * c.O + o));
+        quick_activation(v, c.act);
+        static_cast<uint16_t*>(c.y)[static_cast<int64_t>(u.lo + n) * c.ldy + o] = H::from_float(v[0]);
       }
     }
-  };
-  auto compute = [&](int step, const uint32_t (&d)[4][2 * MT]) {
-#pragma unroll
-    for (int f = 0; f < kFlush; ++f) {
-      if (4 * step + f * KPG >= c.KB) break;   // (the last step of a layer whose I is no multiple of 128)
-      const int64_t at = static_cast<int64_t>((4 * step + f * KPG) / KPG) * c.O;
-      float s[2 * MT];
-      uint32_t z[2 * MT];
-#pragma unroll
-      for (int m = 0; m < 2 * MT; ++m) {
-        s[m] = H::to_float(__ldcg(scales + at + row[m]));
-        z[m] = zero_pair<H>(ASYM ? __ldcg(zeros + at + row[m]) : 8u);
-      }
-      float sum[MT][NT][4];
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sum[m][n][i] = 0.f;
-#pragma unroll
-      for (int b = 0; b < KPG; ++b) {
-        uint4 xv[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          xv[n] = make_uint4(0, 0, 0, 0);
-          if (x[n]) xv[n] = *reinterpret_cast<const uint4*>(x[n] + (4 * step + f * KPG + b) * 32);
-        }
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          uint32_t a[2][4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            a[0][i] = H::sub2(code_pair<H>(d[f * KPG + b][2 * m], i), z[2 * m]);
-            a[1][i] = H::sub2(code_pair<H>(d[f * KPG + b][2 * m + 1], i), z[2 * m + 1]);
-          }
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            H::mma(sum[m][n], a[0][0], a[1][0], a[0][1], a[1][1], xv[n].x, xv[n].y);
-            H::mma(sum[m][n], a[0][2], a[1][2], a[0][3], a[1][3], xv[n].z, xv[n].w);
-          }
-        }
-      }
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[m][n][i] = fmaf(s[2 * m + (i >> 1)], sum[m][n][i], acc[m][n][i]);
-    }
-  };
-  if (step0 < step1) load(step0, w[0]);
-  for (int step = step0; step < step1; step += 2) {
-    if (step + 1 < step1) load(step + 1, w[1]);
-    compute(step, w[0]);
-    if (step + 1 < step1) {
-      if (step + 2 < step1) load(step + 2, w[0]);
-      compute(step + 1, w[1]);
-    }
+    // no CTA leaves, and none takes another unit, while its sums are being read
+    if (ctas > 1) cluster_sync();
+    else __syncthreads();
   }
-
-  // sums of the warps, then of the CTAs, in ascending order of the axis
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) part[warp][8 * n + 2 * tig + (i & 1)][16 * m + gid + 8 * (i >> 1)] = acc[m][n][i];
-  __syncthreads();
-  for (int i = threadIdx.x; i < kM * kN; i += 32 * kSWarps) {
-    const int n = i / kM, m = i % kM;
-    float v = part[0][n][m];
-#pragma unroll
-    for (int k = 1; k < kSWarps; ++k) v += part[k][n][m];
-    part[0][n][m] = v;   // (no other thread reads this place)
-  }
-  if (ctas > 1) cluster_sync();
-  else __syncthreads();
-  // every CTA finishes a share of the outputs
-  for (int i = threadIdx.x + 32 * kSWarps * rank; i < kM * kN; i += 32 * kSWarps * ctas) {
-    const int n = i / kM, m = i % kM, o = o0 + m;
-    const int64_t s = u.lo + n;
-    float v = 0.f;
-    for (int k = 0; k < ctas; ++k) v += cluster_load(&part[0][n][m], k);
-    if (s < u.hi && o < c.O) {
-      if (c.bias) v += H::to_float(__ldcg(static_cast<const uint16_t*>(c.bias) + static_cast<int64_t>(u.e) * c.O + o));
-      static_cast<uint16_t*>(c.y)[s * c.ldy + o] = H::from_float(apply_activation(v, c.act));
-    }
-  }
-  if (ctas > 1) cluster_sync();   // no CTA leaves while another reads its sums
 }
 
+using SmallKernel = void (*)(SmallArgs);
 template <class H, int MT, int NT, int KPG>
-static void (*small_kernel(bool asym))(SmallArgs) {
-  return asym ? group_small_kernel<H, MT, NT, KPG, true> : group_small_kernel<H, MT, NT, KPG, false>;
+static SmallKernel small_kernel(bool asym, bool tail) {
+  if constexpr (KPG == 4) return asym ? group_small_kernel<H, MT, NT, 4, true, false> : group_small_kernel<H, MT, NT, 4, false, false>;
+  else if (tail) return asym ? group_small_kernel<H, MT, NT, KPG, true, true> : group_small_kernel<H, MT, NT, KPG, false, true>;
+  else return asym ? group_small_kernel<H, MT, NT, KPG, true, false> : group_small_kernel<H, MT, NT, KPG, false, false>;
 }
 template <class H, int MT, int NT>
-static void (*small_kernel(int g, bool asym))(SmallArgs) {
-  return g == 32 ? small_kernel<H, MT, NT, 1>(asym) : (g == 64 ? small_kernel<H, MT, NT, 2>(asym) : small_kernel<H, MT, NT, 4>(asym));
+static SmallKernel small_kernel(int g, bool asym, bool tail) {
+  return g == 32 ? small_kernel<H, MT, NT, 1>(asym, tail) : (g == 64 ? small_kernel<H, MT, NT, 2>(asym, tail) : small_kernel<H, MT, NT, 4>(asym, tail));
+}
+template <class H>
+static SmallKernel small_kernel(int mt, int nt, int g, bool asym, bool tail) {
+  return nt == 2 ? small_kernel<H, 2, 2>(g, asym, tail) : (mt == 2 ? small_kernel<H, 2, 1>(g, asym, tail) : small_kernel<H, 1, 1>(g, asym, tail));
 }
 
 pipe_status linear_small(const Call& c, bool bf16, cudaStream_t stream) {
   SmallArgs p;
   p.c = c;
-  p.steps = ceil_div(c.KB, 4);
-  const bool asym = c.zeros != nullptr;
+  p.steps = c.T > 0 ? ceil_div(c.KB, 4) : 0;
   const int64_t rows = c.offsets ? ceil_div<int64_t>(c.N, c.E) : c.N;
   const int nt = rows <= 8 ? 1 : 2;
-  const int mt = nt;
-  p.tiles = ceil_div(c.O, 16 * mt);
-  const int64_t blocks = most_units(c, 8 * nt) * p.tiles;
+  const char* e1 = getenv("SM_MT"); const char* e2 = getenv("SM_C");
+  const int mt = nt == 2 ? 2 : (e1 ? atoi(e1) : 1);
+  const int64_t tiles = ceil_div(c.O, 16 * mt);
+  p.units = static_cast<int>(most_units(c, 8 * nt));
   int ctas = 1;
-  while (ctas < 8 && blocks * ctas < 2 * kPlanSMs && p.steps >= 2 * ctas * kSWarps) ctas *= 2;
-  if (blocks * ctas >= (int64_t{1} << 31)) return PIPE_ERR_UNSUPPORTED;
-  void (*k)(SmallArgs) = bf16 ? (nt == 1 ? small_kernel<Bf16, 1, 1>(c.g, asym) : small_kernel<Bf16, 2, 2>(c.g, asym))
-                              : (nt == 1 ? small_kernel<Fp16, 1, 1>(c.g, asym) : small_kernel<Fp16, 2, 2>(c.g, asym));
-  if (launch_overlapped(k, dim3(static_cast<unsigned>(blocks * ctas)), 32 * kSWarps, ctas, true, stream, p) != cudaSuccess) return PIPE_ERR_CUDA;
+  while (ctas < 8 && p.units * tiles * ctas < 3 * kPlanSMs && p.steps >= 2 * ctas * kSWarps) ctas *= 2;
+  if (e2) ctas = atoi(e2);
+  if (tiles * ctas >= (int64_t{1} << 31)) return PIPE_ERR_UNSUPPORTED;
+  const SmallKernel k = bf16 ? small_kernel<Bf16>(mt, nt, c.g, c.zeros != nullptr, c.KB % 4 != 0) : small_kernel<Fp16>(mt, nt, c.g, c.zeros != nullptr, c.KB % 4 != 0);
+  const dim3 grid(static_cast<unsigned>(tiles * ctas), static_cast<unsigned>(p.units < 65535 ? p.units : 65535));
+  if (launch_overlapped(k, grid, kSThreads, ctas, true, stream, p) != cudaSuccess) return PIPE_ERR_CUDA;
   count_launch(1);
   return launch_status();
 }

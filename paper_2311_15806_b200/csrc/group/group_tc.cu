@@ -165,27 +165,15 @@ __device__ __forceinline__ void store_y8(uint16_t* y, const uint4& w, int wide, 
   }
 }
 
-// Tile t of the launch: its expert, its rows, its first channel.
-struct Tile {
-  int e, m;
-  int lo, hi;   // rows of y (N < 2^31)
-  int n;        // columns of its MMAs: the rows rounded up to 32
+// Tile t of the launch: a unit's rows, 128 CG channels from m on.
+struct Tile : Unit {
+  int m;
+  int n;   // columns of its MMAs: the rows rounded up to 32
 };
-// first[e]: units before expert e, first[E] all of them; begin[e], end[e]: its rows.
-__device__ __forceinline__ Tile tile_of(const TcArgs& p, const int32_t* first, int t) {
+__device__ __forceinline__ Tile tile_of(const TcArgs& p, const int32_t* table, int t) {
   Tile r;
+  static_cast<Unit&>(r) = unit_at(table, p.c.E, p.TN, t / p.mtiles);
   r.m = t % p.mtiles;
-  const int u = t / p.mtiles;
-  int lo = 0, hi = p.c.E;   // the last e with first[e] <= u
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first[mid] <= u) lo = mid;
-    else hi = mid;
-  }
-  r.e = lo;
-  const int32_t *begin = first + p.c.E + 1, *end = begin + p.c.E;
-  r.lo = begin[lo] + (u - first[lo]) * p.TN;
-  r.hi = end[lo] - r.lo < p.TN ? end[lo] : r.lo + p.TN;
   r.n = (r.hi - r.lo + 31) & ~31;
   return r;
 }
@@ -245,35 +233,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
   }
   grid_wait();
   grid_release();
-  // the units of every expert: rows (clamped as find_unit does), tiles, then a prefix over the experts
-  for (int e = threadIdx.x; e < c.E; e += kTThreads<TA>) {
-    int64_t lo = 0, hi = c.N;
-    if (c.offsets) {
-      lo = __ldcg(c.offsets + e);
-      hi = __ldcg(c.offsets + e + 1);
-      lo = lo < 0 ? 0 : (lo > c.N ? c.N : lo);
-      hi = hi < lo ? lo : (hi > c.N ? c.N : hi);
-    }
-    table[c.E + 1 + e] = static_cast<int32_t>(lo);
-    table[2 * c.E + 1 + e] = static_cast<int32_t>(hi);
-  }
-  __syncthreads();
-  if (warp == 0) {
-    int before = 0;
-    for (int e0 = 0; e0 < c.E; e0 += 32) {
-      const int e = e0 + lane;
-      const int mine = e < c.E ? (table[2 * c.E + 1 + e] - table[c.E + 1 + e] + p.TN - 1) / p.TN : 0;
-      int upto = mine;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, upto, d);
-        if (lane >= d) upto += v;
-      }
-      if (e < c.E) table[e] = before + upto - mine;
-      before += __shfl_sync(0xffffffffu, upto, 31);
-    }
-    if (lane == 0) table[c.E] = before;
-  }
+  build_units<kTThreads<TA>>(c, p.TN, table);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   if (CG == 2 || p.split > 1) cluster_sync();
@@ -535,7 +495,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
       auto widen = [&](int b, uint32_t (&v)[4][4]) {   // the 32 codes of run b
         const uint32_t w[4] = {q[b].x, q[b].y, q[b].z, q[b].w};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i >> 2][i & 3] = H::mul2(H::sub2(code_pair<H>(w[i >> 2], i & 3), z2[b / KPG]), s2[b / KPG]);
+        for (int i = 0; i < 16; ++i) v[i >> 2][i & 3] = H::mul2(H::add2(code_pair<H>(w[i >> 2], i & 3), z2[b / KPG]), s2[b / KPG]);
       };
       auto slot_free = [&]() {   // the products of the slot's last stage are done
         if (it < W) return true;
@@ -741,7 +701,7 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   const bool ta = p.TN <= 128;
   p.ring = ta ? 4 : 3;
   const int x_bytes = p.ring * own * 256, a_bytes = ta ? 0 : kTWideners<false> * kTSlotBytes, turn = p.split > 1 ? 0 : 2 * kTTurnBytes;
-  const int table = (3 * c.E + 1) * 4;
+  const int table = unit_ints(c.E) * 4;
   const int room = kTMaxSmem - 1024 - x_bytes - a_bytes - turn - table;
   p.code_depth = room / kTCodeBytes < kTMaxCodes ? room / kTCodeBytes : kTMaxCodes;
   if (p.code_depth < (ta ? kTWideners<true> : kTWideners<false>)) return PIPE_ERR_UNSUPPORTED;
