@@ -9,8 +9,6 @@
 // share the reduction axis in steps of 128 codes.  A warp's activations are asked into L1, which the CTAs of an SM share, at once;
 // codes, scales and zero points of its next steps are in flight in registers (copies through shared memory cost more instructions
 // than the arithmetic).  Sums are added in a fixed order.
-#include <cstdlib>
-
 #include "group_common.cuh"
 
 namespace pipe {
@@ -67,7 +65,7 @@ __device__ __forceinline__ bool find_unit(const Call& c, int u, int per, Unit& o
 // NT: 8-column tiles (rows of a unit: 8 NT); KPG: runs of 32 codes per group.
 // TAIL: I is no multiple of 128, the last step has fewer runs.
 template <class H, int MT, int NT, int KPG, bool ASYM, bool TAIL>
-__global__ void __launch_bounds__(kSThreads, MT == 1 ? 5 : (NT == 1 ? 4 : 3)) group_small_kernel(SmallArgs p) {
+__global__ void __launch_bounds__(kSThreads, MT == 1 ? 5 : (MT * NT == 2 ? 4 : 3)) group_small_kernel(SmallArgs p) {
   constexpr int kM = 16 * MT, kN = 8 * NT, kP = kM + 4;   // kP: pitch of a row of sums (its writers then meet different banks)
   constexpr int kGroups = 4 / KPG;                         // groups of a step
   constexpr int kAhead = MT == 1 ? 4 : 2;                  // steps of codes in registers
@@ -291,7 +289,7 @@ static SmallKernel small_kernel(int g, bool asym, bool tail) {
 }
 template <class H>
 static SmallKernel small_kernel(int mt, int nt, int g, bool asym, bool tail) {
-  return nt == 2 ? small_kernel<H, 2, 2>(g, asym, tail) : (mt == 2 ? small_kernel<H, 2, 1>(g, asym, tail) : small_kernel<H, 1, 1>(g, asym, tail));
+  return nt == 2 ? small_kernel<H, 2, 2>(g, asym, tail) : (mt == 4 ? small_kernel<H, 4, 1>(g, asym, tail) : (mt == 2 ? small_kernel<H, 2, 1>(g, asym, tail) : small_kernel<H, 1, 1>(g, asym, tail)));
 }
 
 pipe_status linear_small(const Call& c, bool bf16, cudaStream_t stream) {
@@ -300,13 +298,26 @@ pipe_status linear_small(const Call& c, bool bf16, cudaStream_t stream) {
   p.steps = c.T > 0 ? ceil_div(c.KB, 4) : 0;
   const int64_t rows = c.offsets ? ceil_div<int64_t>(c.N, c.E) : c.N;
   const int nt = rows <= 8 ? 1 : 2;
-  const char* e1 = getenv("SM_MT"); const char* e2 = getenv("SM_C");
-  const int mt = nt == 2 ? 2 : (e1 ? atoi(e1) : 1);
-  const int64_t tiles = ceil_div(c.O, 16 * mt);
+  // Channels of a tile (16 mt) and CTAs that share an axis: a round of CTAs costs some 3 us before its first product (launch, addresses,
+  // first loads), and each step of a warp's share 0.3, 0.46 or 0.85 us (mt = 1, 2, 4; two column tiles 0.75).  Measured against this
+  // (one token): 4096 -> 11008 mt = 1 alone 8.2 us, with two CTAs to a tile 12.0, mt = 2 alone 9.4; 11008 -> 4096 mt = 2 with four 8.5,
+  // with two 10.0, mt = 1 with two 10.7, with four 14.7; 54 units of 2048 -> 1408 mt = 4 18, mt = 2 20, mt = 1 32.
   p.units = static_cast<int>(most_units(c, 8 * nt));
-  int ctas = 1;
-  while (ctas < 8 && p.units * tiles * ctas < 3 * kPlanSMs && p.steps >= 2 * ctas * kSWarps) ctas *= 2;
-  if (e2) ctas = atoi(e2);
+  int mt = 0, ctas = 0;
+  int64_t best = 0;
+  for (int m = nt; m <= (nt == 2 ? 2 : 4); m *= 2)
+    for (int k = 1; k == 1 || (k <= 8 && p.steps >= k * kSWarps); k *= 2) {
+      const int per_sm = nt == 2 || m == 4 ? 3 : (m == 2 ? 4 : 5);   // CTAs that an SM holds (by registers)
+      const int64_t blocks = p.units * ceil_div<int64_t>(c.O, 16 * m) * k;
+      const int64_t step_cost = nt == 2 ? 75 : (m == 1 ? 30 : (m == 2 ? 46 : 85));
+      const int64_t cost = ceil_div<int64_t>(blocks, per_sm * kPlanSMs) * (300 + (k > 1 ? 50 : 0) + step_cost * ceil_div(p.steps, k * kSWarps));
+      if (!mt || cost < best) {
+        best = cost;
+        mt = m;
+        ctas = k;
+      }
+    }
+  const int64_t tiles = ceil_div(c.O, 16 * mt);
   if (tiles * ctas >= (int64_t{1} << 31)) return PIPE_ERR_UNSUPPORTED;
   const SmallKernel k = bf16 ? small_kernel<Bf16>(mt, nt, c.g, c.zeros != nullptr, c.KB % 4 != 0) : small_kernel<Fp16>(mt, nt, c.g, c.zeros != nullptr, c.KB % 4 != 0);
   const dim3 grid(static_cast<unsigned>(tiles * ctas), static_cast<unsigned>(p.units < 65535 ? p.units : 65535));
