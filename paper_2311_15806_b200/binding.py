@@ -469,26 +469,51 @@ def _wants(where: str, ok: bool, what: str) -> None:
 def _on_current(where: str, first: torch.Tensor, *others) -> None:
     """Every tensor lies on the current device: the library launches there, on that device's stream."""
     dev = first.get_device()
-    if dev < 0 or dev != _current_device() or any(t is not None and t.get_device() != dev for t in others):
+    ok = dev >= 0 and dev == _current_device()
+    for t in others:
+        ok = ok and (t is None or t.get_device() == dev)
+    if not ok:
         raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: all tensors have to be on the current device")
 
 
 def _rows_of(where: str, t: torch.Tensor, cols: int) -> int:
     """Row pitch of a [rows, cols] matrix whose rows are contiguous."""
-    if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
-        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: a matrix of shape {tuple(t.shape)} and strides {t.stride()}, {cols} contiguous columns are needed")
-    return t.stride(0) if t.shape[0] > 1 else max(cols + 7 & ~7, t.stride(0) & ~7)
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[1] != cols or (stride[1] != 1 and cols > 1):
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: a matrix of shape {tuple(shape)} and strides {stride}, {cols} contiguous columns are needed")
+    return stride[0] if shape[0] > 1 else max(cols + 7 & ~7, stride[0] & ~7)
+
+
+def _weight_rows_of(where: str, t: torch.Tensor, E: int, O: int, I: int) -> int:
+    """Row pitch of weights [E, O, I] or [E * O, I] whose rows are contiguous and at one distance."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 3 and shape[0] == E and shape[1] == O and shape[2] == I and (stride[2] == 1 or I == 1):
+        if E == 1:
+            return stride[1] if O > 1 else max(I, stride[1])
+        if O == 1:
+            return stride[0]
+        if stride[0] == O * stride[1]:
+            return stride[1]
+    elif len(shape) == 2 and shape[0] == E * O and shape[1] == I and (stride[1] == 1 or I == 1):
+        return stride[0] if E * O > 1 else max(I, stride[0])
+    raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: weights of shape {tuple(shape)} and strides {stride}, rows of {I} at one distance are needed")
+
+
+_GROUP_DTYPES = (torch.bfloat16, torch.float16)
 
 
 def _group_arrays(where: str, desc: GroupDesc, codes, scales, zeros, *others) -> torch.dtype:
     """Checks the three arrays of a layer against the descriptor; the layer's torch type."""
-    E, O, I, g = desc.experts, desc.out_features, desc.in_features, desc.group_size
-    h = torch.bfloat16 if desc.dtype == DTYPE_BF16 else torch.float16
-    if codes.dtype != torch.uint8 or scales.dtype != h or codes.numel() * 2 != E * O * I or scales.numel() * g != E * O * I \
-            or not codes.is_contiguous() or not scales.is_contiguous():
+    n = desc.experts * desc.out_features * desc.in_features
+    h = _GROUP_DTYPES[desc.dtype]
+    g = desc.group_size
+    if codes.dtype != torch.uint8 or scales.dtype != h or codes.numel() * 2 != n or scales.numel() * g != n or not codes.is_contiguous() \
+            or not scales.is_contiguous():
         raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: codes / scales are not the descriptor's arrays")
-    if (zeros is not None) != bool(desc.asymmetric) or \
-            (zeros is not None and (zeros.dtype != torch.uint8 or zeros.numel() * g != E * O * I or not zeros.is_contiguous())):
+    if zeros is None:
+        if desc.asymmetric:
+            raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: an asymmetric layer has zeros")
+    elif not desc.asymmetric or zeros.dtype != torch.uint8 or zeros.numel() * g != n or not zeros.is_contiguous():
         raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: zeros are not the descriptor's array")
     _on_current(where, codes, scales, zeros, *others)
     return h
@@ -497,21 +522,17 @@ def _group_arrays(where: str, desc: GroupDesc, codes, scales, zeros, *others) ->
 def pipe_group_quantize(desc: GroupDesc, W: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor | None = None,
                         values: torch.Tensor | None = None, stream=None) -> None:
     """W: cuda float32 / bfloat16 / float16 [E, O, I] or [E*O, I]; codes, scales, zeros: the layer's arrays (see alloc_group);
-    values: float32 of W's shape, or None."""
+    values: float32 of either shape, or None."""
     where = "pipe_group_quantize"
     _group_arrays(where, desc, codes, scales, zeros, W, values)
-    rows, I = desc.experts * desc.out_features, desc.in_features
-    _wants(where, W.dtype in _DTYPES and W.numel() == rows * I, "W is not the descriptor's weights")
-    W = W.view(rows, I) if W.dim() != 2 else W
-    ldv = 0
+    E, O, I = desc.experts, desc.out_features, desc.in_features
+    w_dtype = _DTYPES.get(W.dtype, -1)
+    ldw, ldv, v = _weight_rows_of(where, W, E, O, I), 0, None
     if values is not None:
-        _wants(where, values.dtype == torch.float32 and values.numel() == rows * I, "values have another shape or type")
-        values = values.view(rows, I) if values.dim() != 2 else values
-        _wants(where, I == 1 or values.stride(1) == 1, "values: rows are not contiguous")
-        ldv = values.stride(0) if rows > 1 else max(I, values.stride(0))
-    _wants(where, I == 1 or W.stride(1) == 1, "W: rows are not contiguous")
-    _check(lib().pipe_group_quantize(C.byref(desc), W.data_ptr(), _DTYPES[W.dtype], W.stride(0) if rows > 1 else max(I, W.stride(0)),
-                                     codes.data_ptr(), scales.data_ptr(), _dp(zeros), _dp(values), ldv, _stream_ptr(stream)), where)
+        _wants(where, values.dtype == torch.float32, "values are float32")
+        ldv, v = _weight_rows_of(where, values, E, O, I), values.data_ptr()
+    _check(lib().pipe_group_quantize(C.byref(desc), W.data_ptr(), w_dtype, ldw, codes.data_ptr(), scales.data_ptr(), _dp(zeros), v, ldv,
+                                     _stream_ptr(stream)), where)
 
 
 def pipe_group_linear(desc: GroupDesc, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor | None, x: torch.Tensor,
@@ -519,10 +540,15 @@ def pipe_group_linear(desc: GroupDesc, codes: torch.Tensor, scales: torch.Tensor
     """x: cuda [T, I], y: cuda [T, O], bias: [O] (or [1, O]), all in the layer's type."""
     where = "pipe_group_linear"
     h = _group_arrays(where, desc, codes, scales, zeros, x, y, bias)
-    _wants(where, x.dtype == h and y.dtype == h and x.shape[0] == y.shape[0], "x and y differ in rows or from the layer's type")
-    _wants(where, bias is None or (bias.dtype == h and bias.numel() == desc.out_features and bias.is_contiguous()), "bias")
-    _check(lib().pipe_group_linear(C.byref(desc), codes.data_ptr(), scales.data_ptr(), _dp(zeros), x.data_ptr(), x.shape[0],
-                                   _rows_of(where, x, desc.in_features), _dp(bias), activation, y.data_ptr(),
+    T = x.shape[0]
+    if x.dtype != h or y.dtype != h or T != y.shape[0]:
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: x and y differ in rows or from the layer's type")
+    b = None
+    if bias is not None:
+        _wants(where, bias.dtype == h and bias.numel() == desc.out_features and bias.is_contiguous(), "bias")
+        b = bias.data_ptr()
+    _check(lib().pipe_group_linear(C.byref(desc), codes.data_ptr(), scales.data_ptr(), _dp(zeros), x.data_ptr(), T,
+                                   _rows_of(where, x, desc.in_features), b, activation, y.data_ptr(),
                                    _rows_of(where, y, desc.out_features), _stream_ptr(stream)), where)
 
 
@@ -530,7 +556,9 @@ def pipe_expert_rows(choice: torch.Tensor, experts: int, offsets: torch.Tensor, 
     """choice: cuda int32 [T, k]; offsets: int32 [experts + 1]; rows: int32 [T*k]; slots: int32 [T, k]."""
     where = "pipe_expert_rows"
     _on_current(where, choice, offsets, rows, slots)
-    _wants(where, choice.dim() == 2 and all(t.dtype == torch.int32 and t.is_contiguous() for t in (choice, offsets, rows, slots)),
+    i32 = torch.int32
+    _wants(where, choice.dim() == 2 and choice.dtype == i32 and offsets.dtype == i32 and rows.dtype == i32 and slots.dtype == i32 and
+           choice.is_contiguous() and offsets.is_contiguous() and rows.is_contiguous() and slots.is_contiguous(),
            "int32 tensors with contiguous entries are needed")
     T, k = choice.shape
     _wants(where, offsets.numel() == experts + 1 and rows.numel() == T * k and slots.numel() == T * k, "sizes do not match the choice")

@@ -26,14 +26,27 @@ struct QuantArgs {
   int* status;
 };
 
-// The integer nearest the exact quotient w / s (s > 0), ties to even.  q0, from a rounded quotient, is off by one at most; the
-// remainder w - q0 s is exact: w has 24 bits, s at most 11 and q0 few, so the remainder, no larger than w unless q0 is 0, is a
-// whole number of units of w's last place.
-__device__ __forceinline__ float nearest_code(float w, float s, float inv, bool fast) {
-  float q = rintf(fast ? __fmul_rn(w, inv) : __fdiv_rn(w, s));
+// The integers nearest the exact quotients w / s (s > 0), ties to even.  An estimate rounded by an addition (1.5 * 2^23, where the
+// spacing of binary32 is one) is off by one at most.  The remainder w - q s is exact: w has 24 bits, s at most 11 and q few, so the
+// remainder, no larger than w unless q is 0, is a whole number of units of w's last place.  Only where it reaches half a step, on a
+// tie or where the estimate went wrong, is anything more done.
+__device__ __forceinline__ float settle_code(float w, float s, float q) {
   const float r = fmaf(-q, s, w), twice = 2.f * fabsf(r);
   if (twice > s || (twice == s && (static_cast<int>(q) & 1))) q += r > 0.f ? 1.f : -1.f;
   return q;
+}
+template <int N>
+__device__ __forceinline__ void nearest_codes(const float (&w)[N], float s, float inv, bool fast, float (&q)[N]) {
+  float edge = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    q[i] = __fsub_rn(__fadd_rn(fast ? __fmul_rn(w[i], inv) : __fdiv_rn(w[i], s), 12582912.f), 12582912.f);
+    edge = fmaxf(edge, fabsf(fmaf(-q[i], s, w[i])));
+  }
+  if (2.f * edge >= s) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) q[i] = settle_code(w[i], s, q[i]);
+  }
 }
 
 template <class S>
@@ -105,16 +118,25 @@ __global__ void __launch_bounds__(kQThreads) group_quantize_kernel(QuantArgs a) 
   const bool fast = quant_step_is_fast(s);
   const float inv = fast ? __frcp_rn(s) : 0.f;
   float z = ASYM ? 0.f : 8.f;
-  if (ASYM && s > 0.f) z = fminf(nearest_code(-lo, s, inv, fast), 15.f);
-  uint32_t word = 0;
+  uint32_t word = ASYM ? 0u : 0x88888888u;
   float c[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float q = 0.f;
-    if (s > 0.f && finite) q = nearest_code(w[i], s, inv, fast);
-    q = ASYM ? fminf(fmaxf(q + z, 0.f), 15.f) : fminf(fmaxf(q, -7.f), 7.f) + 8.f;
-    c[i] = q - z;
-    word |= static_cast<uint32_t>(q) << (4 * ((i >> 1) + 4 * (i & 1)));
+  for (int i = 0; i < 8; ++i) c[i] = 0.f;
+  if (s > 0.f && finite) {
+    if (ASYM) {
+      float first[1] = {-lo}, q[1];
+      nearest_codes(first, s, inv, fast, q);
+      z = fminf(q[0], 15.f);
+    }
+    float q[8];
+    nearest_codes(w, s, inv, fast, q);
+    word = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      c[i] = ASYM ? fminf(fmaxf(q[i], -z), 15.f - z) : fminf(fmaxf(q[i], -7.f), 7.f);
+      // (the code in the low bits of a sum on top of 2^23)
+      word |= (__float_as_uint(c[i] + (8388608.f + z)) & 15u) << (4 * ((i >> 1) + 4 * (i & 1)));
+    }
   }
   if (!here) return;
   const int64_t e = row / a.O;
