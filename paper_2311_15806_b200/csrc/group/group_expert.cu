@@ -5,87 +5,198 @@
 namespace pipe {
 namespace grp {
 
-// ---- rows by expert: a stable counting sort in one launch.  Every warp owns a run of the choice and counts its experts in a row
-// of shared memory of its own; the counts become first slots by a prefix over the warps, the CTAs of the cluster (distributed
-// shared memory) and the experts; then every warp walks its run again, 32 places at a time, equal experts among them ranked by a
-// match.  Integer counts only, so no order of atomics shows.  Bound by latency: two walks and three barriers.
-constexpr int kRWarps = 32;
-constexpr int kRCtas = 8;
+// ---- rows by expert: a stable counting sort.  Every warp owns a run of the choice and counts its experts in a row of shared memory
+// of its own; the counts become first slots by a prefix over the warps and the experts; then every warp walks its run again, 32 places
+// at a time, equal experts among them ranked by a match.  Integer counts only, so no order of atomics shows.  Bound by latency: up to
+// kROne places one CTA does all of it.  Beyond that the walks are the blocks' of a grid, between them one CTA's prefix over the blocks
+// (262144 places on 256 experts: one cluster of eight CTAs 41 us).  What the three launches hand on, the counts and then the first
+// slots of every block, lies in that block's own part of d_slots, which it overwrites at last.
+constexpr int kROne = 8192;       // most places of the one-launch form
+constexpr int kRBlock = 2048;     // places of a block (the last one: up to twice that), at least PIPE_MAX_EXPERTS
+static_assert(kRBlock >= PIPE_MAX_EXPERTS, "a block's part of d_slots holds a count per expert");
 
 struct RowsArgs {
   const int32_t* choice;
   int n, k, E;           // n = T * k places
-  int per;               // places of a warp, a multiple of 32
+  int blocks;
   int32_t *offsets, *rows, *slots;
 };
 
-__global__ void __launch_bounds__(32 * kRWarps) expert_rows_kernel(RowsArgs a) {
-  extern __shared__ int32_t smem[];   // count[kRWarps][E], total[E], first[E]
-  const int rank = cluster_rank(), ctas = cluster_ctas();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int32_t *count = smem + warp * a.E, *total = smem + kRWarps * a.E, *first = total + a.E;
-  __shared__ int32_t sums[kRWarps];
-  grid_wait();
-  grid_release();
+// Counts of this warp's run, one per expert.
+__device__ __forceinline__ void count_run(const RowsArgs& a, int begin, int end, int32_t* count) {
+  const int lane = threadIdx.x & 31;
   for (int e = lane; e < a.E; e += 32) count[e] = 0;
   __syncwarp();
-  const int64_t begin = static_cast<int64_t>(rank * kRWarps + warp) * a.per;
-  const int64_t end = begin + a.per < a.n ? begin + a.per : a.n;
-  for (int64_t i = begin + lane; i < end; i += 32) {
+#pragma unroll 4
+  for (int i = begin + lane; i < end; i += 32) {
     const int e = __ldcg(a.choice + i);
     if (e >= 0 && e < a.E) atomicAdd(count + e, 1);
   }
-  __syncthreads();
-  for (int e = tid; e < a.E; e += 32 * kRWarps) {
-    int run = 0;
-    for (int w = 0; w < kRWarps; ++w) {
-      const int v = smem[w * a.E + e];
-      smem[w * a.E + e] = run;
-      run += v;
-    }
-    total[e] = run;
-  }
-  cluster_sync();
-  // E <= PIPE_MAX_EXPERTS = the block's threads: one expert per thread
-  int before = 0, all = 0;
-  if (tid < a.E)
-    for (int r = 0; r < ctas; ++r) {
-      const int v = cluster_load(total + tid, r);
-      before += r < rank ? v : 0;
-      all += v;
-    }
-  int upto = all;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, upto, d);
-    if (lane >= d) upto += v;
-  }
-  if (lane == 31) sums[warp] = upto;
-  __syncthreads();
-  int base = 0;
-  for (int w = 0; w < warp; ++w) base += sums[w];
-  if (tid < a.E) {
-    first[tid] = base + upto - all + before;
-    if (rank == 0) {
-      a.offsets[tid] = base + upto - all;
-      if (tid == a.E - 1) a.offsets[a.E] = base + upto;
-    }
-  }
-  cluster_sync();   // (also: no CTA leaves while another reads its totals)
-  for (int64_t i0 = begin; i0 < end; i0 += 32) {
-    const int64_t i = i0 + lane;
-    int e = i < end ? __ldcg(a.choice + i) : -1;
+}
+// Places this warp's run; next[e]: the slot of the run's next place of expert e.
+__device__ __forceinline__ void place_run(const RowsArgs& a, int begin, int end, int32_t* next) {
+  const int lane = threadIdx.x & 31;
+  int coming = begin + lane < end ? __ldcg(a.choice + begin + lane) : -1;
+  for (int i0 = begin; i0 < end; i0 += 32) {
+    const int i = i0 + lane;
+    int e = coming;
+    coming = i + 32 < end ? __ldcg(a.choice + i + 32) : -1;
     if (e < 0 || e >= a.E) e = -1;
     const uint32_t same = __match_any_sync(0xffffffffu, e);
-    const int at = e >= 0 ? first[e] + count[e] + __popc(same & ((1u << lane) - 1)) : -1;
+    const int at = e >= 0 ? next[e] + __popc(same & ((1u << lane) - 1)) : -1;
     __syncwarp();
-    if (e >= 0 && lane == __ffs(same) - 1) count[e] += __popc(same);
+    if (e >= 0 && lane == 31 - __clz(same)) next[e] = at + 1;
     __syncwarp();
     if (i < end) {
       a.slots[i] = at;
-      if (at >= 0) a.rows[at] = static_cast<int32_t>(i) / a.k;
+      if (at >= 0) a.rows[at] = i / a.k;
     }
   }
+}
+// smem[w * E + e]: counts of WARPS warps -> the counts of the warps before; their sum is returned.
+template <int WARPS>
+__device__ __forceinline__ int prefix_warps(int32_t* smem, int E, int e) {
+  int v[WARPS], run = 0;
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) v[w] = smem[w * E + e];
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) {
+    smem[w * E + e] = run;
+    run += v[w];
+  }
+  return run;
+}
+// Exclusive prefix of one value per thread over 1024 threads; `all`: their sum.
+__device__ __forceinline__ int prefix_block(int v, int32_t* sums, int& all) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int upto = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, upto, d);
+    if (lane >= d) upto += u;
+  }
+  if (lane == 31) sums[warp] = upto;
+  __syncthreads();
+  int before = 0;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < 32; ++w) {
+    before += w < warp ? sums[w] : 0;
+    all += sums[w];
+  }
+  return before + upto - v;
+}
+
+__global__ void __launch_bounds__(1024) expert_rows_kernel(RowsArgs a) {
+  extern __shared__ int32_t smem[];   // [32][E]
+  __shared__ int32_t sums[32];
+  const int tid = threadIdx.x, warp = tid >> 5;
+  const int per = (a.n + 1023) / 1024 * 32;
+  const int begin = min(warp * per, a.n), end = min(begin + per, a.n);
+  grid_wait();
+  grid_release();
+  count_run(a, begin, end, smem + warp * a.E);
+  __syncthreads();
+  const int mine = tid < a.E ? prefix_warps<32>(smem, a.E, tid) : 0;   // E <= 1024: one expert per thread
+  int all;
+  const int first = prefix_block(mine, sums, all);
+  if (tid < a.E) {
+    a.offsets[tid] = first;
+    if (tid == a.E - 1) a.offsets[a.E] = all;
+#pragma unroll
+    for (int w = 0; w < 32; ++w) smem[w * a.E + tid] += first;
+  }
+  __syncthreads();
+  place_run(a, begin, end, smem + warp * a.E);
+}
+
+__device__ __forceinline__ int block_places(const RowsArgs& a) { return blockIdx.x == a.blocks - 1 ? a.n - static_cast<int>(blockIdx.x) * kRBlock : kRBlock; }
+
+__global__ void __launch_bounds__(256) expert_count_kernel(RowsArgs a) {
+  extern __shared__ int32_t smem[];   // [E]
+  grid_wait();
+  grid_release();
+  const int begin = static_cast<int>(blockIdx.x) * kRBlock, end = begin + block_places(a);
+  for (int e = threadIdx.x; e < a.E; e += 256) smem[e] = 0;
+  __syncthreads();
+#pragma unroll 8
+  for (int i = begin + threadIdx.x; i < end; i += 256) {
+    const int e = __ldcg(a.choice + i);
+    if (e >= 0 && e < a.E) atomicAdd(smem + e, 1);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.E; e += 256) a.slots[begin + e] = smem[e];
+}
+
+// The blocks' counts of every expert -> their first slots: neighbouring threads have neighbouring experts (a warp per expert with the
+// blocks as lanes, every load 32 sectors, took 70 us for 128 blocks of 256 experts), groups of threads a share of the blocks each.
+__global__ void __launch_bounds__(1024) expert_scan_kernel(RowsArgs a) {
+  __shared__ int32_t part[1024], total[PIPE_MAX_EXPERTS], sums[32];
+  const int tid = threadIdx.x;
+  grid_wait();
+  grid_release();
+  const int width = (a.E + 31) & ~31, groups = 1024 / width;
+  const int group = tid / width, e = tid - group * width;
+  const bool here = group < groups && e < a.E;
+  const int b0 = static_cast<int>(static_cast<int64_t>(a.blocks) * group / groups), b1 = static_cast<int>(static_cast<int64_t>(a.blocks) * (group + 1) / groups);
+  int run = 0;
+  if (here) {
+#pragma unroll 8
+    for (int b = b0; b < b1; ++b) run += __ldcg(a.slots + b * kRBlock + e);
+  }
+  part[tid] = run;
+  __syncthreads();
+  int mine = 0;
+  if (tid < a.E)
+    for (int g = 0; g < groups; ++g) mine += part[g * width + tid];
+  int all;
+  const int first = prefix_block(mine, sums, all);
+  if (tid < a.E) {
+    a.offsets[tid] = first;
+    if (tid == a.E - 1) a.offsets[a.E] = all;
+    total[tid] = first;
+  }
+  __syncthreads();
+  if (here) {
+    int at = total[e];
+    for (int g = 0; g < group; ++g) at += part[g * width + e];
+    int b = b0;
+    for (; b + 8 <= b1; b += 8) {   // (eight loads in flight)
+      int v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = __ldcg(a.slots + (b + i) * kRBlock + e);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        a.slots[(b + i) * kRBlock + e] = at;
+        at += v[i];
+      }
+    }
+    for (; b < b1; ++b) {
+      const int v = __ldcg(a.slots + b * kRBlock + e);
+      a.slots[b * kRBlock + e] = at;
+      at += v;
+    }
+  }
+}
+
+__global__ void __launch_bounds__(256) expert_place_kernel(RowsArgs a) {
+  extern __shared__ int32_t smem[];   // [8][E]
+  const int warp = threadIdx.x >> 5;
+  grid_wait();
+  grid_release();
+  const int first = static_cast<int>(blockIdx.x) * kRBlock, places = block_places(a);
+  const int per = (places + 255) / 256 * 32;
+  const int begin = first + min(warp * per, places), end = min(begin + per, first + places);
+  count_run(a, begin, end, smem + warp * a.E);
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.E; e += 256) {
+    prefix_warps<8>(smem, a.E, e);
+    const int at = __ldcg(a.slots + first + e);
+#pragma unroll
+    for (int w = 0; w < 8; ++w) smem[w * a.E + e] += at;
+  }
+  __syncthreads();   // (the block's first slots are read: its part of d_slots may be overwritten)
+  place_run(a, begin, end, smem + warp * a.E);
 }
 
 // ---- a token's experts joined: every output is k products in binary32; bound by reading the k rows.
@@ -159,29 +270,29 @@ extern "C" pipe_status pipe_expert_rows(const int32_t* d_choice, int64_t T, int3
   a.offsets = d_offsets;
   a.rows = d_rows;
   a.slots = d_slots;
-  // one CTA while its warps have few steps of 32 places each: a cluster costs two barriers across SMs
-  const int ctas = a.n <= 8 * 32 * grp::kRWarps ? 1 : grp::kRCtas;
-  a.per = static_cast<int>(round_up<int64_t>(ceil_div<int64_t>(a.n, ctas * grp::kRWarps), 32));
-  const size_t smem = static_cast<size_t>(grp::kRWarps + 2) * experts * 4;
-  if (smem > 48 * 1024 &&
-      cudaFuncSetAttribute(grp::expert_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
-    return PIPE_ERR_CUDA;
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = ctas;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.gridDim = dim3(ctas);
-  cfg.blockDim = dim3(32 * grp::kRWarps);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = static_cast<cudaStream_t>(stream);
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  if (cudaLaunchKernelEx(&cfg, grp::expert_rows_kernel, a) != cudaSuccess) return PIPE_ERR_CUDA;
-  count_launch(1);
-  take_expansion_mark(cfg.stream);
+  a.blocks = a.n / grp::kRBlock;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  auto launch = [&](void (*kernel)(grp::RowsArgs), int blocks, int threads, int smem) {
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return false;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) return false;
+    count_launch(1);
+    return true;
+  };
+  const bool ok = a.n <= grp::kROne ? launch(grp::expert_rows_kernel, 1, 1024, 32 * experts * 4)
+                                    : launch(grp::expert_count_kernel, a.blocks, 256, experts * 4) && launch(grp::expert_scan_kernel, 1, 1024, 0) &&
+                                          launch(grp::expert_place_kernel, a.blocks, 256, 8 * experts * 4);
+  if (!ok) return PIPE_ERR_CUDA;
+  take_expansion_mark(s);
   return launch_status();
 }
 
