@@ -627,15 +627,26 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
         float v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = 0.f;
-        for (int q = 0; q < p.split; ++q) {
-          const uint32_t a = cluster_address(sums + r * 128 + col, q);
+        // (loads of four CTAs in flight: one after the other, each some 1000 cycles, eight CTAs' took 10 us)
+        for (int q0 = 0; q0 < p.split; q0 += 4) {
+          float w[4][8];
 #pragma unroll
-          for (int k = 0; k < 8; k += 4) {
-            float w[4];
-            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(w[0]), "=f"(w[1]), "=f"(w[2]), "=f"(w[3]) : "r"(a + 4 * k) : "memory");
+          for (int q = 0; q < 4; ++q)
+            if (q0 + q < p.split) {
+              const uint32_t a = cluster_address(sums + r * 128 + col, q0 + q);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[k + j] += w[j];
-          }
+              for (int k = 0; k < 8; k += 4)
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(w[q][k]), "=f"(w[q][k + 1]), "=f"(w[q][k + 2]), "=f"(w[q][k + 3])
+                             : "r"(a + 4 * k)
+                             : "memory");
+            }
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (q0 + q < p.split) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k) v[k] += w[q][k];
+            }
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -678,22 +689,54 @@ static bool encode_2d(CUtensorMap* map, CUtensorMapDataType type, const void* ba
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The tile's rows (p->TN), the CTAs of a tile (*cg) and those that share its axis (p->split): the least of
+//     rounds of tiles on the SMs * (stages of a CTA * time of a stage + half a microsecond) + the sum over the CTAs of a split,
+// in nanoseconds, with the times of a stage that were measured (11008 <-> 4096 and 2048 x 2048, 17 to 1024 rows):
+//     one CTA 0.31 + TN / 1000 us, a pair with its weights in tensor memory 0.31 + 0.8 TN / 1000, in shared memory 0.36 + 1.2 TN / 1000,
+//     the split's sums 0.5 us + 3 ns a row and CTA.
+// Either side of its choices there (us): 2048 x 2048, 128 rows: units of 32 rows 10.3, of 128 12.4, those split four ways 11.4, eight ways 28;
+// 4096 -> 11008: 300 rows as 3 units of pairs 33.5, as 2 43.6, 512 rows 46.4 and 49.4, 1024 rows 74.3 and 70.4; 11008 -> 4096, 17 rows: split
+// four ways 15.6, not split 34.7.  Clusters of more than four CTAs (of a whole SM each) are left to few tiles: sixteen of eight CTAs do not
+// stand on the chip at once.
+static void choose_tile(const Call& c, TcArgs* p, int* cg) {
+  const int64_t experts = c.offsets ? (c.N < c.E ? c.N : c.E) : 1;
+  const int64_t mean = ceil_div<int64_t>(c.N, experts);   // rows of an expert
+  int64_t best = -1;
+  for (int cap = 32; cap <= 256; cap *= 2) {
+    // rows fill units evenly where there is one expert; otherwise an expert's last unit is half full, on average
+    const int64_t units2 = c.offsets ? (2 * mean > cap ? 2 * mean + cap : 2 * cap) * experts / cap : 2 * ceil_div<int64_t>(c.N, cap);
+    const int rows = c.offsets ? static_cast<int>(mean < cap ? round_up<int64_t>(mean, 32) : cap)
+                               : static_cast<int>(round_up<int64_t>(ceil_div<int64_t>(2 * c.N, units2), 32));
+    for (int pair = 1; pair <= 2; ++pair) {
+      if ((pair == 2 && c.O <= 128) || (pair == 1 && cap > 128)) continue;
+      const int64_t tiles = ceil_div<int64_t>(units2, 2) * ceil_div(c.O, 128 * pair);
+      const int64_t stage = pair == 1 ? 310 + rows : (cap <= 128 ? 310 + rows * 4 / 5 : 360 + rows * 6 / 5);
+      for (int split = 1; split <= 8; ++split) {
+        if (split > 1 && (pair == 2 || tiles * split > kPlanSMs || p->stages < 4 * split || (split > 4 && tiles > 8))) break;
+        const int64_t rounds = ceil_div<int64_t>(tiles, kPlanSMs / (pair * split));
+        const int64_t cost = rounds * (ceil_div(p->stages, split) * stage + 500) + (split > 1 ? 500 + 3 * split * rows : 0);
+        if (best < 0 || cost < best) {
+          best = cost;
+          p->TN = c.offsets ? cap : rows;
+          p->split = split;
+          *cg = pair;
+        }
+      }
+    }
+  }
+  // (the bound on an expert call's units may be more than the clusters of one round can take: those tiles are one each)
+  if (p->split > 1 && most_units(c, p->TN) * ceil_div(c.O, 128) * p->split >= (int64_t{1} << 31)) p->split = 1;
+}
+
 pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   if (c.T == 0) return PIPE_ERR_UNSUPPORTED;   // (no tensor to copy from; the other kernel reads none)
   TcArgs p;
   p.c = c;
-  const int64_t rows = c.offsets ? ceil_div<int64_t>(c.N, c.E) : c.N;
-  p.TN = rows <= 32 ? 32 : (rows <= 64 ? 64 : (rows <= 128 || c.O <= 128 ? 128 : 256));
-  const int64_t units = most_units(c, p.TN);
-  const int cg = c.O > 128 && units * ceil_div(c.O, 128) > kPlanSMs ? 2 : 1;
-  if (cg == 1 && p.TN == 256) p.TN = 128;
-  if (!c.offsets) p.TN = static_cast<int>(round_up<int64_t>(ceil_div<int64_t>(c.N, ceil_div<int64_t>(c.N, p.TN)), 32));   // units of one size
   p.stages = ceil_div(c.I, kTStage);
+  int cg = 1;
+  choose_tile(c, &p, &cg);
   p.mtiles = ceil_div(c.O, 128 * cg);
   const int64_t tiles = most_units(c, p.TN) * p.mtiles;
-  p.split = 1;
-  if (cg == 1)
-    while (p.split < 8 && tiles * p.split * 2 <= kPlanSMs && p.stages >= 4 * p.split) p.split *= 2;
   int64_t teams = p.split > 1 ? tiles : kPlanSMs / cg;
   if (teams > tiles) teams = tiles;
   p.wide_y = !(reinterpret_cast<uintptr_t>(c.y) & 15) && c.ldy % 8 == 0;
