@@ -693,11 +693,13 @@ static bool encode_2d(CUtensorMap* map, CUtensorMapDataType type, const void* ba
 //     rounds of tiles on the SMs * (stages of a CTA * time of a stage + half a microsecond) + the sum over the CTAs of a split,
 // in nanoseconds, with the times of a stage that were measured (11008 <-> 4096 and 2048 x 2048, 17 to 1024 rows):
 //     one CTA 0.31 + TN / 1000 us, a pair with its weights in tensor memory 0.31 + 0.8 TN / 1000, in shared memory 0.36 + 1.2 TN / 1000,
+//     and 0.6 at least (its two groups of wideners),
 //     the split's sums 0.5 us + 3 ns a row and CTA.
 // Either side of its choices there (us): 2048 x 2048, 128 rows: units of 32 rows 10.3, of 128 12.4, those split four ways 11.4, eight ways 28;
 // 4096 -> 11008: 300 rows as 3 units of pairs 33.5, as 2 43.6, 512 rows 46.4 and 49.4, 1024 rows 74.3 and 70.4; 11008 -> 4096, 17 rows: split
-// four ways 15.6, not split 34.7.  Clusters of more than four CTAs (of a whole SM each) are left to few tiles: sixteen of eight CTAs do not
-// stand on the chip at once.
+// four ways 15.6, not split 34.7.  kClusters: the clusters of 1, 2, .. CTAs, a whole SM each, that stand on the chip at once (as the runtime
+// counts them, less one or two where they leave SMs of a processing cluster free: those differ from chip to chip).
+constexpr int kClusters[9] = {0, 148, 74, 44, 32, 24, 20, 14, 14};
 static void choose_tile(const Call& c, TcArgs* p, int* cg) {
   const int64_t experts = c.offsets ? (c.N < c.E ? c.N : c.E) : 1;
   const int64_t mean = ceil_div<int64_t>(c.N, experts);   // rows of an expert
@@ -710,10 +712,10 @@ static void choose_tile(const Call& c, TcArgs* p, int* cg) {
     for (int pair = 1; pair <= 2; ++pair) {
       if ((pair == 2 && c.O <= 128) || (pair == 1 && cap > 128)) continue;
       const int64_t tiles = ceil_div<int64_t>(units2, 2) * ceil_div(c.O, 128 * pair);
-      const int64_t stage = pair == 1 ? 310 + rows : (cap <= 128 ? 310 + rows * 4 / 5 : 360 + rows * 6 / 5);
+      const int64_t stage = pair == 1 ? 310 + rows : (cap <= 128 ? 310 + rows * 4 / 5 : (rows < 200 ? 600 : 360 + rows * 6 / 5));
       for (int split = 1; split <= 8; ++split) {
-        if (split > 1 && (pair == 2 || tiles * split > kPlanSMs || p->stages < 4 * split || (split > 4 && tiles > 8))) break;
-        const int64_t rounds = ceil_div<int64_t>(tiles, kPlanSMs / (pair * split));
+        if (split > 1 && (pair == 2 || tiles > kClusters[split] || p->stages < 4 * split)) break;
+        const int64_t rounds = ceil_div<int64_t>(tiles, pair == 2 ? kClusters[2] : kClusters[split]);
         const int64_t cost = rounds * (ceil_div(p->stages, split) * stage + 500) + (split > 1 ? 500 + 3 * split * rows : 0);
         if (best < 0 || cost < best) {
           best = cost;
