@@ -519,8 +519,8 @@ pipe_status pipe_lower_conv_input(const pipe_conv_geom* geom, const int8_t* d_xq
 #define PIPE_MAX_EXPERTS 1024
 typedef struct pipe_group_desc {
   int32_t experts;       /* E, 1..PIPE_MAX_EXPERTS (1: a plain layer) */
-  int32_t out_features;  /* O: rows of W */
-  int32_t in_features;   /* I: reduction length, a multiple of g */
+  int32_t out_features;  /* O: rows of W, at most 2^29 */
+  int32_t in_features;   /* I: reduction length, a multiple of g, at most 2^29 */
   int32_t group_size;    /* g: 32, 64 or 128 */
   int32_t dtype;         /* activations, scales, bias and outputs: PIPE_DTYPE_BF16 or PIPE_DTYPE_FP16 */
   int32_t asymmetric;    /* 0, or 1: the layer has zero points */
@@ -557,7 +557,7 @@ pipe_status pipe_group_quantize(const pipe_group_desc* desc, const void* d_W, in
  * and the scale is applied to a group's binary32 sum; beyond that, on the tensor cores' operands, s * (code - z) is first
  * rounded to the layer's type (half a step of it at most, like the activations themselves).
  * d_x: [T, I] pitch ldx, 16-byte aligned, ldx a multiple of 8.  d_bias: [O] or NULL.  d_y: [T, O] pitch ldy.
- * T = 0 is a no-op.  d_y must not overlap the inputs.
+ * T = 0 is a no-op, T is at most 2^30.  d_y must not overlap the inputs.  Equal calls give equal bits.
  */
 pipe_status pipe_group_linear(const pipe_group_desc* desc, const void* d_codes, const void* d_scales, const uint8_t* d_zeros,
                               const void* d_x, int64_t T, int64_t ldx, const void* d_bias, int32_t activation, void* d_y,
@@ -581,7 +581,8 @@ pipe_status pipe_expert_rows(const int32_t* d_choice, int64_t T, int32_t k, int3
  *     y[s, o] = h(sigma(sum_i x[r, i] W_e[o, i] + bias[e, o])),   r = d_rows[s], or s itself where d_rows is NULL.
  * Ragged sizes, empty experts among them, are read on the device; nothing is copied to the host.  d_x: [T, I] pitch ldx (16-byte
  * aligned, ldx a multiple of 8); d_rows: int32 [N] or NULL; d_offsets: int32 [E+1] ascending; d_bias: [E, O] or NULL; d_y: [N, O]
- * pitch ldy, of which the rows behind d_offsets[E] are left as they were.  N: the rows that d_y and d_rows have room for.  Offsets
+ * pitch ldy, of which the rows behind d_offsets[E] are left as they were.  N: the rows that d_y and d_rows have room for
+ * (T and N at most 2^30).  d_y must not overlap the inputs.  Offsets
  * are taken as clamped to [0, N], and a row index outside [0, T) reads as a row of zeros.  Arithmetic as in pipe_group_linear,
  * with N / E (rounded up) in the place of the tokens.
  */

@@ -4,9 +4,13 @@
 namespace pipe {
 namespace grp {
 
+constexpr int kMostFeatures = 1 << 29;       // channels, doubled, are coordinates of 32 bits
+constexpr int64_t kMostRows = int64_t{1} << 30;
+
 static pipe_status check_desc(const pipe_group_desc* d) {
   if (!d) return PIPE_ERR_INVALID_ARG;
   if (d->experts < 1 || d->experts > PIPE_MAX_EXPERTS || d->out_features < 1 || d->in_features < 1) return PIPE_ERR_INVALID_ARG;
+  if (d->out_features > kMostFeatures || d->in_features > kMostFeatures) return PIPE_ERR_INVALID_ARG;
   if (d->dtype != PIPE_DTYPE_BF16 && d->dtype != PIPE_DTYPE_FP16) return PIPE_ERR_INVALID_ARG;
   if (d->asymmetric != 0 && d->asymmetric != 1) return PIPE_ERR_INVALID_ARG;
   if (d->group_size < 1) return PIPE_ERR_INVALID_ARG;
@@ -22,7 +26,7 @@ static pipe_status check_product(const pipe_group_desc* desc, const void* codes,
                                  int64_t T, int64_t ldx, const void* bias, int32_t act, int64_t N, void* y, int64_t ldy, Call* c) {
   const pipe_status st = check_desc(desc);
   if (st != PIPE_OK) return st;
-  if (T < 0 || N < 0 || T >= (int64_t{1} << 31) || N >= (int64_t{1} << 31)) return PIPE_ERR_INVALID_ARG;
+  if (T < 0 || N < 0 || T > kMostRows || N > kMostRows) return PIPE_ERR_INVALID_ARG;
   if (act < PIPE_ACT_IDENTITY || act > PIPE_ACT_SIGMOID) return PIPE_ERR_INVALID_ARG;
   if (!codes || !scales || (zeros != nullptr) != (desc->asymmetric != 0)) return PIPE_ERR_INVALID_ARG;
   if ((T > 0 && !x) || (N > 0 && !y)) return PIPE_ERR_INVALID_ARG;

@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(kSThreads, MT == 1 ? 5 : (MT * NT == 2 ? 4 : 3
     const int n = (step1 - step0) * 4 * 2 * MT;
     for (int i = lane; i < n; i += 32) {
       const int kb = 4 * step0 + i / (2 * MT), o = o0 + 8 * (i % (2 * MT));
-      if (kb < c.KB && o < c.O) asm volatile("prefetch.global.L2 [%0];" ::"l"(c.codes + kb * run_bytes + o * 16));
+      if (kb < c.KB && o < c.O) asm volatile("prefetch.global.L2 [%0];" ::"l"(c.codes + kb * run_bytes + o * int64_t{16}));
     }
   }
   grid_wait();
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kSThreads, MT == 1 ? 5 : (MT * NT == 2 ? 4 : 3
     for (int m = 0; m < 2 * MT; ++m) real[m] = o0 + 8 * m + gid < c.O;
     const uint8_t* code[4];   // the four runs of the next step to be asked for
 #pragma unroll
-    for (int b = 0; b < 4; ++b) code[b] = c.codes + (static_cast<int64_t>(u.e) * c.KB + 4 * step0 + b) * run_bytes + (o0 + gid) * 16 + 4 * tig;
+    for (int b = 0; b < 4; ++b) code[b] = c.codes + (static_cast<int64_t>(u.e) * c.KB + 4 * step0 + b) * run_bytes + (o0 + gid) * int64_t{16} + 4 * tig;
     const int64_t meta0 = (static_cast<int64_t>(u.e) * groups + step0 * kGroups) * c.O + o0 + gid;
     const uint16_t* scales = static_cast<const uint16_t*>(c.scales) + meta0;
     const uint8_t* zeros = ASYM ? c.zeros + meta0 : nullptr;
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kSThreads, MT == 1 ? 5 : (MT * NT == 2 ? 4 : 3
       if (!ok) r = 0;
       x[n] = static_cast<const uint16_t*>(c.x) + r * c.ldx + 128 * step0 + 8 * tig;
     }
-    uint32_t w[kAhead][4][2 * MT];
+    uint32_t w[kAhead][4][2 * MT] = {};
     auto load = [&](int step, uint32_t (&d)[4][2 * MT]) {
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kSThreads, MT == 1 ? 5 : (MT * NT == 2 ? 4 : 3
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.f;
 
-    uint32_t sc[kMeta][kGroups][2 * MT], zp[kMeta][kGroups][2 * MT];
+    uint32_t sc[kMeta][kGroups][2 * MT] = {}, zp[kMeta][kGroups][2 * MT] = {};
     auto fetch = [&](int step, uint32_t (&s)[kGroups][2 * MT], uint32_t (&z)[kGroups][2 * MT]) {
 #pragma unroll
       for (int f = 0; f < kGroups; ++f) {

@@ -83,15 +83,10 @@ __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
         : "memory");
-  else if constexpr (TA)
+  else   // (one CTA alone always has them in tensor memory)
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(static_cast<uint32_t>(a)), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
-        : "memory");
-  else
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
         : "memory");
 }
 template <int CG>
@@ -731,7 +726,8 @@ static void choose_tile(const Call& c, TcArgs* p, int* cg) {
 }
 
 pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
-  if (c.T == 0) return PIPE_ERR_UNSUPPORTED;   // (no tensor to copy from; the other kernel reads none)
+  // (no tensor to copy from; more runs of codes than a copy's coordinate counts: the other kernel)
+  if (c.T == 0 || static_cast<int64_t>(c.E) * c.KB >= (int64_t{1} << 31)) return PIPE_ERR_UNSUPPORTED;
   TcArgs p;
   p.c = c;
   p.stages = ceil_div(c.I, kTStage);

@@ -119,6 +119,38 @@ def test_experts_with_more_tiles_than_sms(E, O, mean, gather):
     _expert(E, O, 256, 128, "fp16", O % 2 == 1, counts, 333, gather, False, B.ACT_IDENTITY, O + 1)
 
 
+@pytest.mark.parametrize("E,O,I,g", [(40, 1500, 256, 64), (64, 1411, 2048, 128), (24, 5000, 96, 32)])
+def test_few_rows_on_many_tiles(E, O, I, g):
+    """The kernel for few rows at each height of its tiles, one to seventeen rows an expert, some of them none."""
+    gen = _gen(E * O)
+    counts = [0 if e % 5 == 2 else int(v) for e, v in enumerate(torch.randint(1, 6, (E,), generator=gen))]
+    _expert(E, O, I, g, "bf16", False, counts, 20, True, True, B.ACT_SILU, O)
+    counts[1] = 17
+    _expert(E, O, I, g, "fp16", True, counts, 20, False, False, B.ACT_GELU, O + 1)
+    _expert(E, O, I, g, "bf16", True, [9 + e % 7 for e in range(E)], 20, True, False, B.ACT_IDENTITY, O + 2)
+
+
+@pytest.mark.parametrize("counts", [[1], [16], [17], [200]])
+def test_one_expert_is_a_plain_layer(counts):
+    _expert(1, 130, 160, 32, "bf16", True, counts, 40, False, True, B.ACT_RELU, counts[0])
+    _expert(1, 130, 2176, 128, "fp16", False, counts, 40, True, True, B.ACT_IDENTITY, counts[0] + 1)
+
+
+@pytest.mark.parametrize("N", [3, 500])
+def test_rows_without_any_tokens_are_sigma_of_the_bias(N):
+    """T = 0: every row index lies outside, every row reads as zeros."""
+    gen = _gen(N)
+    E, O, I, g = 2, 37, 64, 32
+    u, s, _ = R.random_layer(gen, E, O, I, g, "bf16", False)
+    b = torch.randn((E, O), generator=gen).to(torch.bfloat16)
+    for rows in (None, torch.zeros(N, dtype=torch.int32, device="cuda")):
+        y = torch.full((N, O), 7.0, dtype=torch.bfloat16, device="cuda")
+        B.pipe_expert_linear(B.make_group_desc(O, I, g, experts=E), R.pack(u).cuda(), s.cuda(), None, torch.empty((0, I), dtype=torch.bfloat16, device="cuda"),
+                             torch.tensor([0, 1, N - 1], dtype=torch.int32).cuda(), y, rows=rows, bias=b.cuda(), activation=B.ACT_RELU)
+        _ok()
+        assert torch.equal(y[:1].cpu(), b[:1].clamp(min=0)) and torch.equal(y[1:N - 1].cpu(), b[1:].clamp(min=0).expand(N - 2, O)) and (y[N - 1] == 7).all()
+
+
 def test_more_experts_than_a_warp_looks_at():
     gen = _gen(3)
     counts = torch.randint(0, 3, (1024,), generator=gen).tolist()

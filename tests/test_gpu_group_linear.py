@@ -229,6 +229,29 @@ def test_linear_is_the_same_every_time_and_in_a_graph(T):
     assert torch.equal(ys[0], ys[2])
 
 
+def test_calls_on_two_streams_at_once():
+    """No call shares anything with another: two layers on two streams, and on the default one, give what they give alone."""
+    gen = _gen(31)
+    layers = []
+    for O, I, g, asym in ((1500, 2048, 128, False), (700, 4096, 32, True)):
+        u, s, z = R.random_layer(gen, 1, O, I, g, "bf16", asym)
+        layers.append((B.make_group_desc(O, I, g, asymmetric=asym), R.pack(u).cuda(), s.cuda(), None if z is None else z.cuda()))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for T in (1, 12, 40, 300):
+        xs = [torch.randn((T, d[0].in_features), generator=gen).to(torch.bfloat16).cuda() for d in layers]
+        alone = [torch.empty((T, d[0].out_features), dtype=torch.bfloat16, device="cuda") for d in layers]
+        for d, x, y in zip(layers, xs, alone):
+            B.pipe_group_linear(*d, x, y)
+        torch.cuda.synchronize()
+        both = [[torch.empty_like(y) for _ in range(8)] for y in alone]
+        for i in range(8):
+            for k, st in enumerate(streams):
+                B.pipe_group_linear(*layers[k], xs[k], both[k][i], stream=st)
+        _ok()
+        for k in range(2):
+            assert all(torch.equal(alone[k], y) for y in both[k])
+
+
 def test_quantize_then_multiply_without_a_synchronization():
     """The weights of every call are made by the call before it on the same stream."""
     gen = _gen(2)

@@ -38,6 +38,7 @@ def test_layout_sizes(lib):
 
 @pytest.mark.parametrize("field,value,status", [
     ("experts", 0, B.PIPE_ERR_INVALID_ARG), ("experts", B.MAX_EXPERTS + 1, B.PIPE_ERR_INVALID_ARG), ("out_features", 0, B.PIPE_ERR_INVALID_ARG),
+    ("out_features", (1 << 29) + 1, B.PIPE_ERR_INVALID_ARG), ("in_features", (1 << 29) + 32, B.PIPE_ERR_INVALID_ARG),
     ("in_features", 0, B.PIPE_ERR_INVALID_ARG), ("in_features", -32, B.PIPE_ERR_INVALID_ARG), ("in_features", 144, B.PIPE_ERR_SHAPE),
     ("group_size", 0, B.PIPE_ERR_INVALID_ARG), ("group_size", 16, B.PIPE_ERR_UNSUPPORTED), ("group_size", 256, B.PIPE_ERR_UNSUPPORTED),
     ("dtype", 2, B.PIPE_ERR_INVALID_ARG), ("dtype", -1, B.PIPE_ERR_INVALID_ARG), ("asymmetric", 2, B.PIPE_ERR_INVALID_ARG)])
@@ -74,7 +75,7 @@ def test_quantize_refuses(lib, change, status):
 BAD_PRODUCTS = [
     (dict(codes=None), B.PIPE_ERR_INVALID_ARG), (dict(scales=None), B.PIPE_ERR_INVALID_ARG), (dict(zeros=4096), B.PIPE_ERR_INVALID_ARG),
     (dict(x=None), B.PIPE_ERR_INVALID_ARG), (dict(y=None), B.PIPE_ERR_INVALID_ARG), (dict(T=-1), B.PIPE_ERR_INVALID_ARG),
-    (dict(T=1 << 31), B.PIPE_ERR_INVALID_ARG), (dict(act=5), B.PIPE_ERR_INVALID_ARG), (dict(act=-1), B.PIPE_ERR_INVALID_ARG),
+    (dict(T=1 << 31), B.PIPE_ERR_INVALID_ARG), (dict(T=(1 << 30) + 1), B.PIPE_ERR_INVALID_ARG), (dict(act=5), B.PIPE_ERR_INVALID_ARG), (dict(act=-1), B.PIPE_ERR_INVALID_ARG),
     (dict(ldx=120), B.PIPE_ERR_INVALID_ARG), (dict(ldy=63), B.PIPE_ERR_INVALID_ARG), (dict(ldx=132), B.PIPE_ERR_ALIGNMENT),
     (dict(x=4104), B.PIPE_ERR_ALIGNMENT), (dict(codes=4104), B.PIPE_ERR_ALIGNMENT), (dict(scales=4097), B.PIPE_ERR_ALIGNMENT),
     (dict(bias=4097), B.PIPE_ERR_ALIGNMENT), (dict(y=4097), B.PIPE_ERR_ALIGNMENT)]
