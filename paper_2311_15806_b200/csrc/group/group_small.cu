@@ -9,6 +9,9 @@
 // share the reduction axis in steps of 128 codes.  A warp's activations are asked into L1, which the CTAs of an SM share, at once;
 // codes, scales and zero points of its next steps are in flight in registers (copies through shared memory cost more instructions
 // than the arithmetic).  Sums are added in a fixed order.
+// Measured, back to back in a graph (weights then in L2): 4096 -> 11008 on one row 8.5 us (23.3 MB), on 8 rows 10.3, on 16 rows 13.3; 64
+// experts 2048 -> 1408, 48 rows on 31 of them, 18.4 (46 MB), 22.5 among other calls, where the weights come from HBM.  Bound by the
+// latency of a CTA's chain (unit, addresses, first codes, sums): issue slots are 20 to 36 % busy.
 #include "group_common.cuh"
 
 namespace pipe {

@@ -9,7 +9,7 @@
 //   TN <= 128 has half of that or less, and its 112 KB of shared-memory traffic a stage would be the bound; there the weights go to
 //     tensor memory, which tcgen05.mma takes A from as well: four slots of 64 columns behind the two accumulators, one to each of four
 //     groups of warps
-// Activations come by tensor copies in the 128-byte swizzle, codes by bulk copies, each on a ring.  Rows that are gathered come by
+// Activations come by tensor copies in the 128-byte swizzle, a stage's codes by one more, each on a ring.  Rows that are gathered come by
 // 16-byte asynchronous copies of two warps (a tensor copy that gathers four rows takes some 75 cycles of an SM, 64 of them a stage).
 // The fence that makes ordinary writes visible to the tensor core waits for everything the thread has in flight, so gathered rows
 // are fenced by the warp that issues the MMAs, the pair's second CTA's by the same warp there, which has nothing to issue.  Scales
@@ -19,6 +19,9 @@
 //   warps 4-7   drain accumulators (bias, sigma, rounding, a turn in shared memory to rows of y)
 //   warps 8-    groups that widen weights, stages in turn
 // Few tiles: the CTAs of a cluster share a tile's reduction axis and add their sums through distributed shared memory, in order.
+// Measured (bf16, groups of 128): 4096 -> 11008 on 4096 rows 249 us alone in a graph, 1.48 PFLOP/s, tensor pipe 85 % active; with SiLU,
+// among other passes, at the power cap 292; 8 experts of it, 8192 gathered rows, 566 alone, 640 to 670 among others (tensor pipe 72 %).
+// 1024 rows 72, 128 rows 20, 17 rows 18: there a stage takes its fixed time, whatever its width, and 86 tiles leave 62 SMs idle.
 #include "group_common.cuh"
 #include "pipe_tc_common.cuh"
 
