@@ -570,8 +570,8 @@ pipe_status pipe_group_linear(const pipe_group_desc* desc, const void* d_codes, 
  *   d_offsets int32 [E + 1]: the slots of expert e are d_offsets[e] .. d_offsets[e+1] - 1
  *   d_rows    int32 [T*k]:   the token of every slot (entries from d_offsets[E] on are left as they were)
  *   d_slots   int32 [T, k]:  the slot of every place, -1 for a choice outside [0, E), which gets none
- * No atomics decide an order: equal inputs give equal outputs.  T*k < 2^31, 1 <= E <= PIPE_MAX_EXPERTS.  No workspace (beyond 8192 places
- * d_slots holds counts meanwhile).
+ * No atomics decide an order: equal inputs give equal outputs.  T*k is at most 2^30, 1 <= E <= PIPE_MAX_EXPERTS.  No workspace
+ * (beyond 8192 places d_slots holds counts meanwhile).
  */
 pipe_status pipe_expert_rows(const int32_t* d_choice, int64_t T, int32_t k, int32_t experts, int32_t* d_offsets, int32_t* d_rows,
                              int32_t* d_slots, void* stream);

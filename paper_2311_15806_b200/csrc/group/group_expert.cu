@@ -258,7 +258,7 @@ using namespace pipe;
 extern "C" pipe_status pipe_expert_rows(const int32_t* d_choice, int64_t T, int32_t k, int32_t experts, int32_t* d_offsets, int32_t* d_rows,
                                         int32_t* d_slots, void* stream) {
   if (T < 0 || k < 1 || experts < 1 || experts > PIPE_MAX_EXPERTS) return PIPE_ERR_INVALID_ARG;
-  if (T > (int64_t{0x7fffffff} - 1) / k) return PIPE_ERR_UNSUPPORTED;
+  if (T > (int64_t{1} << 30) / k) return PIPE_ERR_UNSUPPORTED;   // (a place's number plus a step of a walk stays below 2^31)
   if (!d_offsets || (T > 0 && (!d_choice || !d_rows || !d_slots))) return PIPE_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(d_choice) | reinterpret_cast<uintptr_t>(d_offsets) | reinterpret_cast<uintptr_t>(d_rows) |
        reinterpret_cast<uintptr_t>(d_slots)) & 3)

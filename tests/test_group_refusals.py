@@ -116,6 +116,11 @@ def test_expert_rows_refuses(lib, change, status):
     assert lib.pipe_expert_rows(a["choice"], a["T"], a["k"], a["E"], a["offsets"], a["rows"], a["slots"], None) == status
 
 
+@pytest.mark.parametrize("T,k", [((1 << 31) - 2, 1), ((1 << 30) + 1, 1), ((1 << 30) - 1, 2), (1, (1 << 30) + 1)])
+def test_expert_rows_refuses_places_that_its_steps_would_carry_past_31_bits(lib, T, k):
+    assert lib.pipe_expert_rows(4096, T, k, 8, 4096, 4096, 4096, None) == B.PIPE_ERR_UNSUPPORTED
+
+
 @pytest.mark.parametrize("change,status", [
     (dict(T=-1), B.PIPE_ERR_INVALID_ARG), (dict(N=-1), B.PIPE_ERR_INVALID_ARG), (dict(k=0), B.PIPE_ERR_INVALID_ARG), (dict(O=0), B.PIPE_ERR_INVALID_ARG),
     (dict(dtype=2), B.PIPE_ERR_INVALID_ARG), (dict(ldy=63), B.PIPE_ERR_INVALID_ARG), (dict(ldo=63), B.PIPE_ERR_INVALID_ARG),
