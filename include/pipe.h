@@ -546,7 +546,8 @@ pipe_status pipe_group_layout(const pipe_group_desc* desc, pipe_group_layout_t* 
  * d_values (NULL, or float [E*O, I] pitch ldv): receives s * (code - z), which binary32 holds exactly: the weights that the layer
  * stands for, from which a caller forms the residual that the next order of an expansion quantizes.
  * A NaN or Inf among the weights, or a scale beyond the range of fp16, sets PIPE_ERR_NONFINITE in the device status word.
- * d_W and d_values need the alignment of their type (16-byte aligned rows are faster); d_codes 16 bytes.
+ * d_W and d_values need the alignment of their type (16-byte aligned rows are faster); d_codes 16 bytes.  What is written must
+ * not overlap d_W.
  */
 pipe_status pipe_group_quantize(const pipe_group_desc* desc, const void* d_W, int32_t w_dtype, int64_t ldw, void* d_codes,
                                 void* d_scales, uint8_t* d_zeros, float* d_values, int64_t ldv, void* stream);
@@ -555,7 +556,7 @@ pipe_status pipe_group_quantize(const pipe_group_desc* desc, const void* d_W, in
  * y[t, o] = h(sigma(sum_i x[t, i] W[o, i] + bias[o])) for a layer of one expert: products with a vector for one token, with a
  * matrix for more.  sums and sigma (PIPE_ACT_*) in binary32.  Up to 16 tokens codes and activations are multiplied as they are
  * and the scale is applied to a group's binary32 sum; beyond that, on the tensor cores' operands, s * (code - z) is first
- * rounded to the layer's type (half a step of it at most, like the activations themselves).
+ * rounded to the layer's type (half a step of it at most, like the activations themselves; beyond fp16's range infinite).
  * d_x: [T, I] pitch ldx, 16-byte aligned, ldx a multiple of 8.  d_bias: [O] or NULL.  d_y: [T, O] pitch ldy.
  * T = 0 is a no-op, T is at most 2^30.  d_y must not overlap the inputs.  Equal calls give equal bits.
  */
@@ -571,7 +572,7 @@ pipe_status pipe_group_linear(const pipe_group_desc* desc, const void* d_codes, 
  *   d_rows    int32 [T*k]:   the token of every slot (entries from d_offsets[E] on are left as they were)
  *   d_slots   int32 [T, k]:  the slot of every place, -1 for a choice outside [0, E), which gets none
  * No atomics decide an order: equal inputs give equal outputs.  T*k is at most 2^30, 1 <= E <= PIPE_MAX_EXPERTS.  No workspace
- * (beyond 8192 places d_slots holds counts meanwhile).
+ * (beyond 8192 places d_slots holds counts meanwhile): the four arrays must not overlap.
  */
 pipe_status pipe_expert_rows(const int32_t* d_choice, int64_t T, int32_t k, int32_t experts, int32_t* d_offsets, int32_t* d_rows,
                              int32_t* d_slots, void* stream);
@@ -592,7 +593,7 @@ pipe_status pipe_expert_linear(const pipe_group_desc* desc, const void* d_codes,
 
 /*
  * The experts' outputs of every token joined: out[t, o] = h(sum_j weights[t, j] * y[slots[t, j], o]), j ascending, in binary32.
- * A slot outside [0, N) contributes nothing; a token without slots gets zeros.  d_y: [N, O] pitch ldy; d_slots: int32 [T, k] dense;
+ * A slot outside [0, N) contributes nothing; a token without slots gets zeros.  d_out must not overlap the inputs.  d_y: [N, O] pitch ldy; d_slots: int32 [T, k] dense;
  * d_weights: float [T, k] dense; d_out: [T, O] pitch ldo; dtype: PIPE_DTYPE_BF16 or PIPE_DTYPE_FP16, of d_y and d_out.
  */
 pipe_status pipe_expert_combine(const void* d_y, int64_t N, int64_t ldy, const int32_t* d_slots, const float* d_weights, int64_t T,

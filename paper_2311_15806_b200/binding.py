@@ -499,13 +499,13 @@ def _weight_rows_of(where: str, t: torch.Tensor, E: int, O: int, I: int) -> int:
     raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: weights of shape {tuple(shape)} and strides {stride}, rows of {I} at one distance are needed")
 
 
-_GROUP_DTYPES = (torch.bfloat16, torch.float16)
+_GROUP_DTYPES = {DTYPE_BF16: torch.bfloat16, DTYPE_FP16: torch.float16}
 
 
 def _group_arrays(where: str, desc: GroupDesc, codes, scales, zeros, *others) -> torch.dtype:
     """Checks the three arrays of a layer against the descriptor; the layer's torch type."""
     n = desc.experts * desc.out_features * desc.in_features
-    h = _GROUP_DTYPES[desc.dtype]
+    h = _GROUP_DTYPES.get(desc.dtype)   # (None: of no tensor here)
     g = desc.group_size
     if codes.dtype != torch.uint8 or scales.dtype != h or codes.numel() * 2 != n or scales.numel() * g != n or not codes.is_contiguous() \
             or not scales.is_contiguous():

@@ -143,6 +143,18 @@ def test_the_binding_refuses_tensors_of_another_device():
         B.pipe_expert_rows(torch.zeros((2, 2), dtype=torch.int32), 4, *(torch.zeros(n, dtype=torch.int32) for n in (5, 4, 4)))
 
 
+@pytest.mark.parametrize("dtype", [2, -1, 7])
+def test_the_binding_refuses_a_descriptor_of_another_type(dtype):
+    d = desc()
+    codes, scales, _ = B.alloc_group(d, device="cpu")
+    d.dtype = dtype
+    x, y = torch.zeros((2, 128), dtype=torch.bfloat16), torch.zeros((2, 64), dtype=torch.bfloat16)
+    with pytest.raises(B.PipeError):
+        B.pipe_group_linear(d, codes, scales, None, x, y)
+    with pytest.raises(B.PipeError):
+        B.pipe_group_quantize(d, torch.zeros((64, 128)), codes, scales)
+
+
 def test_pack_and_unpack_are_inverses():
     u = torch.randint(0, 16, (2, 5, 96))
     assert torch.equal(R.unpack(R.pack(u), 96), u)
