@@ -584,7 +584,8 @@ pipe_status pipe_expert_rows(const int32_t* d_choice, int64_t T, int32_t k, int3
  * aligned, ldx a multiple of 8); d_rows: int32 [N] or NULL; d_offsets: int32 [E+1] ascending; d_bias: [E, O] or NULL; d_y: [N, O]
  * pitch ldy, of which the rows behind d_offsets[E] are left as they were.  N: the rows that d_y and d_rows have room for
  * (T and N at most 2^30).  d_y must not overlap the inputs.  Offsets
- * are taken as clamped to [0, N], and a row index outside [0, T) reads as a row of zeros.  Arithmetic as in pipe_group_linear,
+ * are taken as clamped to [0, N], one that is below an earlier one as equal to it, and a row index outside [0, T) reads as a row of
+ * zeros.  Arithmetic as in pipe_group_linear,
  * with N / E (rounded up) in the place of the tokens.
  */
 pipe_status pipe_expert_linear(const pipe_group_desc* desc, const void* d_codes, const void* d_scales, const uint8_t* d_zeros,

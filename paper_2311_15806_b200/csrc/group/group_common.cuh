@@ -149,6 +149,22 @@ __device__ __forceinline__ void quick_activation(float (&v)[N], int kind) {
   }
 }
 
+// Offsets of 32 experts, lo and hi of this lane's (lo = hi = 0 behind the last, which lane `last` has), made ascending: an offset below
+// one before it counts as that one, so that no row has two experts and the units stay as few as their bound.  top: the last offset of
+// the experts before, and then of these.
+__device__ __forceinline__ void make_ascending(int& lo, int& hi, int& top, bool here, int last) {
+  if (__any_sync(0xffffffffu, here && (hi < lo || lo < top))) {
+    lo = max(lo, top);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, lo, d);
+      if ((threadIdx.x & 31) >= d) lo = max(lo, v);
+    }
+    hi = max(hi, lo);
+  }
+  top = __shfl_sync(0xffffffffu, hi, last);
+}
+
 // The rows cut into units of at most `per` rows of one expert, numbered expert by expert.  The table, unit_ints(E) integers of shared
 // memory: first[e], the units before expert e (first[E]: all of them), begin[e] and end[e], its rows.  Offsets are taken as clamped to
 // [0, N] and ascending, whatever they hold.
@@ -161,7 +177,7 @@ __device__ __forceinline__ void build_units(const Call& c, int per, int32_t* tab
       lo = __ldcg(c.offsets + e);
       hi = __ldcg(c.offsets + e + 1);
       lo = lo < 0 ? 0 : (lo > c.N ? c.N : lo);
-      hi = hi < lo ? lo : (hi > c.N ? c.N : hi);
+      hi = hi < 0 ? 0 : (hi > c.N ? c.N : hi);
     }
     table[c.E + 1 + e] = static_cast<int32_t>(lo);   // N < 2^31
     table[2 * c.E + 1 + e] = static_cast<int32_t>(hi);
@@ -169,10 +185,20 @@ __device__ __forceinline__ void build_units(const Call& c, int per, int32_t* tab
   __syncthreads();
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x;
-    int before = 0;
+    int before = 0, top = 0;
     for (int e0 = 0; e0 < c.E; e0 += 32) {
       const int e = e0 + lane;
-      const int mine = e < c.E ? (table[2 * c.E + 1 + e] - table[c.E + 1 + e] + per - 1) / per : 0;
+      int lo = 0, hi = 0;
+      if (e < c.E) {
+        lo = table[c.E + 1 + e];
+        hi = table[2 * c.E + 1 + e];
+      }
+      make_ascending(lo, hi, top, e < c.E, min(31, c.E - 1 - e0));
+      if (e < c.E) {
+        table[c.E + 1 + e] = lo;
+        table[2 * c.E + 1 + e] = hi;
+      }
+      const int mine = (hi - lo + per - 1) / per;
       int upto = mine;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {

@@ -36,14 +36,15 @@ __device__ __forceinline__ bool find_unit(const Call& c, int u, int per, Unit& o
     return out.lo < c.N;
   }
   const int lane = threadIdx.x & 31, N = static_cast<int>(c.N);
-  int before = 0;
+  int before = 0, top = 0;
   for (int e0 = 0; e0 < c.E; e0 += 32) {
     const int e = e0 + lane;
     int lo = 0, hi = 0;
     if (e < c.E) {
       lo = min(max(__ldcg(c.offsets + e), 0), N);
-      hi = min(max(__ldcg(c.offsets + e + 1), lo), N);
+      hi = min(max(__ldcg(c.offsets + e + 1), 0), N);
     }
+    make_ascending(lo, hi, top, e < c.E, min(31, c.E - 1 - e0));
     const int mine = (hi - lo + per - 1) / per;
     int upto = mine;
 #pragma unroll

@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) {
+  if (warp == 1) {   // (two CTAs of this kernel never meet on an SM: with 129 KB or more each they do not fit)
     if (CG == 2) {
       asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -237,10 +237,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
   if (CG == 2 || p.split > 1) cluster_sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_slot;
-  // (offsets out of order can make more units than the host's bound: the rest is not computed, and a tile number stays below 2^31)
-  const int64_t all = static_cast<int64_t>(table[c.E]) * p.mtiles;
-  const int most = p.split > 1 ? teams : 0x7fffffff;   // (a cluster that shares the axis does one tile)
-  const int tiles = static_cast<int>(all < most ? all : most);
+  const int tiles = table[c.E] * p.mtiles;   // (below 2^31: the host has looked; of a cluster that shares the axis one at most)
 
   if (warp == 0 && !c.rows) {
     // ---- activations
@@ -738,6 +735,7 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   choose_tile(c, &p, &cg);
   p.mtiles = ceil_div(c.O, 128 * cg);
   const int64_t tiles = most_units(c, p.TN) * p.mtiles;
+  if (tiles >= (int64_t{1} << 31)) return PIPE_ERR_UNSUPPORTED;
   int64_t teams = p.split > 1 ? tiles : kPlanSMs / cg;
   if (teams > tiles) teams = tiles;
   p.wide_y = !(reinterpret_cast<uintptr_t>(c.y) & 15) && c.ldy % 8 == 0;

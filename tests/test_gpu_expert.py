@@ -182,6 +182,28 @@ def test_bad_offsets_and_rows_stay_in_bounds(N):
     R.check_product(y[4:], xe[4:], W[1], b[1], 0, "bf16", g, R.few(N // 2))
 
 
+@pytest.mark.parametrize("scale", [1, 10])
+@pytest.mark.parametrize("offsets", [[0, 30, 10, 40, 20], [40, 30, 20, 10, 0], [0, 25] + [3] * 35 + [40, 38, 39], [0, -7, 4, 2, 99, 8, 8]])
+def test_offsets_out_of_order_count_as_the_highest_before_them(offsets, scale):
+    """No row gets two experts' results: the offsets in use are the running maximum of the clamped ones."""
+    gen = _gen(9)
+    E, O, I, g, N = len(offsets) - 1, 72, 96, 32, 40 * scale
+    off = torch.tensor(offsets) * scale
+    used = torch.cummax(off.clamp(0, N), 0).values
+    u, s, _ = R.random_layer(gen, E, O, I, g, "bf16", False)
+    x = torch.randn((N, I), generator=gen).to(torch.bfloat16)
+    y = torch.full((N, O), 7.0, dtype=torch.bfloat16, device="cuda")
+    B.pipe_expert_linear(B.make_group_desc(O, I, g, experts=E), R.pack(u).cuda(), s.cuda(), None, x.cuda(), off.to(torch.int32).cuda(), y)
+    _ok()
+    W = R.dense(u, s, None, g)
+    for e in range(E):
+        a, b = int(used[e]), int(used[e + 1])
+        if a < b:
+            R.check_product(y[a:b], x[a:b], W[e], None, 0, "bf16", g, R.few((N + E - 1) // E))
+    for a, b in ((0, int(used[0])), (int(used[-1]), N)):
+        assert torch.all(y[a:b].cpu() == 7.0)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("T,k,O,ldy,ldo", [(1, 1, 1, 1, 1), (5, 2, 64, 64, 64), (7, 8, 72, 80, 88), (33, 3, 65, 65, 67), (200, 6, 520, 520, 520), (9, 17, 24, 24, 24)])
 def test_combine(T, k, O, ldy, ldo, dtype):
