@@ -149,7 +149,27 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(pred));
   return pred != 0;
 }
+// A bounded wait by a whole warp: false when the CTA is aborting.  Its lanes may see a wait that gives up end differently (the barrier may
+// complete between two polls), and what follows is done by whole warps: they go on together or leave together.  (Where the vote would
+// stand between a barrier and the work that everything waits for, it stands behind that work instead.)
+template <int SLEEP_NS = 0>
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
+  return __all_sync(0xffffffffu, mbar_wait<false, SLEEP_NS>(bar, parity, abort_flag, status)) != 0;
+}
 __device__ __forceinline__ void drain_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+// Whether all four warps of the drain may go on: behind it they meet at barriers without a limit, so that one that has given up must
+// not leave the others waiting.
+__device__ __forceinline__ bool drain_agrees(bool ok) {
+  uint32_t all;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.and.pred q, 1, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(all)
+      : "r"(ok ? 1u : 0u)
+      : "memory");
+  return all != 0;
+}
 
 // Eight neighbouring outputs of a row of y, `room` of them inside the layer.
 __device__ __forceinline__ void store_y8(uint16_t* y, const uint4& w, int wide, int room) {
@@ -249,7 +269,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
       const Tile tl = tile_of(p, table, static_cast<int>(t));
       const int row0 = tl.lo + rank * (tl.n / CG);
       for (int st = st0; st < st1; ++st, ++it, rp.advance(1, ring)) {
-        if (!mbar_wait(done + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
+        if (!warp_wait(done + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
         if (elect_one()) {
           if (rank == 0) mbar_expect_tx(x_full + 8 * rp.slot, CG * x_bytes);
 #pragma unroll
@@ -298,7 +318,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
             copy16((i & 1 ? odd : even) + x_bytes / 2 + i * 512, src[i] + AHEAD * kTStage + 64, 16);
           }
       };
-      auto free_slot = [&]() { return mbar_wait(done + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status); };
+      auto free_slot = [&]() { return warp_wait(done + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status); };
       auto hand_on = [&]() {
         arrive_behind_copies(x_full + 8 * rp.slot);
         rp.advance(1, ring);
@@ -357,7 +377,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
       const int64_t meta0 = (static_cast<int64_t>(tl.e) * groups + piece_group) * c.O + o0;
       const uint8_t* meta = (is_zero ? c.zeros + meta0 : static_cast<const uint8_t*>(c.scales) + 2 * meta0) + (piece_byte < run_bytes ? piece_byte : run_bytes - 1);
       for (int st = st0; st < st1; ++st, ++it, rp.advance(1, p.code_depth)) {
-        if (!mbar_wait(c_empty + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
+        if (!warp_wait(c_empty + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
         if (elect_one()) {
           mbar_expect_tx(c_full + 8 * rp.slot, kTCodeBytes);
           tma_load_2d(base + p.off_codes + rp.slot * kTCodeBytes, &cmap, 2 * o0, tl.e * c.KB + 4 * st, c_full + 8 * rp.slot);
@@ -378,23 +398,22 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
       const uint32_t a_lo = TA ? tmem + kTAcol : static_cast<uint32_t>(adesc), a_hi = TA ? 0u : static_cast<uint32_t>(adesc >> 32);
       const uint32_t x_stage = x_bytes >> 4, x_half = x_bytes >> 5;
       RingPos rp{0, 0}, wp{0, 0};
-      uint32_t n = 0;
+      uint32_t n = 0, issued = 0;
       bool ok = true;
       for (int64_t t = team; ok && t < tiles; t += teams, ++n) {
         const uint32_t buf = n & 1, use = n >> 1;
         const uint32_t idesc = idesc0 | (static_cast<uint32_t>(tile_of(p, table, static_cast<int>(t)).n >> 3) << 17);
-        if (!mbar_wait(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status)) break;
+        ok = warp_wait(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status);
+        if (!ok) break;
         const uint32_t d = tmem + buf * p.TN;
         for (int st = st0; st < st1; ++st, rp.advance(1, ring), wp.advance(1, kTWideners<TA>)) {
-          if (!mbar_wait(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status) ||
-              (CG == 2 && c.rows && !mbar_wait(x_peer + 8 * rp.slot, rp.phase, abort_flag, c.status)) || !mbar_wait(a_full + 8 * rp.slot, rp.phase, abort_flag, c.status)) {
-            ok = false;
-            break;
-          }
+          ok = mbar_wait(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status);
+          if (CG == 2 && c.rows) ok = mbar_wait(x_peer + 8 * rp.slot, rp.phase, abort_flag, c.status) && ok;
+          ok = mbar_wait(a_full + 8 * rp.slot, rp.phase, abort_flag, c.status) && ok;
           if (c.rows) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t xl = x_lo + rp.slot * x_stage, al = a_lo + wp.slot * (TA ? 64u : kTSlotBytes >> 4);
-          if (elect_one()) {
+          if (elect_one() && ok) {   // (what did not come is not handed on)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               const uint32_t ak = TA ? al + 8u * k : al + (k >> 2) * (kTSlotBytes >> 5) + 2u * (k & 3);
@@ -403,11 +422,14 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
             }
             commit<CG>(done + 8 * rp.slot);
           }
-          __syncwarp();
+          ++issued;
+          ok = __all_sync(0xffffffffu, ok) != 0;
+          if (!ok) break;
         }
         if (ok && elect_one()) commit<CG>(d_full + 8 * buf);
         __syncwarp();
       }
+      if (!ok) drain_ring(done, issued, p.ring, 20000000ll);   // no products in flight when tensor memory goes
     } else if (c.rows) {
       // the pair's second CTA: its gathered rows, made visible to the tensor core, are reported to the first
       const uint32_t lead = cluster_address(bars, 0) + (x_peer - bar0);
@@ -415,7 +437,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
       bool ok = true;
       for (int64_t t = team; ok && t < tiles; t += teams)
         for (int st = st0; st < st1; ++st, rp.advance(1, ring)) {
-          if (!mbar_wait(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status)) { ok = false; break; }
+          if (!warp_wait(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status)) { ok = false; break; }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) arrive_lead(lead + 8 * rp.slot);
@@ -482,7 +504,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
         settle();
         fetch();
       }
-      if (!mbar_wait(c_full + 8 * cp.slot, cp.phase, abort_flag, c.status)) break;
+      bool ok = mbar_wait(c_full + 8 * cp.slot, cp.phase, abort_flag, c.status);
       const uint8_t* at = gen + p.off_codes + cp.slot * kTCodeBytes;
       uint4 q[4];
 #pragma unroll
@@ -493,13 +515,12 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
         for (int i = 0; i < 16; ++i) v[i >> 2][i & 3] = H::mul2(H::add2(code_pair<H>(w[i >> 2], i & 3), z2[b / KPG]), s2[b / KPG]);
       };
       auto slot_free = [&]() {   // the products of the slot's last stage are done
-        if (it < W) return true;
-        const bool ok = mbar_wait(done + 8 * past.slot, past.phase, abort_flag, c.status);
+        if (it < W) return;
+        ok = mbar_wait(done + 8 * past.slot, past.phase, abort_flag, c.status) && ok;
         past.advance(W, ring);
-        return ok;
       };
       if constexpr (TA) {
-        if (!slot_free()) break;
+        slot_free();
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t to = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kTAcol + wg * 64;
 #pragma unroll
@@ -509,7 +530,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
           tmem_st16(to + b * 16, v);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(c_empty + 8 * cp.slot);
+        if (lane == 0 && ok) mbar_arrive(c_empty + 8 * cp.slot);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       } else {
@@ -517,8 +538,8 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
 #pragma unroll
         for (int b = 0; b < 4; ++b) widen(b, v[b]);
         __syncwarp();
-        if (lane == 0) mbar_arrive(c_empty + 8 * cp.slot);
-        if (!slot_free()) break;
+        if (lane == 0 && ok) mbar_arrive(c_empty + 8 * cp.slot);
+        slot_free();
         uint8_t* to = gen + p.off_a + wg * kTSlotBytes + row * 128;
 #pragma unroll
         for (int b = 0; b < 4; ++b)
@@ -530,7 +551,8 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // visible to the tensor core
       }
       __syncwarp();
-      if (lane == 0) arrive_lead(lead_a + 8 * rp.slot);
+      if (lane == 0 && ok) arrive_lead(lead_a + 8 * rp.slot);
+      if (!__all_sync(0xffffffffu, ok)) break;
       rp.advance(W, ring);
       cp.advance(W, p.code_depth);
     }
@@ -554,7 +576,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
       }
       const int col = o0 + 8 * piece;
       uint16_t* y = static_cast<uint16_t*>(c.y) + (static_cast<int64_t>(tl.lo) + r0) * c.ldy + col;
-      if (!mbar_wait<false, 64>(d_full + 8 * buf, use & 1, abort_flag, c.status)) break;
+      if (!drain_agrees(warp_wait<64>(d_full + 8 * buf, use & 1, abort_flag, c.status))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const int count = tl.hi - tl.lo;   // rows of y, 32 at a time
       for (int n0 = 0; n0 < count; n0 += 32, ++chunk) {
@@ -600,7 +622,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
     bool ok = work;
     if (work && warp >= 4 && warp < 8) {
       const int row = (warp & 3) * 32 + lane;
-      ok = mbar_wait<false, 64>(d_full, 0, abort_flag, c.status);
+      ok = warp_wait<64>(d_full, 0, abort_flag, c.status);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       if (ok)
         for (int n0 = 0; n0 < p.TN; n0 += 16) {
