@@ -286,7 +286,7 @@ using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, voi
                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-inline EncodeFn encode_fn() {
+inline EncodeFn driver_encode_fn() {
   static std::once_flag once;
   static EncodeFn fn = nullptr;
   std::call_once(once, [] {
@@ -298,6 +298,19 @@ inline EncodeFn encode_fn() {
   });
   return fn;
 }
+// The driver's call wants a current context, which a host thread has only from its first call into the runtime on that makes it one
+// (a launch does, asking for the device does not).  Where there is none, the current device's is made current.
+inline CUresult encode_in_context(CUtensorMap* map, CUtensorMapDataType type, cuuint32_t rank, void* base, const cuuint64_t* dims,
+                                  const cuuint64_t* strides, const cuuint32_t* box, const cuuint32_t* estr, CUtensorMapInterleave inter,
+                                  CUtensorMapSwizzle swz, CUtensorMapL2promotion l2, CUtensorMapFloatOOBfill fill) {
+  const EncodeFn fn = driver_encode_fn();
+  CUresult r = fn(map, type, rank, base, dims, strides, box, estr, inter, swz, l2, fill);
+  int dev = -1;
+  if (r == CUDA_ERROR_INVALID_CONTEXT && cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess)
+    r = fn(map, type, rank, base, dims, strides, box, estr, inter, swz, l2, fill);
+  return r;
+}
+inline EncodeFn encode_fn() { return driver_encode_fn() ? encode_in_context : nullptr; }
 
 inline bool make_map_2d(CUtensorMap* map, const void* base, uint64_t inner_bytes, uint64_t rows, uint64_t pitch_bytes,
                         uint32_t box_inner, uint32_t box_rows, CUtensorMapSwizzle swz) {
