@@ -236,6 +236,15 @@ inline int64_t most_units(const Call& c, int per) {
   return (c.N < c.E ? c.N : static_cast<int64_t>(c.E)) + c.N / per;
 }
 
+// What a failed call of the runtime leaves behind is taken away with it: launch_status() of this thread's next call would report it.
+inline pipe_status runtime_failed() {
+  cudaGetLastError();
+  return PIPE_ERR_CUDA;
+}
+// Lets a kernel be launched with up to `most` bytes of dynamic shared memory on the current device.  That limit is the kernel's, for all
+// host threads: it is set once, to the most that any call asks for, so that no call lowers it under another one's launch.
+bool allow_dynamic_smem(const void* kernel, int most);
+
 pipe_status linear_small(const Call& c, bool bf16, cudaStream_t stream);
 pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream);
 

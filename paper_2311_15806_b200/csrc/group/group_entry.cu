@@ -1,4 +1,6 @@
 // Entry points of the 4-bit layers with group scales: checks of arguments and the choice of a kernel.
+#include <mutex>
+
 #include "group_common.cuh"
 
 namespace pipe {
@@ -17,6 +19,21 @@ static pipe_status check_desc(const pipe_group_desc* d) {
   if (d->group_size != 32 && d->group_size != 64 && d->group_size != 128) return PIPE_ERR_UNSUPPORTED;
   if (d->in_features % d->group_size) return PIPE_ERR_SHAPE;
   return PIPE_OK;
+}
+
+bool allow_dynamic_smem(const void* kernel, int most) {
+  constexpr int kMost = 4096;   // kernels (some twenty) times devices; beyond, the limit is set again by every call, to the same value
+  static std::mutex lock;
+  static struct { const void* kernel; int device; } done[kMost];
+  static int n = 0;
+  int device = -1;
+  if (cudaGetDevice(&device) != cudaSuccess) return false;
+  const std::lock_guard<std::mutex> held(lock);
+  for (int i = 0; i < n; ++i)
+    if (done[i].kernel == kernel && done[i].device == device) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) return false;
+  if (n < kMost) done[n++] = {kernel, device};
+  return true;
 }
 
 static bool misaligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
@@ -51,7 +68,7 @@ static pipe_status check_product(const pipe_group_desc* desc, const void* codes,
 static pipe_status product(Call& c, bool bf16, cudaStream_t stream) {
   if (c.N == 0) return PIPE_OK;
   c.status = device_status_word();
-  if (!c.status) return PIPE_ERR_CUDA;
+  if (!c.status) return runtime_failed();
   // Up to 16 rows (on experts: on average, rounded up) the codes' bytes are what counts; the small kernel holds 16 rows a unit.
   const int64_t rows = c.offsets ? ceil_div<int64_t>(c.N, c.E) : c.N;
   pipe_status st = rows > 16 ? linear_tc(c, bf16, stream) : PIPE_ERR_UNSUPPORTED;

@@ -274,7 +274,7 @@ extern "C" pipe_status pipe_expert_rows(const int32_t* d_choice, int64_t T, int3
   a.blocks = a.n / grp::kRBlock;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   auto launch = [&](void (*kernel)(grp::RowsArgs), int blocks, int threads, int smem) {
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return false;
+    if (smem > 48 * 1024 && !grp::allow_dynamic_smem(reinterpret_cast<const void*>(kernel), 32 * PIPE_MAX_EXPERTS * 4)) return false;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -292,7 +292,7 @@ extern "C" pipe_status pipe_expert_rows(const int32_t* d_choice, int64_t T, int3
   const bool ok = a.n <= grp::kROne ? launch(grp::expert_rows_kernel, 1, 1024, 32 * experts * 4)
                                     : launch(grp::expert_count_kernel, a.blocks, 256, experts * 4) && launch(grp::expert_scan_kernel, 1, 1024, 0) &&
                                           launch(grp::expert_place_kernel, a.blocks, 256, 8 * experts * 4);
-  if (!ok) return PIPE_ERR_CUDA;
+  if (!ok) return grp::runtime_failed();
   take_expansion_mark(s);
   return launch_status();
 }
@@ -326,7 +326,7 @@ extern "C" pipe_status pipe_expert_combine(const void* d_y, int64_t N, int64_t l
   void (*kern)(grp::CombineArgs) = wide ? (bf16 ? grp::expert_combine_kernel<grp::Bf16, 8> : grp::expert_combine_kernel<grp::Fp16, 8>)
                                         : (bf16 ? grp::expert_combine_kernel<grp::Bf16, 1> : grp::expert_combine_kernel<grp::Fp16, 1>);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (launch_overlapped(kern, dim3(static_cast<unsigned>(blocks)), grp::kCThreads, 1, true, s, a) != cudaSuccess) return PIPE_ERR_CUDA;
+  if (launch_overlapped(kern, dim3(static_cast<unsigned>(blocks)), grp::kCThreads, 1, true, s, a) != cudaSuccess) return grp::runtime_failed();
   count_launch(1);
   take_expansion_mark(s);
   return launch_status();

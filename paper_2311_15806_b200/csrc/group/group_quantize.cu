@@ -280,13 +280,13 @@ extern "C" pipe_status pipe_group_quantize(const pipe_group_desc* desc, const vo
   const int64_t across = static_cast<int64_t>(ceil_div(a.I, 128)) * desc->experts, want = ceil_div<int64_t>(2 * 8 * kPlanSMs, across);
   const dim3 grid(ceil_div(a.I, 128), static_cast<unsigned>(row_blocks < want ? row_blocks : want), desc->experts);
   a.status = device_status_word();
-  if (!a.status) return PIPE_ERR_CUDA;
+  if (!a.status) return grp::runtime_failed();
   const bool bf16 = desc->dtype == PIPE_DTYPE_BF16;
   const grp::QuantKernel k =
       bf16 ? (desc->asymmetric ? grp::quantize_kernel<grp::Bf16, true>(w_dtype, a.g) : grp::quantize_kernel<grp::Bf16, false>(w_dtype, a.g))
            : (desc->asymmetric ? grp::quantize_kernel<grp::Fp16, true>(w_dtype, a.g) : grp::quantize_kernel<grp::Fp16, false>(w_dtype, a.g));
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (launch_overlapped(k, grid, grp::kQThreads, 1, true, s, a) != cudaSuccess) return PIPE_ERR_CUDA;
+  if (launch_overlapped(k, grid, grp::kQThreads, 1, true, s, a) != cudaSuccess) return grp::runtime_failed();
   count_launch(1);
   take_expansion_mark(s);
   return launch_status();

@@ -325,7 +325,7 @@ pipe_status linear_small(const Call& c, bool bf16, cudaStream_t stream) {
   if (tiles * ctas >= (int64_t{1} << 31)) return PIPE_ERR_UNSUPPORTED;
   const SmallKernel k = bf16 ? small_kernel<Bf16>(mt, nt, c.g, c.zeros != nullptr, c.KB % 4 != 0) : small_kernel<Fp16>(mt, nt, c.g, c.zeros != nullptr, c.KB % 4 != 0);
   const dim3 grid(static_cast<unsigned>(tiles * ctas), static_cast<unsigned>(p.units < 65535 ? p.units : 65535));
-  if (launch_overlapped(k, grid, kSThreads, ctas, true, stream, p) != cudaSuccess) return PIPE_ERR_CUDA;
+  if (launch_overlapped(k, grid, kSThreads, ctas, true, stream, p) != cudaSuccess) return runtime_failed();
   count_launch(1);
   return launch_status();
 }

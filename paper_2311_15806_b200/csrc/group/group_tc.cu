@@ -780,9 +780,9 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   if (!encode_2d(&xmap, CU_TENSOR_MAP_DATA_TYPE_UINT16, c.x, c.I, c.T, static_cast<uint64_t>(c.ldx) * 2, 64, p.TN / cg, CU_TENSOR_MAP_SWIZZLE_128B) ||
       !encode_2d(&cmap, CU_TENSOR_MAP_DATA_TYPE_FLOAT64, c.codes, static_cast<uint64_t>(c.O) * 2, static_cast<uint64_t>(c.E) * c.KB,
                  static_cast<uint64_t>(c.O) * 16, 256, 4, CU_TENSOR_MAP_SWIZZLE_NONE))
-    return PIPE_ERR_CUDA;
+    return runtime_failed();
   void (*k)(TcArgs, CUtensorMap, CUtensorMap) = bf16 ? tc_kernel<Bf16>(cg, ta, c.g) : tc_kernel<Fp16>(cg, ta, c.g);
-  if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return PIPE_ERR_CUDA;
+  if (!allow_dynamic_smem(reinterpret_cast<const void*>(k), kTMaxSmem)) return runtime_failed();
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -796,7 +796,7 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  if (cudaLaunchKernelEx(&cfg, k, p, xmap, cmap) != cudaSuccess) return PIPE_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, k, p, xmap, cmap) != cudaSuccess) return runtime_failed();
   count_launch(1);
   return launch_status();
 }
