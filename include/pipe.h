@@ -556,7 +556,8 @@ pipe_status pipe_group_quantize(const pipe_group_desc* desc, const void* d_W, in
  * y[t, o] = h(sigma(sum_i x[t, i] W[o, i] + bias[o])) for a layer of one expert: products with a vector for one token, with a
  * matrix for more.  sums and sigma (PIPE_ACT_*) in binary32.  Up to 16 tokens codes and activations are multiplied as they are
  * and the scale is applied to a group's binary32 sum; beyond that, on the tensor cores' operands, s * (code - z) is first
- * rounded to the layer's type (half a step of it at most, like the activations themselves; beyond fp16's range infinite).
+ * rounded to the layer's type (half a step of it at most, like the activations themselves).  Channels with a scale so large that
+ * the type may not hold its weights (fp16: 4368 or more) are computed as for few tokens at any number of them, slowly.
  * d_x: [T, I] pitch ldx, 16-byte aligned, ldx a multiple of 8.  d_bias: [O] or NULL.  d_y: [T, O] pitch ldy.
  * T = 0 is a no-op, T is at most 2^30.  d_y must not overlap the inputs.  Equal calls give equal bits.
  */

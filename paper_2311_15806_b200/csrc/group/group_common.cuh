@@ -59,10 +59,12 @@ __device__ __forceinline__ int cluster_load(const int32_t* own, int rank) {
 }
 
 // The two element types: packed arithmetic on pairs, and the number whose low mantissa bits a 4-bit code can be or-ed into
-// (128 + u in bf16, 1024 + u in fp16: both exact, as is the difference of two of them).
+// (128 + u in bf16, 1024 + u in fp16: both exact, as is the difference of two of them).  kOver: the least magnitude of a scale whose
+// fifteenfold is beyond the type's range when rounded to it; kInf: infinity.  (As they lie in memory.)
 struct Bf16 {
   using T = __nv_bfloat16;
   static constexpr uint32_t kBase = 0x43004300u;
+  static constexpr uint32_t kOver = 0x7D89u, kInf = 0x7F80u;   // (1.0625 * 2^124 times 15 is the largest number of the type)
   static __device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {   // (one fused operation; an addition costs two)
     uint32_t d;
     asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(0x3F803F80u), "r"(b));
@@ -71,6 +73,11 @@ struct Bf16 {
   static __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("mul.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+  }
+  static __device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {   // (magnitudes; the signs mean nothing)
+    uint32_t d;
+    asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
   }
   static __device__ __forceinline__ float to_float(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
@@ -89,6 +96,7 @@ struct Bf16 {
 struct Fp16 {
   using T = __half;
   static constexpr uint32_t kBase = 0x64006400u;
+  static constexpr uint32_t kOver = 0x6C44u, kInf = 0x7C00u;   // (4368 times 15 is 65520, which rounds to infinity)
   static __device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("add.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
@@ -97,6 +105,11 @@ struct Fp16 {
   static __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("mul.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+  }
+  static __device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {   // (magnitudes; the signs mean nothing)
+    uint32_t d;
+    asm("max.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
   }
   static __device__ __forceinline__ float to_float(uint16_t v) { return __half2float(__ushort_as_half(v)); }

@@ -14,6 +14,9 @@
 // The fence that makes ordinary writes visible to the tensor core waits for everything the thread has in flight, so gathered rows
 // are fenced by the warp that issues the MMAs, the pair's second CTA's by the same warp there, which has nothing to issue.  Scales
 // and zero points are read by the threads that use them, a stage of theirs ahead.
+// A scale that the type has may stand for weights that it has not (fp16: from 4368 on).  Such a weight's product is infinite or NaN, though
+// the sum that it belongs to need not be: the wideners report that there is such a scale, and the outputs of its channels are then
+// computed as for few rows, by the threads that store them.
 // Sums are binary32 in tensor memory, in two accumulators, so that the drain of a tile overlaps the next one's products.
 //   warp 0  activations (gathered: and warp 3)   warp 1  MMA issue, tensor memory   warp 2  codes
 //   warps 4-7   drain accumulators (bias, sigma, rounding, a turn in shared memory to rows of y)
@@ -183,6 +186,59 @@ __device__ __forceinline__ void store_y8(uint16_t* y, const uint4& w, int wide, 
   }
 }
 
+// Scales whose weights may be beyond the type's range (an infinite or NaN scale has no finite outputs to save).
+template <class H>
+__device__ __forceinline__ bool over_range(uint32_t scale) {
+  const uint32_t m = scale & 0x7FFFu;
+  return m >= H::kOver && m < H::kInf;
+}
+// The outputs of those among the eight channels from o on that have such a scale, in rows slot, slot + 8, .. below `end`: a group's sum of
+// exact products in binary32, times its scale.  (Seldom run: kept small, and inline, for a call would cost the kernel spills.)
+template <class H>
+__device__ __forceinline__ void store_by_groups(const Call& c, int e, int o, int slot, int end) {
+  const int groups = c.I / c.g, runs = c.g / 32;
+  uint32_t which = 0;
+  for (int k = 0; k < 8 && o + k < c.O; ++k)
+#pragma unroll 4
+    for (int f = 0; f < groups; ++f)
+      if (over_range<H>(__ldcg(static_cast<const uint16_t*>(c.scales) + (static_cast<int64_t>(e) * groups + f) * c.O + o + k))) which |= 1u << k;
+  for (; slot < end; slot += 8) {
+    for (uint32_t left = which; left; left &= left - 1) {
+      const int ch = o + __ffs(left) - 1;
+      const int64_t r = c.rows ? __ldcg(c.rows + slot) : slot;
+      const bool real = r >= 0 && r < c.T;
+      float v[1] = {0.f};
+#pragma unroll 1
+      for (int f = 0; real && f < groups; ++f) {
+        const int64_t meta = (static_cast<int64_t>(e) * groups + f) * c.O + ch;
+        const uint32_t zero = zero_pair<H>(c.zeros ? __ldcg(c.zeros + meta) : 8u);
+        float sum = 0.f;
+#pragma unroll 1
+        for (int b = f * runs; b < (f + 1) * runs; ++b) {
+          const uint4 q = __ldcg(reinterpret_cast<const uint4*>(c.codes + ((static_cast<int64_t>(e) * c.KB + b) * c.O + ch) * 16));
+          const uint4* x = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(c.x) + r * c.ldx + 32 * b);
+          const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+  #pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint4 a = __ldcg(x + i);
+            const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+  #pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t n = H::add2(code_pair<H>(w[i], k), zero);
+              sum = fmaf(H::to_float(static_cast<uint16_t>(u[k])), H::to_float(static_cast<uint16_t>(n)), sum);
+              sum = fmaf(H::to_float(static_cast<uint16_t>(u[k] >> 16)), H::to_float(static_cast<uint16_t>(n >> 16)), sum);
+            }
+          }
+        }
+        v[0] = fmaf(H::to_float(__ldcg(static_cast<const uint16_t*>(c.scales) + meta)), sum, v[0]);
+      }
+      if (c.bias) v[0] += H::to_float(__ldcg(static_cast<const uint16_t*>(c.bias) + static_cast<int64_t>(e) * c.O + ch));
+      quick_activation(v, c.act);
+      static_cast<uint16_t*>(c.y)[static_cast<int64_t>(slot) * c.ldy + ch] = H::from_float(v[0]);
+    }
+  }
+}
+
 // Tile t of the launch: a unit's rows, 128 CG channels from m on.
 struct Tile : Unit {
   int m;
@@ -204,6 +260,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
   __shared__ uint64_t bars[4 * kTMaxRing + 2 * kTMaxCodes + 4];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_s;
+  __shared__ int over_s;   // a scale has been met whose weights may be beyond the type's range
   const Call& c = p.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -213,6 +270,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
   const uint32_t x_full = bar0, a_full = bar0 + 8 * kTMaxRing, done = bar0 + 16 * kTMaxRing, d_full = bar0 + 24 * kTMaxRing, d_empty = d_full + 16,
                  c_full = d_empty + 16, c_empty = c_full + 8 * kTMaxCodes, x_peer = c_empty + 8 * kTMaxCodes;
   volatile int* abort_flag = &abort_s;
+  volatile int* over_flag = &over_s;
   const int crank = cluster_rank();
   const int rank = CG == 2 ? crank : 0;                 // within the pair
   const int part = CG == 1 && p.split > 1 ? crank : 0;  // of the reduction axis
@@ -224,6 +282,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
 
   if (threadIdx.x == 0) {
     abort_s = 0;
+    over_s = 0;
     for (int s = 0; s < kTMaxRing; ++s) {
       mbar_init(x_full + 8 * s, c.rows ? 64 : 1);
       mbar_init(x_peer + 8 * s, 1);
@@ -509,6 +568,10 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
       uint4 q[4];
 #pragma unroll
       for (int b = 0; b < 4; ++b) q[b] = reinterpret_cast<const uint4*>(at)[b * 128 + row];
+      uint32_t largest = s2[0];   // (while the codes are on their way)
+#pragma unroll
+      for (int f = 1; f < 4 / KPG; ++f) largest = H::max_abs2(largest, s2[f]);
+      if ((largest & 0x7FFFu) >= H::kOver) *over_flag = 1;
       auto widen = [&](int b, uint32_t (&v)[4][4]) {   // the 32 codes of run b
         const uint32_t w[4] = {q[b].x, q[b].y, q[b].z, q[b].w};
 #pragma unroll
@@ -611,6 +674,8 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
           if (n0 + r0 + 8 * i < count && col < c.O) store_y8(y + static_cast<int64_t>(8 * i) * c.ldy, w[i], p.wide_y, c.O - col);
         y += 32 * c.ldy;
       }
+      // (set ahead of the arrivals that this tile's products waited for; a later tile's scale may have set it too)
+      if (*over_flag) store_by_groups<H>(c, tl.e, col, tl.lo + r0, tl.hi);
     }
   }
   if (CG == 1 && p.split > 1) {
@@ -674,6 +739,13 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
         store_y8(static_cast<uint16_t*>(c.y) + at * c.ldy + o0 + col,
                  make_uint4(H::pack(v[0], v[1]), H::pack(v[2], v[3]), H::pack(v[4], v[5]), H::pack(v[6], v[7])), p.wide_y, c.O - o0 - col);
       }
+      int over = 0;   // (of any CTA: each has met its own share of the scales)
+      for (int q = 0; q < p.split; ++q) over |= cluster_load(&over_s, q);
+      if (over)
+        for (int i = crank * kTThreads<TA> + threadIdx.x; i < p.TN * 16; i += p.split * kTThreads<TA>) {
+          const int row = tl.lo + (i >> 4);
+          if (row < tl.hi) store_by_groups<H>(c, tl.e, o0 + (i & 15) * 8, row, row + 1);
+        }
     }
     cluster_sync();   // no CTA leaves while another reads its sums
   }
