@@ -140,8 +140,10 @@ __device__ __forceinline__ uint32_t zero_pair(uint32_t z) {
 }
 
 // sigma of N sums, with SiLU and sigmoid on the approximate exponential and reciprocal (2^-22 and 2^-23 of their values, the
-// exponential's argument rounded: |v| 2^-24): far below half a step of a 16-bit output.  The kind is asked once for all of them:
-// asked per value, unrolled, it took a drain 85 cycles a value.
+// exponential's argument rounded: |v| 2^-24): far below half a step of a 16-bit output.  The exponential is that of -|v|, which cannot
+// overflow: sigmoid(v) = t / (1 + t) and SiLU v t / (1 + t) for v < 0, t = exp v, keep every value that the type has (an exponential of -v
+// overflows from v = -88.7 on, where bf16 has numbers down to v = -92 and more).  The kind is asked once for all of them: asked per
+// value, unrolled, it took a drain 85 cycles a value.
 template <int N>
 __device__ __forceinline__ void quick_activation(float (&v)[N], int kind) {
   if (kind == PIPE_ACT_IDENTITY) return;
@@ -155,9 +157,10 @@ __device__ __forceinline__ void quick_activation(float (&v)[N], int kind) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float e, r;
-      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v[i] * -1.44269504f));
+      asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(fabsf(v[i]) * -1.44269504f));
       asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
-      v[i] = kind == PIPE_ACT_SILU ? v[i] * r : r;
+      if (v[i] >= 0.f) e = 1.f;
+      v[i] = (kind == PIPE_ACT_SILU ? v[i] * e : e) * r;   // (a NaN is not >= 0: e is NaN then)
     }
   }
 }

@@ -644,25 +644,24 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
       const int count = tl.hi - tl.lo;   // rows of y, 32 at a time
       for (int n0 = 0; n0 < count; n0 += 32, ++chunk) {
         uint8_t* to = turn + (chunk & 1) * kTTurnBytes;
-        float v[2][16];   // 16 channels each
-        tmem_ld_16x32(from + buf * p.TN + n0, v[0]);
-        tmem_ld_16x32(from + (16u << 16) + buf * p.TN + n0, v[1]);
-        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-        if (n0 + 32 >= count) {   // the accumulator is read
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) arrive_lead(lead_e + 8 * buf);
-        }
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
+        for (int g = 0; g < 2; ++g) {   // 16 channels each
+          float v[16];
+          tmem_ld_16x32(from + (static_cast<uint32_t>(16 * g) << 16) + buf * p.TN + n0, v);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          if (g == 1 && n0 + 32 >= count) {   // the accumulator is read
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) arrive_lead(lead_e + 8 * buf);
+          }
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[g][i] += bias[2 * g + ((i >> 1) & 1)];
-          quick_activation(v[g], c.act);
+          for (int i = 0; i < 16; ++i) v[i] += bias[2 * g + ((i >> 1) & 1)];
+          quick_activation(v, c.act);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {   // 8 channels: four blocks of 8 rows; a row's 16-byte pieces lie permuted by its number
             const int at = (4 * q + 2 * g + h) ^ (lane & 7);
-            turn_store(smem_u32(to) + lane * 256 + at * 16, H::pack(v[g][2 * h], v[g][2 * h + 1]), H::pack(v[g][4 + 2 * h], v[g][5 + 2 * h]),
-                       H::pack(v[g][8 + 2 * h], v[g][9 + 2 * h]), H::pack(v[g][12 + 2 * h], v[g][13 + 2 * h]));
+            turn_store(smem_u32(to) + lane * 256 + at * 16, H::pack(v[2 * h], v[2 * h + 1]), H::pack(v[4 + 2 * h], v[5 + 2 * h]),
+                       H::pack(v[8 + 2 * h], v[9 + 2 * h]), H::pack(v[12 + 2 * h], v[13 + 2 * h]));
           }
         }
         drain_sync();
