@@ -146,15 +146,14 @@ __device__ __forceinline__ void turn_store(uint32_t addr, uint32_t a, uint32_t b
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 // One lane of a converged warp, in the form that the compiler knows as one thread of a uniform warp: asked by its lane number
-// instead, the thread that issues the MMAs takes 1150 cycles for a stage of any width.
+// instead, the thread that issues the MMAs took 1150 cycles for a stage of any width.
 __device__ __forceinline__ bool elect_one() {
   uint32_t pred;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(pred));
   return pred != 0;
 }
 // A bounded wait by a whole warp: false when the CTA is aborting.  Its lanes may see a wait that gives up end differently (the barrier may
-// complete between two polls), and what follows is done by whole warps: they go on together or leave together.  (Where the vote would
-// stand between a barrier and the work that everything waits for, it stands behind that work instead.)
+// complete between two polls), and what follows is done by whole warps: they go on together or leave together.
 template <int SLEEP_NS = 0>
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
   return __all_sync(0xffffffffu, mbar_wait<false, SLEEP_NS>(bar, parity, abort_flag, status)) != 0;
@@ -447,9 +446,9 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
     }
     if (*abort_flag) drain_ring(c_full, it, p.code_depth, 20000000ll);
   } else if (warp == 1) {
-    // ---- MMA.  The whole warp runs the loop, one elected lane issues.  Of a descriptor only the low word changes (its address field,
-    // in 16-byte units, never carries out of it).
-    if (rank == 0) {
+    // ---- MMA.  One elected lane waits and issues (the whole warp waiting and electing every stage, with a vote on its waits: 4096 -> 11008,
+    // 17 to 512 rows, 4 to 8 % slower).  Of a descriptor only the low word changes (its address field, in 16-byte units, never carries out of it).
+    if (rank == 0 && elect_one()) {
       const uint32_t type = H::kBase == Bf16::kBase ? 1u : 0u;
       const uint32_t idesc0 = (1u << 4) | (type << 7) | (type << 10) | (static_cast<uint32_t>(128 * CG >> 4) << 24);
       const uint64_t xdesc = smem_desc_sw128(base), adesc = smem_desc_sw128(base + p.off_a);
@@ -462,34 +461,31 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
       for (int64_t t = team; ok && t < tiles; t += teams, ++n) {
         const uint32_t buf = n & 1, use = n >> 1;
         const uint32_t idesc = idesc0 | (static_cast<uint32_t>(tile_of(p, table, static_cast<int>(t)).n >> 3) << 17);
-        ok = warp_wait(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status);
+        ok = mbar_wait(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status);
         if (!ok) break;
         const uint32_t d = tmem + buf * p.TN;
         for (int st = st0; st < st1; ++st, rp.advance(1, ring), wp.advance(1, kTWideners<TA>)) {
-          ok = mbar_wait(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status);
-          if (CG == 2 && c.rows) ok = mbar_wait(x_peer + 8 * rp.slot, rp.phase, abort_flag, c.status) && ok;
-          ok = mbar_wait(a_full + 8 * rp.slot, rp.phase, abort_flag, c.status) && ok;
+          if (!mbar_wait(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status) ||
+              (CG == 2 && c.rows && !mbar_wait(x_peer + 8 * rp.slot, rp.phase, abort_flag, c.status)) || !mbar_wait(a_full + 8 * rp.slot, rp.phase, abort_flag, c.status)) {
+            ok = false;
+            break;
+          }
           if (c.rows) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t xl = x_lo + rp.slot * x_stage, al = a_lo + wp.slot * (TA ? 64u : kTSlotBytes >> 4);
-          if (elect_one() && ok) {   // (what did not come is not handed on)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const uint32_t ak = TA ? al + 8u * k : al + (k >> 2) * (kTSlotBytes >> 5) + 2u * (k & 3);
-              const uint32_t xk = xl + (k >> 2) * x_half + 2u * (k & 3);
-              mma_f16<CG, TA>(d, (static_cast<uint64_t>(a_hi) << 32) | ak, (static_cast<uint64_t>(x_hi) << 32) | xk, idesc, k > 0 || st > st0);
-            }
-            commit<CG>(done + 8 * rp.slot);
+          for (int k = 0; k < 8; ++k) {
+            const uint32_t ak = TA ? al + 8u * k : al + (k >> 2) * (kTSlotBytes >> 5) + 2u * (k & 3);
+            const uint32_t xk = xl + (k >> 2) * x_half + 2u * (k & 3);
+            mma_f16<CG, TA>(d, (static_cast<uint64_t>(a_hi) << 32) | ak, (static_cast<uint64_t>(x_hi) << 32) | xk, idesc, k > 0 || st > st0);
           }
+          commit<CG>(done + 8 * rp.slot);
           ++issued;
-          ok = __all_sync(0xffffffffu, ok) != 0;
-          if (!ok) break;
         }
-        if (ok && elect_one()) commit<CG>(d_full + 8 * buf);
-        __syncwarp();
+        if (ok) commit<CG>(d_full + 8 * buf);
       }
       if (!ok) drain_ring(done, issued, p.ring, 20000000ll);   // no products in flight when tensor memory goes
-    } else if (c.rows) {
+    } else if (rank != 0 && c.rows) {
       // the pair's second CTA: its gathered rows, made visible to the tensor core, are reported to the first
       const uint32_t lead = cluster_address(bars, 0) + (x_peer - bar0);
       RingPos rp{0, 0};
@@ -551,6 +547,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
     rp.advance(wg, ring);
     cp.advance(wg, p.code_depth);
     past.advance(wg, ring);
+    bool ok = true;   // (a lane that gives up goes on without waiting: the warp stays whole, and what did not come is not handed on)
     for (uint32_t it = wg; it < total; it += W) {
       // (zero where there is no such channel or group: what is widened there is zero, whatever its codes)
 #pragma unroll
@@ -563,7 +560,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
         settle();
         fetch();
       }
-      bool ok = mbar_wait(c_full + 8 * cp.slot, cp.phase, abort_flag, c.status);
+      ok = ok && mbar_wait(c_full + 8 * cp.slot, cp.phase, abort_flag, c.status);
       const uint8_t* at = gen + p.off_codes + cp.slot * kTCodeBytes;
       uint4 q[4];
 #pragma unroll
@@ -579,7 +576,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
       };
       auto slot_free = [&]() {   // the products of the slot's last stage are done
         if (it < W) return;
-        ok = mbar_wait(done + 8 * past.slot, past.phase, abort_flag, c.status) && ok;
+        ok = ok && mbar_wait(done + 8 * past.slot, past.phase, abort_flag, c.status);
         past.advance(W, ring);
       };
       if constexpr (TA) {
@@ -615,7 +612,6 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
       }
       __syncwarp();
       if (lane == 0 && ok) arrive_lead(lead_a + 8 * rp.slot);
-      if (!__all_sync(0xffffffffu, ok)) break;
       rp.advance(W, ring);
       cp.advance(W, p.code_depth);
     }
@@ -655,13 +651,13 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
             if (lane == 0) arrive_lead(lead_e + 8 * buf);
           }
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] += bias[2 * g + ((i >> 1) & 1)];
-          quick_activation(v, c.act);
-#pragma unroll
           for (int h = 0; h < 2; ++h) {   // 8 channels: four blocks of 8 rows; a row's 16-byte pieces lie permuted by its number
+            float u[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = v[4 * (i >> 1) + 2 * h + (i & 1)] + bias[2 * g + h];
+            quick_activation(u, c.act);
             const int at = (4 * q + 2 * g + h) ^ (lane & 7);
-            turn_store(smem_u32(to) + lane * 256 + at * 16, H::pack(v[2 * h], v[2 * h + 1]), H::pack(v[4 + 2 * h], v[5 + 2 * h]),
-                       H::pack(v[8 + 2 * h], v[9 + 2 * h]), H::pack(v[12 + 2 * h], v[13 + 2 * h]));
+            turn_store(smem_u32(to) + lane * 256 + at * 16, H::pack(u[0], u[1]), H::pack(u[2], u[3]), H::pack(u[4], u[5]), H::pack(u[6], u[7]));
           }
         }
         drain_sync();
@@ -701,6 +697,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
     cluster_sync();
     if (work) {
       const int o0 = tl.m * 128;
+      const int over = lane < p.split ? cluster_load(&over_s, lane) : 0;   // (each CTA has met its own share of the scales)
       for (int i = crank * kTThreads<TA> + threadIdx.x; i < p.TN * 16; i += p.split * kTThreads<TA>) {
         const int r = i >> 4, col = (i & 15) * 8;
         const int64_t at = static_cast<int64_t>(tl.lo + r);
@@ -738,9 +735,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
         store_y8(static_cast<uint16_t*>(c.y) + at * c.ldy + o0 + col,
                  make_uint4(H::pack(v[0], v[1]), H::pack(v[2], v[3]), H::pack(v[4], v[5]), H::pack(v[6], v[7])), p.wide_y, c.O - o0 - col);
       }
-      int over = 0;   // (of any CTA: each has met its own share of the scales)
-      for (int q = 0; q < p.split; ++q) over |= cluster_load(&over_s, q);
-      if (over)
+      if (__any_sync(0xffffffffu, over))
         for (int i = crank * kTThreads<TA> + threadIdx.x; i < p.TN * 16; i += p.split * kTThreads<TA>) {
           const int row = tl.lo + (i >> 4);
           if (row < tl.hi) store_by_groups<H>(c, tl.e, o0 + (i & 15) * 8, row, row + 1);

@@ -19,20 +19,22 @@ def _kernel():
 
 
 def test_the_lanes_of_a_warp_leave_a_wait_together():
-    """Every wait of the kernel is followed by operations of whole warps; its verdict is the warp's, at once or, in the two loops that
-    everything waits for, at the end of the stage, up to which nothing is handed on that did not come."""
+    """A wait's verdict is the whole warp's, but for two loops: the products are one elected thread's, which meets the others only at the
+    kernel's end; where weights are widened a lane that gives up goes on with the others, without further waits, and nothing is handed
+    on that did not come."""
     assert re.search(r"bool warp_wait\([^)]*\) \{\s*return __all_sync\(0xffffffffu, mbar_wait<", _text())
     kernel = _kernel()
-    stages = {"products": ("ok = mbar_wait(x_full", "ok = __all_sync(0xffffffffu, ok) != 0;", 3),
-              "weights": ("bool ok = mbar_wait(c_full", "if (!__all_sync(0xffffffffu, ok)) break;", 2)}
-    assert kernel.count("mbar_wait") == sum(n for _, _, n in stages.values())
-    for begin, vote, waits in stages.values():
-        part = kernel[kernel.index(begin):]
-        part = part[:part.index(vote)]
-        assert part.count("mbar_wait") == waits and "break" not in part
-        assert re.findall(r"[^\n]*return[^\n]*", part) in ([], ["        if (it < W) return;"])
-        for line in re.findall(r"[^\n]*(?:arrive|elect_one)[^\n]*\(.*", part):
-            assert "&& ok)" in line, line
+    products = kernel[kernel.index("if (rank == 0 && elect_one()) {"):]
+    products = products[:products.index("} else if (rank != 0 && c.rows) {")]
+    weights = kernel[re.search(r"bool ok = true;\s*for \(uint32_t it = wg;", kernel).start():]
+    weights = weights[:weights.index("} else if (warp >= 4 && p.split == 1) {")]
+    assert kernel.count("mbar_wait") == 6 and products.count("mbar_wait") == 4
+    assert not re.search(r"__sync|_sync\(|elect|warp_wait|lane", products[len("if (rank == 0 && elect_one()) {"):])
+    assert products.rstrip().endswith("if (!ok) drain_ring(done, issued, p.ring, 20000000ll);")
+    assert weights.count("mbar_wait") == weights.count("ok = ok && mbar_wait(") == 2
+    assert "break" not in weights and re.findall(r"[^\n]*return[^\n]*", weights) == ["        if (it < W) return;"]
+    for line in re.findall(r"[^\n]*arrive[^\n]*\(.*", weights):
+        assert "&& ok)" in line, line
 
 
 def test_the_drain_decides_before_its_barriers():
