@@ -6,7 +6,7 @@ from paper_2311_15806_b200 import binding as B
 from tests import group_reference as R
 
 pytestmark = pytest.mark.gpu
-KINDS = [B.ACT_IDENTITY, B.ACT_RELU, B.ACT_SILU, B.ACT_SIGMOID]
+KINDS = [B.ACT_IDENTITY, B.ACT_RELU, B.ACT_SILU, B.ACT_GELU, B.ACT_SIGMOID]
 # (tokens, reduction length): the kernel for few rows, the tensor-core kernel, and its form whose CTAs share an axis (few channels then)
 FORMS = [(1, 32), (20, 32), (20, 2048)]
 
@@ -37,6 +37,8 @@ def test_every_value_of_the_type(kind, dtype, T, I):
     """Distance allowed, as a fraction of sigma(v): half a step of the output, and
       SiLU, sigmoid   |v| 2^-23 + 2^-20: the exponential's argument is a product with a rounded constant (2^-26 + 2^-24 of |v| log2 e,
                       an exponent of two), the exponential 2^-22, the reciprocal 2^-23, the other roundings 2^-24 each
+      GELU            (v^2 + 2) 2^-23 + 2^-20: erfc's argument z = |v| / sqrt 2 is off by less than 2^-23 of itself, which erfc answers
+                      with at most 2 z^2 + 2 of that; erfcf is documented to 4 units in the last place (2^-21), the products 2^-24 each
     and behind that where an exponential is no normal number any more its spacing, |v| 2^-147, and half the type's smallest number."""
     h = R.TYPES[dtype]
     v = _finite(h)
@@ -44,8 +46,10 @@ def test_every_value_of_the_type(kind, dtype, T, I):
         v = v[::61]
     got = _outputs(v, T, I, h, kind).double()
     d = v.double()
-    want = R.sigma(d, kind)
-    part = {B.ACT_SILU: d.abs() * 2.0 ** -23 + 2.0 ** -20, B.ACT_SIGMOID: d.abs() * 2.0 ** -23 + 2.0 ** -20}.get(kind, torch.zeros_like(d))
+    # (erfc, not the normal distribution, which is 0 in 64 bits from -8.3 on: (1 + erf) / 2)
+    want = 0.5 * d * torch.special.erfc(-d / 2 ** 0.5) if kind == B.ACT_GELU else R.sigma(d, kind)
+    part = {B.ACT_SILU: d.abs() * 2.0 ** -23 + 2.0 ** -20, B.ACT_SIGMOID: d.abs() * 2.0 ** -23 + 2.0 ** -20,
+            B.ACT_GELU: (d * d + 2) * 2.0 ** -23 + 2.0 ** -20}.get(kind, torch.zeros_like(d))
     tol = torch.where(want == 0, 0, part * want.abs()) + (0 if kind <= B.ACT_RELU else (d.abs().clamp(max=200) + 1) * 2.0 ** -147)
     tol = tol + torch.finfo(h).eps / 2 * (want.abs() + tol) + torch.finfo(h).smallest_normal * torch.finfo(h).eps / 2
     off = (got - want[None]).abs()
@@ -61,4 +65,5 @@ def test_infinities(T, I):
     v = torch.tensor([inf, -inf], dtype=torch.bfloat16)
     for kind, want in ((B.ACT_IDENTITY, [inf, -inf]), (B.ACT_RELU, [inf, 0]), (B.ACT_SIGMOID, [1, 0])):
         assert _outputs(v, T, I, torch.bfloat16, kind)[0].tolist() == want
-    assert float(_outputs(v, T, I, torch.bfloat16, B.ACT_SILU)[0, 0]) == inf
+    for kind in (B.ACT_SILU, B.ACT_GELU):
+        assert float(_outputs(v, T, I, torch.bfloat16, kind)[0, 0]) == inf
