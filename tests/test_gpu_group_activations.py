@@ -1,4 +1,4 @@
-"""sigma of the 4-bit layers where it is delicate: every finite value of the layer's type, far tails among them, and infinities."""
+"""sigma of the 4-bit layers where it is delicate: every finite value of the layer's type, far tails among them, NaN and infinities."""
 import pytest
 import torch
 
@@ -57,6 +57,29 @@ def test_every_value_of_the_type(kind, dtype, T, I):
     at = int(worst.max(0).values.argmax())
     assert torch.isfinite(got).all() and float(worst.max()) <= 1, f"v {float(d[at])}: {float(got[0, at])}, not {float(want[at])}"
     assert torch.equal(got, got[:1].expand_as(got))
+
+
+@pytest.mark.parametrize("T,I", FORMS)
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_nan_stays_a_nan(kind, T, I):
+    h, O = torch.bfloat16, 130
+    desc = B.make_group_desc(O, I, 32)
+    codes, scales, _ = B.alloc_group(desc)
+    codes.fill_(0x5A)
+    scales.fill_(0.01)
+    x = torch.zeros((T, I), dtype=h)
+    x[T - 1, 3] = float("nan")
+    bias = torch.zeros(O, dtype=h)
+    bias[7] = float("nan")
+    y = torch.empty((T, O), dtype=h, device="cuda")
+    B.pipe_group_linear(desc, codes, scales, None, x.cuda(), y, bias=bias.cuda(), activation=kind)
+    torch.cuda.synchronize()
+    assert B.pipe_poll_status() == B.PIPE_OK
+    nan = torch.isnan(y.cpu())
+    want = torch.zeros_like(nan)
+    want[T - 1] = True
+    want[:, 7] = True
+    assert torch.equal(nan, want)
 
 
 @pytest.mark.parametrize("T,I", FORMS)
