@@ -446,9 +446,11 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
     }
     if (*abort_flag) drain_ring(c_full, it, p.code_depth, 20000000ll);
   } else if (warp == 1) {
-    // ---- MMA.  One elected lane waits and issues (the whole warp waiting and electing every stage, with a vote on its waits: 4096 -> 11008,
-    // 17 to 512 rows, 4 to 8 % slower).  Of a descriptor only the low word changes (its address field, in 16-byte units, never carries out of it).
-    if (rank == 0 && elect_one()) {
+    // ---- MMA.  With weights in tensor memory one elected lane waits and issues; otherwise the whole warp waits, one lane elected every stage
+    // issues, and the waits' verdict is voted on behind it.  (4096 -> 11008, 17 to 512 rows: the first 17.9 to 49.5 us, the second 19.1 to
+    // 54; 8 gathered experts, 4096 tokens: 670 and 658.)  Of a descriptor only the low word changes (its address field, in 16-byte units,
+    // never carries out of it).
+    if (rank == 0 && (!TA || elect_one())) {
       const uint32_t type = H::kBase == Bf16::kBase ? 1u : 0u;
       const uint32_t idesc0 = (1u << 4) | (type << 7) | (type << 10) | (static_cast<uint32_t>(128 * CG >> 4) << 24);
       const uint64_t xdesc = smem_desc_sw128(base), adesc = smem_desc_sw128(base + p.off_a);
@@ -461,28 +463,30 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
       for (int64_t t = team; ok && t < tiles; t += teams, ++n) {
         const uint32_t buf = n & 1, use = n >> 1;
         const uint32_t idesc = idesc0 | (static_cast<uint32_t>(tile_of(p, table, static_cast<int>(t)).n >> 3) << 17);
-        ok = mbar_wait(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status);
+        ok = TA ? mbar_wait(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status) : warp_wait(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status);
         if (!ok) break;
         const uint32_t d = tmem + buf * p.TN;
         for (int st = st0; st < st1; ++st, rp.advance(1, ring), wp.advance(1, kTWideners<TA>)) {
-          if (!mbar_wait(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status) ||
-              (CG == 2 && c.rows && !mbar_wait(x_peer + 8 * rp.slot, rp.phase, abort_flag, c.status)) || !mbar_wait(a_full + 8 * rp.slot, rp.phase, abort_flag, c.status)) {
-            ok = false;
-            break;
-          }
+          ok = mbar_wait(x_full + 8 * rp.slot, rp.phase, abort_flag, c.status) &&
+               (CG == 1 || !c.rows || mbar_wait(x_peer + 8 * rp.slot, rp.phase, abort_flag, c.status)) && mbar_wait(a_full + 8 * rp.slot, rp.phase, abort_flag, c.status);
           if (c.rows) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t xl = x_lo + rp.slot * x_stage, al = a_lo + wp.slot * (TA ? 64u : kTSlotBytes >> 4);
+          if ((TA || elect_one()) && ok) {   // (what did not come is not handed on)
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const uint32_t ak = TA ? al + 8u * k : al + (k >> 2) * (kTSlotBytes >> 5) + 2u * (k & 3);
-            const uint32_t xk = xl + (k >> 2) * x_half + 2u * (k & 3);
-            mma_f16<CG, TA>(d, (static_cast<uint64_t>(a_hi) << 32) | ak, (static_cast<uint64_t>(x_hi) << 32) | xk, idesc, k > 0 || st > st0);
+            for (int k = 0; k < 8; ++k) {
+              const uint32_t ak = TA ? al + 8u * k : al + (k >> 2) * (kTSlotBytes >> 5) + 2u * (k & 3);
+              const uint32_t xk = xl + (k >> 2) * x_half + 2u * (k & 3);
+              mma_f16<CG, TA>(d, (static_cast<uint64_t>(a_hi) << 32) | ak, (static_cast<uint64_t>(x_hi) << 32) | xk, idesc, k > 0 || st > st0);
+            }
+            commit<CG>(done + 8 * rp.slot);
           }
-          commit<CG>(done + 8 * rp.slot);
           ++issued;
+          if (!TA) ok = __all_sync(0xffffffffu, ok) != 0;
+          if (!ok) break;
         }
-        if (ok) commit<CG>(d_full + 8 * buf);
+        if (ok && (TA || elect_one())) commit<CG>(d_full + 8 * buf);
+        if (!TA) __syncwarp();
       }
       if (!ok) drain_ring(done, issued, p.ring, 20000000ll);   // no products in flight when tensor memory goes
     } else if (rank != 0 && c.rows) {

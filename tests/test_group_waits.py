@@ -19,17 +19,23 @@ def _kernel():
 
 
 def test_the_lanes_of_a_warp_leave_a_wait_together():
-    """A wait's verdict is the whole warp's, but for two loops: the products are one elected thread's, which meets the others only at the
-    kernel's end; where weights are widened a lane that gives up goes on with the others, without further waits, and nothing is handed
-    on that did not come."""
+    """A wait's verdict is the whole warp's, but for two loops.  Products: one elected thread's, which meets the others only at the kernel's
+    end (TA), or the warp's, which votes at the end of a stage.  Where weights are widened a lane that gives up goes on with the others,
+    without further waits.  In both nothing is handed on that did not come."""
     assert re.search(r"bool warp_wait\([^)]*\) \{\s*return __all_sync\(0xffffffffu, mbar_wait<", _text())
     kernel = _kernel()
-    products = kernel[kernel.index("if (rank == 0 && elect_one()) {"):]
+    products = kernel[kernel.index("if (rank == 0 && (!TA || elect_one())) {"):]
     products = products[:products.index("} else if (rank != 0 && c.rows) {")]
     weights = kernel[re.search(r"bool ok = true;\s*for \(uint32_t it = wg;", kernel).start():]
     weights = weights[:weights.index("} else if (warp >= 4 && p.split == 1) {")]
     assert kernel.count("mbar_wait") == 6 and products.count("mbar_wait") == 4
-    assert not re.search(r"__sync|_sync\(|elect|warp_wait|lane", products[len("if (rank == 0 && elect_one()) {"):])
+    inner = products[products.index("for (int st = st0;"):products.index("if (ok && (TA || elect_one())) commit<CG>(d_full")]
+    assert inner.count("mbar_wait") == 3 and inner.count("break") == 1 and "return" not in inner
+    assert inner.index("if ((TA || elect_one()) && ok) {") < inner.index("mma_f16<") < inner.index("commit<CG>(done") < \
+        inner.index("if (!TA) ok = __all_sync(0xffffffffu, ok) != 0;") < inner.index("if (!ok) break;")
+    # a single thread meets no collective
+    for line in products.splitlines()[1:]:
+        assert not re.search(r"__\w*sync\w*\(|elect_one|warp_wait", line) or re.search(r"!TA\)|TA \|\||TA \? mbar_wait", line), line
     assert products.rstrip().endswith("if (!ok) drain_ring(done, issued, p.ring, 20000000ll);")
     assert weights.count("mbar_wait") == weights.count("ok = ok && mbar_wait(") == 2
     assert "break" not in weights and re.findall(r"[^\n]*return[^\n]*", weights) == ["        if (it < W) return;"]
