@@ -502,20 +502,40 @@ def _weight_rows_of(where: str, t: torch.Tensor, E: int, O: int, I: int) -> int:
 _GROUP_DTYPES = {DTYPE_BF16: torch.bfloat16, DTYPE_FP16: torch.float16}
 
 
-def _group_arrays(where: str, desc: GroupDesc, codes, scales, zeros, *others) -> torch.dtype:
-    """Checks the three arrays of a layer against the descriptor; the layer's torch type."""
-    n = desc.experts * desc.out_features * desc.in_features
+def _laid_out(t: torch.Tensor, *full: int) -> bool:
+    """A contiguous tensor of shape `full`, or of that shape with neighbouring dimensions joined (or dimensions of one left out or put in):
+    the same values in the same order."""
+    shape = t.shape
+    if shape == full:
+        return t.is_contiguous()
+    if 0 in full:
+        return t.numel() == 0
+    i = 0
+    for s in shape:
+        joined = 1
+        while joined < s and i < len(full):
+            joined *= full[i]
+            i += 1
+        if joined != s:
+            return False
+    return all(s == 1 for s in full[i:]) and t.is_contiguous()
+
+
+def _group_arrays(where: str, desc: GroupDesc, codes, scales, zeros, bias, *others) -> torch.dtype:
+    """Checks the arrays of a layer and its bias [E, O] (or None) against the descriptor; the layer's torch type."""
+    E, O, I, g = desc.experts, desc.out_features, desc.in_features, desc.group_size
     h = _GROUP_DTYPES.get(desc.dtype)   # (None: of no tensor here)
-    g = desc.group_size
-    if codes.dtype != torch.uint8 or scales.dtype != h or codes.numel() * 2 != n or scales.numel() * g != n or not codes.is_contiguous() \
-            or not scales.is_contiguous():
+    groups = I // g if g > 0 else 0
+    if codes.dtype != torch.uint8 or scales.dtype != h or not _laid_out(codes, E, I // 32, O, 16) or not _laid_out(scales, E, groups, O):
         raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: codes / scales are not the descriptor's arrays")
     if zeros is None:
         if desc.asymmetric:
             raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: an asymmetric layer has zeros")
-    elif not desc.asymmetric or zeros.dtype != torch.uint8 or zeros.numel() * g != n or not zeros.is_contiguous():
+    elif not desc.asymmetric or zeros.dtype != torch.uint8 or not _laid_out(zeros, E, groups, O):
         raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: zeros are not the descriptor's array")
-    _on_current(where, codes, scales, zeros, *others)
+    if bias is not None and (bias.dtype != h or not _laid_out(bias, E, O)):
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: the bias is not [E, O] in the layer's type")
+    _on_current(where, codes, scales, zeros, bias, *others)
     return h
 
 
@@ -524,7 +544,7 @@ def pipe_group_quantize(desc: GroupDesc, W: torch.Tensor, codes: torch.Tensor, s
     """W: cuda float32 / bfloat16 / float16 [E, O, I] or [E*O, I]; codes, scales, zeros: the layer's arrays (see alloc_group);
     values: float32 of either shape, or None."""
     where = "pipe_group_quantize"
-    _group_arrays(where, desc, codes, scales, zeros, W, values)
+    _group_arrays(where, desc, codes, scales, zeros, None, W, values)
     E, O, I = desc.experts, desc.out_features, desc.in_features
     w_dtype = _DTYPES.get(W.dtype, -1)
     ldw, ldv, v = _weight_rows_of(where, W, E, O, I), 0, None
@@ -539,29 +559,25 @@ def pipe_group_linear(desc: GroupDesc, codes: torch.Tensor, scales: torch.Tensor
                       y: torch.Tensor, bias: torch.Tensor | None = None, activation: int = ACT_IDENTITY, stream=None) -> None:
     """x: cuda [T, I], y: cuda [T, O], bias: [O] (or [1, O]), all in the layer's type."""
     where = "pipe_group_linear"
-    h = _group_arrays(where, desc, codes, scales, zeros, x, y, bias)
+    h = _group_arrays(where, desc, codes, scales, zeros, bias, x, y)
     T = x.shape[0]
     if x.dtype != h or y.dtype != h or T != y.shape[0]:
         raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: x and y differ in rows or from the layer's type")
-    b = None
-    if bias is not None:
-        _wants(where, bias.dtype == h and bias.numel() == desc.out_features and bias.is_contiguous(), "bias")
-        b = bias.data_ptr()
     _check(lib().pipe_group_linear(C.byref(desc), codes.data_ptr(), scales.data_ptr(), _dp(zeros), x.data_ptr(), T,
-                                   _rows_of(where, x, desc.in_features), b, activation, y.data_ptr(),
+                                   _rows_of(where, x, desc.in_features), _dp(bias), activation, y.data_ptr(),
                                    _rows_of(where, y, desc.out_features), _stream_ptr(stream)), where)
 
 
 def pipe_expert_rows(choice: torch.Tensor, experts: int, offsets: torch.Tensor, rows: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
     """choice: cuda int32 [T, k]; offsets: int32 [experts + 1]; rows: int32 [T*k]; slots: int32 [T, k]."""
     where = "pipe_expert_rows"
-    _on_current(where, choice, offsets, rows, slots)
     i32 = torch.int32
     _wants(where, choice.dim() == 2 and choice.dtype == i32 and offsets.dtype == i32 and rows.dtype == i32 and slots.dtype == i32 and
            choice.is_contiguous() and offsets.is_contiguous() and rows.is_contiguous() and slots.is_contiguous(),
            "int32 tensors with contiguous entries are needed")
     T, k = choice.shape
-    _wants(where, offsets.numel() == experts + 1 and rows.numel() == T * k and slots.numel() == T * k, "sizes do not match the choice")
+    _wants(where, offsets.numel() == experts + 1 and rows.numel() == T * k and _laid_out(slots, T, k), "sizes do not match the choice")
+    _on_current(where, choice, offsets, rows, slots)
     _check(lib().pipe_expert_rows(choice.data_ptr(), T, k, experts, offsets.data_ptr(), rows.data_ptr(), slots.data_ptr(),
                                   _stream_ptr(stream)), where)
 
@@ -571,12 +587,11 @@ def pipe_expert_linear(desc: GroupDesc, codes: torch.Tensor, scales: torch.Tenso
                        activation: int = ACT_IDENTITY, stream=None) -> None:
     """x: cuda [T, I]; offsets: int32 [E + 1]; rows: int32 [N] or None; y: [N, O]; bias: [E, O] or None."""
     where = "pipe_expert_linear"
-    h = _group_arrays(where, desc, codes, scales, zeros, x, y, bias, offsets, rows)
+    h = _group_arrays(where, desc, codes, scales, zeros, bias, x, y, offsets, rows)
     N = y.shape[0]
     _wants(where, x.dtype == h and y.dtype == h, "x or y has another type than the layer")
     _wants(where, offsets.dtype == torch.int32 and offsets.numel() == desc.experts + 1 and offsets.is_contiguous(), "offsets")
     _wants(where, rows is None or (rows.dtype == torch.int32 and rows.numel() == N and rows.is_contiguous()), "rows")
-    _wants(where, bias is None or (bias.dtype == h and bias.numel() == desc.experts * desc.out_features and bias.is_contiguous()), "bias")
     _check(lib().pipe_expert_linear(C.byref(desc), codes.data_ptr(), scales.data_ptr(), _dp(zeros), x.data_ptr(), x.shape[0],
                                     _rows_of(where, x, desc.in_features), _dp(rows), offsets.data_ptr(), N, _dp(bias), activation,
                                     y.data_ptr(), _rows_of(where, y, desc.out_features), _stream_ptr(stream)), where)
