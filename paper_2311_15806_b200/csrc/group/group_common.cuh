@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include "group_plan.h"
 #include "pipe_common.cuh"
 
 namespace pipe {
@@ -199,7 +200,6 @@ __device__ __forceinline__ void make_ascending(int& lo, int& hi, int& top, bool 
 // The rows cut into units of at most `per` rows of one expert, numbered expert by expert.  The table, unit_ints(E) integers of shared
 // memory: first[e], the units before expert e (first[E]: all of them), begin[e] and end[e], its rows.  Offsets are taken as clamped to
 // [0, N] and ascending, whatever they hold.
-__host__ __device__ inline int unit_ints(int E) { return 3 * E + 1; }
 template <int THREADS>
 __device__ __forceinline__ void build_units(const Call& c, int per, int32_t* table) {
   for (int e = threadIdx.x; e < c.E; e += THREADS) {
@@ -261,11 +261,7 @@ __device__ __forceinline__ Unit unit_at(const int32_t* table, int E, int per, in
   r.hi = end - r.lo < per ? end : r.lo + per;
   return r;
 }
-// The most units that N rows on E experts can make: every expert with rows has at most one tile that is not full.
-inline int64_t most_units(const Call& c, int per) {
-  if (!c.offsets) return ceil_div<int64_t>(c.N, per);
-  return (c.N < c.E ? c.N : static_cast<int64_t>(c.E)) + c.N / per;
-}
+inline int64_t most_units(const Call& c, int per) { return most_units(c.offsets != nullptr, c.N, c.E, per); }
 
 // What a failed call of the runtime leaves behind is taken away with it: launch_status() of this thread's next call would report it.
 inline pipe_status runtime_failed() {

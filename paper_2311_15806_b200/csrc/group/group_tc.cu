@@ -34,28 +34,13 @@ namespace grp {
 using namespace tcc;
 
 template <bool TA>
-constexpr int kTWideners = TA ? 4 : 2;   // groups of four warps; TA: widened weights in tensor memory
+constexpr int kTWideners = widener_groups(TA);
 template <bool TA>
 constexpr int kTThreads = 256 + 128 * kTWideners<TA>;
 constexpr uint32_t kTAcol = 256;         // their columns
-constexpr int kTStage = 128;         // reduction length of a stage
-constexpr int kTMaxRing = 6;         // most stages of activations
-constexpr int kTMaxCodes = 12;       // most stages of codes
-constexpr int kTMaxSmem = 226 * 1024;   // dynamic shared memory (the rest of 227 KiB: barriers)
-constexpr int kTCodeBytes = 128 * kTStage / 2;            // of a stage
-constexpr int kTSlotBytes = 128 * kTStage * 2;            // widened weights of a stage
-constexpr int kTTurnBytes = 32 * 128 * 2;   // 32 rows of y by 128 channels
-
-struct TcArgs {
+struct TcArgs : TcPlan {
   Call c;
-  int TN;          // rows of a tile
-  int mtiles;      // ceil(O / (128 CG))
-  int stages;      // ceil(I / 128)
-  int split;       // CTAs that share a tile's reduction axis
-  int code_depth;
-  int ring;        // stages of activations, at least the groups of wideners
   int wide_y;      // rows of y are 16-byte aligned
-  uint32_t off_a, off_codes, off_turn, off_table;   // shared memory behind the activations
 };
 
 __device__ __forceinline__ void tma_pair_2d(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
@@ -776,74 +761,15 @@ static bool encode_2d(CUtensorMap* map, CUtensorMapDataType type, const void* ba
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The tile's rows (p->TN), the CTAs of a tile (*cg) and those that share its axis (p->split): the least of
-//     rounds of tiles on the SMs * (stages of a CTA * time of a stage + half a microsecond) + the sum over the CTAs of a split,
-// in nanoseconds, with the times of a stage that were measured (11008 <-> 4096 and 2048 x 2048, 17 to 1024 rows):
-//     one CTA 0.31 + TN / 1000 us, a pair with its weights in tensor memory 0.31 + 0.8 TN / 1000, in shared memory 0.36 + 1.2 TN / 1000,
-//     and 0.6 at least (its two groups of wideners),
-//     the split's sums 0.5 us + 3 ns a row and CTA.
-// Either side of its choices there (us): 2048 x 2048, 128 rows: units of 32 rows 10.3, of 128 12.4, those split four ways 11.4, eight ways 28;
-// 4096 -> 11008: 300 rows as 3 units of pairs 33.5, as 2 43.6, 512 rows 46.4 and 49.4, 1024 rows 74.3 and 70.4; 11008 -> 4096, 17 rows: split
-// four ways 15.6, not split 34.7.  kClusters: the clusters of 1, 2, .. CTAs, a whole SM each, that stand on the chip at once (as the runtime
-// counts them, less one or two where they leave SMs of a processing cluster free: those differ from chip to chip).
-constexpr int kClusters[9] = {0, 148, 74, 44, 32, 24, 20, 14, 14};
-static void choose_tile(const Call& c, TcArgs* p, int* cg) {
-  const int64_t experts = c.offsets ? (c.N < c.E ? c.N : c.E) : 1;
-  const int64_t mean = ceil_div<int64_t>(c.N, experts);   // rows of an expert
-  int64_t best = -1;
-  for (int cap = 32; cap <= 256; cap *= 2) {
-    // rows fill units evenly where there is one expert; otherwise an expert's last unit is half full, on average
-    const int64_t units2 = c.offsets ? (2 * mean > cap ? 2 * mean + cap : 2 * cap) * experts / cap : 2 * ceil_div<int64_t>(c.N, cap);
-    const int rows = c.offsets ? static_cast<int>(mean < cap ? round_up<int64_t>(mean, 32) : cap)
-                               : static_cast<int>(round_up<int64_t>(ceil_div<int64_t>(2 * c.N, units2), 32));
-    for (int pair = 1; pair <= 2; ++pair) {
-      if ((pair == 2 && c.O <= 128) || (pair == 1 && cap > 128)) continue;
-      const int64_t tiles = ceil_div<int64_t>(units2, 2) * ceil_div(c.O, 128 * pair);
-      const int64_t stage = pair == 1 ? 310 + rows : (cap <= 128 ? 310 + rows * 4 / 5 : (rows < 200 ? 600 : 360 + rows * 6 / 5));
-      for (int split = 1; split <= 8; ++split) {
-        if (split > 1 && (pair == 2 || tiles > kClusters[split] || p->stages < 4 * split)) break;
-        const int64_t rounds = ceil_div<int64_t>(tiles, pair == 2 ? kClusters[2] : kClusters[split]);
-        const int64_t cost = rounds * (ceil_div(p->stages, split) * stage + 500) + (split > 1 ? 500 + 3 * split * rows : 0);
-        if (best < 0 || cost < best) {
-          best = cost;
-          p->TN = c.offsets ? cap : rows;
-          p->split = split;
-          *cg = pair;
-        }
-      }
-    }
-  }
-  // (the bound on an expert call's units may be more than the clusters of one round can take: those tiles are one each)
-  if (p->split > 1 && most_units(c, p->TN) * ceil_div(c.O, 128) * p->split >= (int64_t{1} << 31)) p->split = 1;
-}
-
 pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
-  // (no tensor to copy from; more runs of codes than a copy's coordinate counts: the other kernel)
-  if (c.T == 0 || static_cast<int64_t>(c.E) * c.KB >= (int64_t{1} << 31)) return PIPE_ERR_UNSUPPORTED;
   TcArgs p;
   p.c = c;
-  p.stages = ceil_div(c.I, kTStage);
-  int cg = 1;
-  choose_tile(c, &p, &cg);
-  p.mtiles = ceil_div(c.O, 128 * cg);
-  const int64_t tiles = most_units(c, p.TN) * p.mtiles;
-  if (tiles >= (int64_t{1} << 31)) return PIPE_ERR_UNSUPPORTED;
-  int64_t teams = p.split > 1 ? tiles : kPlanSMs / cg;
-  if (teams > tiles) teams = tiles;
+  // (no tensor to copy from, or no plan: the other kernel)
+  if (c.T == 0 || !plan_tc(TcShape{c.E, c.O, c.I, c.offsets != nullptr, c.N}, &p)) return PIPE_ERR_UNSUPPORTED;
+  static_assert(kChipSMs == kPlanSMs, "one chip");
   p.wide_y = !(reinterpret_cast<uintptr_t>(c.y) & 15) && c.ldy % 8 == 0;
-  const int own = p.TN / cg;
-  const bool ta = p.TN <= 128;
-  p.ring = ta ? 4 : 3;
-  const int x_bytes = p.ring * own * 256, a_bytes = ta ? 0 : kTWideners<false> * kTSlotBytes, turn = p.split > 1 ? 0 : 2 * kTTurnBytes;
-  const int table = unit_ints(c.E) * 4;
-  const int room = kTMaxSmem - 1024 - x_bytes - a_bytes - turn - table;
-  p.code_depth = room / kTCodeBytes < kTMaxCodes ? room / kTCodeBytes : kTMaxCodes;
-  if (p.code_depth < (ta ? kTWideners<true> : kTWideners<false>)) return PIPE_ERR_UNSUPPORTED;
-  p.off_a = x_bytes;
-  p.off_codes = p.off_a + a_bytes;
-  p.off_turn = p.off_codes + p.code_depth * kTCodeBytes;
-  p.off_table = p.off_turn + turn;
-  const int smem = 1024 + static_cast<int>(p.off_table) + table;
+  const int cg = p.cg;
+  const bool ta = p.ta;
   // activations: boxes of 64 columns; codes: rows of O runs of 16 bytes, taken as 8-byte elements, a stage's four runs of 128 channels in
   // one box (behind the layer's channels zeros; behind an expert's last run the next one's, which meet scales of zero)
   CUtensorMap xmap, cmap;
@@ -860,9 +786,9 @@ pipe_status linear_tc(const Call& c, bool bf16, cudaStream_t stream) {
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = cg * p.split;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.gridDim = dim3(static_cast<unsigned>(teams * cg * p.split));
+  cfg.gridDim = dim3(static_cast<unsigned>(p.teams * cg * p.split));
   cfg.blockDim = dim3(ta ? kTThreads<true> : kTThreads<false>);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = p.smem;
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
