@@ -476,6 +476,11 @@ def _on_current(where: str, first: torch.Tensor, *others) -> None:
         raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: all tensors have to be on the current device")
 
 
+def _matrices(where: str, a: torch.Tensor, b: torch.Tensor) -> None:
+    if a.dim() != 2 or b.dim() != 2:
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: matrices are needed, not shapes {tuple(a.shape)} and {tuple(b.shape)}")
+
+
 def _rows_of(where: str, t: torch.Tensor, cols: int) -> int:
     """Row pitch of a [rows, cols] matrix whose rows are contiguous."""
     shape, stride = t.shape, t.stride()
@@ -559,6 +564,7 @@ def pipe_group_linear(desc: GroupDesc, codes: torch.Tensor, scales: torch.Tensor
                       y: torch.Tensor, bias: torch.Tensor | None = None, activation: int = ACT_IDENTITY, stream=None) -> None:
     """x: cuda [T, I], y: cuda [T, O], bias: [O] (or [1, O]), all in the layer's type."""
     where = "pipe_group_linear"
+    _matrices(where, x, y)
     h = _group_arrays(where, desc, codes, scales, zeros, bias, x, y)
     T = x.shape[0]
     if x.dtype != h or y.dtype != h or T != y.shape[0]:
@@ -587,6 +593,7 @@ def pipe_expert_linear(desc: GroupDesc, codes: torch.Tensor, scales: torch.Tenso
                        activation: int = ACT_IDENTITY, stream=None) -> None:
     """x: cuda [T, I]; offsets: int32 [E + 1]; rows: int32 [N] or None; y: [N, O]; bias: [E, O] or None."""
     where = "pipe_expert_linear"
+    _matrices(where, x, y)
     h = _group_arrays(where, desc, codes, scales, zeros, bias, x, y, offsets, rows)
     N = y.shape[0]
     _wants(where, x.dtype == h and y.dtype == h, "x or y has another type than the layer")
@@ -600,6 +607,7 @@ def pipe_expert_linear(desc: GroupDesc, codes: torch.Tensor, scales: torch.Tenso
 def pipe_expert_combine(y: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor, out: torch.Tensor, stream=None) -> None:
     """y: cuda [N, O]; slots: int32 [T, k]; weights: float32 [T, k]; out: [T, O] of y's type."""
     where = "pipe_expert_combine"
+    _matrices(where, y, out)
     _on_current(where, y, slots, weights, out)
     _wants(where, y.dtype == out.dtype and y.dtype in _DTYPES and slots.dtype == torch.int32 and weights.dtype == torch.float32, "types")
     _wants(where, slots.dim() == 2 and weights.shape == slots.shape and slots.is_contiguous() and weights.is_contiguous() and

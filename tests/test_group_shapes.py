@@ -77,3 +77,16 @@ def test_slots():
     for shape in ((0, 2), (0,)):
         with pytest.raises(B.PipeError, match="current device"):
             B.pipe_expert_rows(torch.zeros((0, 2), dtype=I32), 4, offsets, torch.zeros(0, dtype=I32), torch.zeros(shape, dtype=I32))
+
+
+@pytest.mark.parametrize("shape", [(), (O,), (1, 5, O)])
+def test_rows_that_are_no_matrix_are_an_argument_error(shape):
+    good_x, good_y = torch.zeros((5, I), dtype=BF16), torch.zeros((5, O), dtype=BF16)
+    bad = torch.zeros(shape, dtype=BF16)
+    for x, y in ((bad, good_y), (good_x, bad)):
+        for call in (lambda: B.pipe_group_linear(*_layer(1), x, y), lambda: B.pipe_expert_linear(*_layer(), x, torch.zeros(E + 1, dtype=I32), y)):
+            with pytest.raises(B.PipeError, match="matrices"):
+                call()
+    for y, out in ((bad, good_y), (good_y, bad)):
+        with pytest.raises(B.PipeError, match="matrices"):
+            B.pipe_expert_combine(y, torch.zeros((5, 2), dtype=I32), torch.zeros((5, 2)), out)
