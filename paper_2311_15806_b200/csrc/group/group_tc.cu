@@ -487,6 +487,7 @@ __global__ void __launch_bounds__(kTThreads<TA>, 1) group_tc_kernel(const __grid
           if (lane == 0) arrive_lead(lead + 8 * rp.slot);
         }
     }
+    __syncwarp();   // (one thread may have been alone)
   } else if (warp >= 8) {
     // ---- weights: a thread's channel is a row of the tile
     constexpr uint32_t W = kTWideners<TA>;

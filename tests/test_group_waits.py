@@ -33,7 +33,9 @@ def test_the_lanes_of_a_warp_leave_a_wait_together():
     assert inner.count("mbar_wait") == 3 and inner.count("break") == 1 and "return" not in inner
     assert inner.index("if ((TA || elect_one()) && ok) {") < inner.index("mma_f16<") < inner.index("commit<CG>(done") < \
         inner.index("if (!TA) ok = __all_sync(0xffffffffu, ok) != 0;") < inner.index("if (!ok) break;")
-    # a single thread meets no collective
+    # a single thread meets no collective, and its warp is whole again before the block's barriers
+    issuing = kernel[kernel.index("if (rank == 0 && (!TA || elect_one())) {"):kernel.index("} else if (warp >= 8) {")]
+    assert issuing.rstrip().endswith("}\n    __syncwarp();")
     for line in products.splitlines()[1:]:
         assert not re.search(r"__\w*sync\w*\(|elect_one|warp_wait", line) or re.search(r"!TA\)|TA \|\||TA \? mbar_wait", line), line
     assert products.rstrip().endswith("if (!ok) drain_ring(done, issued, p.ring, 20000000ll);")
