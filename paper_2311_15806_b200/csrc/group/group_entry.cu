@@ -69,7 +69,9 @@ static pipe_status product(Call& c, bool bf16, cudaStream_t stream) {
   if (c.N == 0) return PIPE_OK;
   c.status = device_status_word();
   if (!c.status) return runtime_failed();
-  // Up to 16 rows (on experts: on average, rounded up) the codes' bytes are what counts; the small kernel holds 16 rows a unit.
+  // Up to 16 rows (on experts: on average, rounded up) go to the kernel that holds them in one unit and whose weights are exact.  Either
+  // side of the border (us): 4096 -> 11008 on 16 rows 13.3 there, on 17 rows 17.4 on the tensor cores; 11008 -> 4096 the other way round,
+  // 13 rows 19.5 to 22 there, 17 rows 16.4 on the tensor cores.
   const int64_t rows = c.offsets ? ceil_div<int64_t>(c.N, c.E) : c.N;
   pipe_status st = rows > 16 ? linear_tc(c, bf16, stream) : PIPE_ERR_UNSUPPORTED;
   if (st == PIPE_ERR_UNSUPPORTED) st = linear_small(c, bf16, stream);

@@ -53,7 +53,7 @@ struct TcPlan {
 //     one CTA 0.31 + TN / 1000 us, a pair with its weights in tensor memory 0.31 + 0.8 TN / 1000, in shared memory 0.36 + 1.2 TN / 1000,
 //     and 0.6 at least (its two groups of wideners),
 //     the split's sums 0.5 us + 3 ns a row and CTA.
-// Either side of its choices there (us): 2048 x 2048, 128 rows: units of 32 rows 10.3, of 128 12.4, those split four ways 11.4, eight ways 28;
+// Either side of its choices there (us, when the rule was made; 17 to 512 rows have since become some 3 % faster): 2048 x 2048, 128 rows: units of 32 rows 10.3, of 128 12.4, those split four ways 11.4, eight ways 28;
 // 4096 -> 11008: 300 rows as 3 units of pairs 33.5, as 2 43.6, 512 rows 46.4 and 49.4, 1024 rows 74.3 and 70.4; 11008 -> 4096, 17 rows: split
 // four ways 15.6, not split 34.7.  kClusters: the clusters of 1, 2, .. CTAs, a whole SM each, that stand on the chip at once (as the runtime
 // counts them, less one or two where they leave SMs of a processing cluster free: those differ from chip to chip).

@@ -303,7 +303,8 @@ pipe_status linear_small(const Call& c, bool bf16, cudaStream_t stream) {
   const int64_t rows = c.offsets ? ceil_div<int64_t>(c.N, c.E) : c.N;
   const int nt = rows <= 8 ? 1 : 2;
   // Channels of a tile (16 mt) and CTAs that share an axis: a round of CTAs costs some 3 us before its first product (launch, addresses,
-  // first loads), and each step of a warp's share 0.3, 0.46 or 0.85 us (mt = 1, 2, 4; two column tiles 0.75).  Measured against this
+  // first loads), and each step of a warp's share 0.3, 0.46 or 0.85 us (mt = 1, 2, 4; two column tiles 0.75).  These are weights that
+  // order the choices below, no times: 11008 -> 4096 on 13 rows comes to 11.8 us by them and takes 19.5 to 22.  Measured against them
   // (one token): 4096 -> 11008 mt = 1 alone 8.2 us, with two CTAs to a tile 12.0, mt = 2 alone 9.4; 11008 -> 4096 mt = 2 with four 8.5,
   // with two 10.0, mt = 1 with two 10.7, with four 14.7; 54 units of 2048 -> 1408 mt = 4 18, mt = 2 20, mt = 1 32.
   p.units = static_cast<int>(most_units(c, 8 * nt));

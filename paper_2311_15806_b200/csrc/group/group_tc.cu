@@ -22,9 +22,10 @@
 //   warps 4-7   drain accumulators (bias, sigma, rounding, a turn in shared memory to rows of y)
 //   warps 8-    groups that widen weights, stages in turn
 // Few tiles: the CTAs of a cluster share a tile's reduction axis and add their sums through distributed shared memory, in order.
-// Measured (bf16, groups of 128): 4096 -> 11008 on 4096 rows 249 us alone in a graph, 1.48 PFLOP/s, tensor pipe 85 % active; with SiLU,
-// among other passes, at the power cap 292; 8 experts of it, 8192 gathered rows, 566 alone, 640 to 670 among others (tensor pipe 72 %).
-// 1024 rows 72, 128 rows 20, 17 rows 18: there a stage takes its fixed time, whatever its width, and 86 tiles leave 62 SMs idle.
+// Measured (bf16, groups of 128): 4096 -> 11008 on 4096 rows 247 us alone in a graph, 1.50 PFLOP/s, tensor pipe 83 % active; with SiLU,
+// among other passes, at the power cap 296; 8 experts of it, 8192 gathered rows, 567 alone, 640 to 670 among others (tensor pipe 70 %).
+// 1024 rows 71, 512 50 (tensor pipe 59 %), 128 19.6 (41 %), 17 17.4 (11 %): there a stage takes its fixed time, whatever its width, and 86
+// tiles leave 62 SMs idle.
 #include "group_common.cuh"
 #include "pipe_tc_common.cuh"
 
