@@ -515,7 +515,7 @@ pipe_status pipe_lower_conv_input(const pipe_conv_geom* geom, const int8_t* d_xq
  */
 #define PIPE_DTYPE_BF16 0
 #define PIPE_DTYPE_FP16 1
-#define PIPE_DTYPE_FP32 2   /* source weights of pipe_group_quantize only */
+#define PIPE_DTYPE_FP32 2   /* in the 4-bit layers: source weights of pipe_group_quantize only */
 #define PIPE_MAX_EXPERTS 1024
 typedef struct pipe_group_desc {
   int32_t experts;       /* E, 1..PIPE_MAX_EXPERTS (1: a plain layer) */
@@ -600,6 +600,84 @@ pipe_status pipe_expert_linear(const pipe_group_desc* desc, const void* d_codes,
  */
 pipe_status pipe_expert_combine(const void* d_y, int64_t N, int64_t ldy, const int32_t* d_slots, const float* d_weights, int64_t T,
                                 int32_t k, int32_t O, int32_t dtype, void* d_out, int64_t ldo, void* stream);
+
+/*
+ * 8-bit integer layers with a scale for each channel, on activations with a scale for each token.
+ *
+ * The other form in which checkpoints of large language models come: int8 codes, a float scale for every row of W, and activations
+ * that are brought to int8 on the way, every token by a scale of its own.  (pipe_quantize_act has one scale for the whole tensor.)  A
+ * layer of E experts [O, I] is two device arrays, which may come from elsewhere than pipe_int8_quantize:
+ *   codes   int8, E*O rows of I at a pitch of ldw bytes, a multiple of 16, 16-byte aligned; expert e's rows follow expert e-1's
+ *   scales  float [E*O]
+ * and stands for W_e[o, i] = scales[e*O + o] * codes[e*O + o, i]; activations likewise, row by row.  -128 is a code like any other.
+ */
+#define PIPE_INT8_MAX_FEATURES 131071   /* 128 * 128 * I stays below 2^31 */
+typedef struct pipe_int8_desc {
+  int32_t experts;       /* E, 1..PIPE_MAX_EXPERTS (1: a plain layer) */
+  int32_t out_features;  /* O: rows of W, at most 2^29, E*O at most 2^30 */
+  int32_t in_features;   /* I: reduction length, any; beyond PIPE_INT8_MAX_FEATURES PIPE_ERR_ACC_OVERFLOW */
+  int32_t dtype;         /* bias and outputs: PIPE_DTYPE_BF16, PIPE_DTYPE_FP16 or PIPE_DTYPE_FP32 */
+} pipe_int8_desc;
+
+/*
+ * Rows to int8, for weights (a row per channel) and activations (a row per token) alike: for every slot s < N, with
+ * r = d_rows[s], or s itself where d_rows is NULL (N = T then, otherwise PIPE_ERR_SHAPE),
+ *     scales[s] = max_i |x[r, i]| / 127 (binary32, IEEE division)      codes[s, i] = clamp(rne(x[r, i] / scales[s]), -127, 127)
+ * rne() is the integer nearest the exact quotient, ties to even.  A row whose scale is zero has codes 0.  With d_rows as
+ * pipe_expert_rows writes them, tokens are quantized in the order of their experts.  A row index outside [0, T) reads as a row of
+ * zeros.  d_count (NULL, or one int32 on the device): slots from *d_count on are left as they were (d_offsets + E of the experts'
+ * offsets: the slots behind the last expert's).  d_values (NULL, or float [N, I] pitch ldv): receives scales[s] * codes[s, i], rounded
+ * once: the numbers that the codes stand for.
+ * d_x: [T, I] pitch ldx of type x_dtype (PIPE_DTYPE_*), aligned to its type (16-byte aligned rows are faster); d_codes: [N, I] pitch
+ * ldc, any (what the products take: see above), 1 <= I <= 2^29; d_scales: [N].  Nothing that is written may overlap anything else.
+ * A NaN or Inf in a row that is read sets PIPE_ERR_NONFINITE in the device status word.  T and N at most 2^30; N = 0 is a no-op.
+ */
+pipe_status pipe_int8_quantize(const void* d_x, int32_t x_dtype, int64_t T, int32_t I, int64_t ldx, const int32_t* d_rows, int64_t N,
+                               const int32_t* d_count, int8_t* d_codes, int64_t ldc, float* d_scales, float* d_values, int64_t ldv,
+                               void* stream);
+
+/*
+ * y[t, o] = h(sigma((float(sum_i xq[t, i] * W[o, i]) * scales[o]) * sx[t] + bias[o])) for a layer of one expert: the sum is exact, what
+ * follows is binary32 (the second product and the bias are one fused operation, sigma is one of PIPE_ACT_*), h() rounds to the layer's
+ * type.  d_xq: int8 [T, I] pitch ldx bytes, a multiple of 16, 16-byte aligned; d_sx: float [T]; d_bias: [O] in the layer's type or
+ * NULL; d_y: [T, O] pitch ldy.  T = 0 is a no-op, T is at most 2^30.  d_y must not overlap the inputs.  A row of y does not depend on
+ * the other rows or on their number; equal calls give equal bits.
+ */
+pipe_status pipe_int8_linear(const pipe_int8_desc* desc, const int8_t* d_codes, int64_t ldw, const float* d_scales, const int8_t* d_xq,
+                             int64_t T, int64_t ldx, const float* d_sx, const void* d_bias, int32_t activation, void* d_y, int64_t ldy,
+                             void* stream);
+
+/*
+ * One launch of all experts, each on its own rows: for d_offsets[e] <= s < d_offsets[e+1]
+ *     y[s, o] = h(sigma((float(sum_i xq[s, i] * W_e[o, i]) * scales[e*O + o]) * sx[s] + bias[e, o])).
+ * d_xq [N, I], d_sx [N] and d_y [N, O] are in the order of the experts (pipe_int8_quantize with d_rows); offsets as in
+ * pipe_expert_linear: int32 [E+1] on the device, ragged, taken as clamped to [0, N] and ascending; rows of y behind the last are left
+ * as they were.  d_bias: [E, O] or NULL.  N at most 2^30.  Everything else, the results too, as in pipe_int8_linear.
+ */
+pipe_status pipe_int8_expert_linear(const pipe_int8_desc* desc, const int8_t* d_codes, int64_t ldw, const float* d_scales,
+                                    const int8_t* d_xq, int64_t ldx, const float* d_sx, const int32_t* d_offsets, int64_t N,
+                                    const void* d_bias, int32_t activation, void* d_y, int64_t ldy, void* stream);
+
+/*
+ * What a language model's logits l [T, V] say: with z = scale * l (scale: the inverse of a temperature, 2^-20 to 2^20) and
+ * norm_t = log sum_v exp z[t, v], sums in binary32,
+ *     logprobs[t, j]     = z[t, tokens[t, j]] - norm_t       the log probabilities of n given tokens; a token outside [0, V) (padding): 0
+ *     entropy[t]         = - sum_v p log p,  p = exp(z[t, v] - norm_t)
+ *     top[t, i]          = the token with the i-th largest logit, equal ones (-0 and 0 are) in ascending order, i < k
+ *     top_logprobs[t, i] = its log probability
+ * A logit of -Inf is a masked token: its probability is 0, its log probability -Inf, and it is not among the top; where fewer than k
+ * tokens are left, what is missing has token -1 and log probability -Inf.  A row of nothing but -Inf has log probabilities -Inf and
+ * entropy 0.  A row with a NaN or +Inf sets PIPE_ERR_NONFINITE in the device status word; its floats are NaN (those of tokens outside
+ * [0, V) 0), its top tokens -1; the other rows are as they would be without it.
+ * d_logits: [T, V] pitch ldl in `dtype` (PIPE_DTYPE_*), aligned to its type; d_tokens: int32 [T, n] dense, d_logprobs: float [T, n]
+ * dense (both NULL: n = 0); d_entropy: float [T] or NULL; d_top: int32 [T, k], d_top_logprobs: float [T, k] dense (both NULL: k = 0;
+ * either may be NULL by itself).  0 <= k <= PIPE_MAX_TOP, 0 <= n <= 2^20, T and V at most 2^30, T * n at most 2^40.  T = 0 is a no-op.  Outputs must not overlap
+ * anything.  A row's results do not depend on the other rows' values; equal calls give equal bits.
+ */
+#define PIPE_MAX_TOP 64
+pipe_status pipe_token_logprobs(const void* d_logits, int32_t dtype, int64_t T, int32_t V, int64_t ldl, float scale,
+                                const int32_t* d_tokens, int32_t n, float* d_logprobs, float* d_entropy, int32_t k, int32_t* d_top,
+                                float* d_top_logprobs, void* stream);
 
 /* Number of kernels the library has launched in this process (all calls, all streams). */
 uint64_t pipe_launch_count(void);

@@ -39,6 +39,7 @@ EXPORTS = ["pipe_keep_groups_from_gamma", "pipe_default_branches", "pipe_layout"
            "pipe_ensemble_forward_q8", "pipe_expanded_conv2d_q8", "pipe_ensemble_conv2d", "pipe_ensemble_conv2d_q8",
            "pipe_lower_conv_input",
            "pipe_group_layout", "pipe_group_quantize", "pipe_group_linear", "pipe_expert_rows", "pipe_expert_linear", "pipe_expert_combine",
+           "pipe_int8_quantize", "pipe_int8_linear", "pipe_int8_expert_linear", "pipe_token_logprobs",
            "pipe_launch_count", "pipe_poll_status", "pipe_status_string",
            # include/pipe_diag.h: tests and measurements only
            "pipe_diag_select_kernel", "pipe_diag_mma_i8_rate", "pipe_diag_bounded_wait"]
@@ -80,6 +81,10 @@ class GroupDesc(C.Structure):
 
 class GroupLayout(C.Structure):
     _fields_ = [("groups", C.c_int32), ("codes_bytes", C.c_uint64), ("scales_bytes", C.c_uint64), ("zeros_bytes", C.c_uint64)]
+
+
+class Int8Desc(C.Structure):
+    _fields_ = [("experts", C.c_int32), ("out_features", C.c_int32), ("in_features", C.c_int32), ("dtype", C.c_int32)]
 
 
 class PipeError(RuntimeError):
@@ -128,6 +133,10 @@ def lib() -> C.CDLL:
         L.pipe_expert_rows.argtypes = [p, i64, i32, i32, p, p, p, p]
         L.pipe_expert_linear.argtypes = [C.POINTER(GroupDesc), p, p, p, p, i64, i64, p, p, i64, p, i32, p, i64, p]
         L.pipe_expert_combine.argtypes = [p, i64, i64, p, p, i64, i32, i32, i32, p, i64, p]
+        L.pipe_int8_quantize.argtypes = [p, i32, i64, i32, i64, p, i64, p, p, i64, p, p, i64, p]
+        L.pipe_int8_linear.argtypes = [C.POINTER(Int8Desc), p, i64, p, p, i64, i64, p, p, i32, p, i64, p]
+        L.pipe_int8_expert_linear.argtypes = [C.POINTER(Int8Desc), p, i64, p, p, i64, p, p, i64, p, i32, p, i64, p]
+        L.pipe_token_logprobs.argtypes = [p, i32, i64, i32, i64, C.c_float, p, i32, p, p, i32, p, p, p]
         L.pipe_diag_select_kernel.argtypes = [i32]
         L.pipe_diag_mma_i8_rate.argtypes = [i32, i64, i32, C.POINTER(C.c_double), p]
         L.pipe_diag_bounded_wait.argtypes = [i64, p]
@@ -626,6 +635,121 @@ def alloc_group(desc: GroupDesc, device="cuda"):
     codes = torch.empty((E, I // 32, O, 16), dtype=torch.uint8, device=device)
     scales = torch.empty((E, lay.groups, O), dtype=h, device=device)
     return codes, scales, torch.empty((E, lay.groups, O), dtype=torch.uint8, device=device) if desc.asymmetric else None
+
+
+# ---- 8-bit integer layers with scales for each token and channel, log probabilities -----------------------------------------------
+INT8_MAX_FEATURES = 131071
+MAX_TOP = 64
+
+
+def make_int8_desc(O: int, I: int, dtype=torch.bfloat16, experts: int = 1) -> Int8Desc:
+    """dtype: of the bias and the outputs."""
+    if dtype not in _DTYPES:
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"make_int8_desc: dtype {dtype}")
+    return Int8Desc(int(experts), int(O), int(I), _DTYPES[dtype])
+
+
+def _pitch_of(where: str, t: torch.Tensor, cols: int) -> int:
+    """Row pitch of a [.., cols] array, [rows, cols] with leading dimensions joined, whose rows are contiguous and at one distance."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 2 and shape[1] == cols and (stride[1] == 1 or cols <= 1):
+        return stride[0] if shape[0] > 1 else max(cols + 15 & ~15, stride[0] & ~15)
+    if len(shape) == 3 and shape[2] == cols and (stride[2] == 1 or cols <= 1) and (shape[0] <= 1 or shape[1] <= 1 or stride[0] == shape[1] * stride[1]):
+        if shape[0] * shape[1] > 1:
+            return stride[1] if shape[1] > 1 else stride[0]
+        return max(cols + 15 & ~15, stride[1] & ~15)
+    raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: an array of shape {tuple(shape)} and strides {stride}, rows of {cols} at one distance are needed")
+
+
+def pipe_int8_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, rows: torch.Tensor | None = None,
+                       count: torch.Tensor | None = None, values: torch.Tensor | None = None, stream=None) -> None:
+    """x: cuda float32 / bfloat16 / float16 [T, I] (weights also [E, O, I]); codes: int8 [N, I] (or x's shape); scales: float32, N of
+    them; rows: int32 [N] or None (N = T); count: one int32 or None; values: float32 of codes' shape or None."""
+    where = "pipe_int8_quantize"
+    I = x.shape[-1] if x.dim() else 0
+    _wants(where, codes.dtype == torch.int8 and scales.dtype == torch.float32 and x.dtype in _DTYPES, "types")
+    ldx, ldc, ldv = _pitch_of(where, x, I), _pitch_of(where, codes, I), 0
+    N = scales.numel()
+    _wants(where, scales.is_contiguous() and N == codes.shape[:-1].numel(), "a scale for every row of codes")
+    _wants(where, rows is None or (rows.dtype == torch.int32 and rows.numel() == N and rows.is_contiguous()), "rows")
+    _wants(where, count is None or (count.dtype == torch.int32 and count.numel() == 1), "count")
+    if values is not None:
+        _wants(where, values.dtype == torch.float32 and values.shape == codes.shape, "values are float32 of the codes' shape")
+        ldv = _pitch_of(where, values, I)
+    _on_current(where, x, codes, scales, rows, count, values)
+    _check(lib().pipe_int8_quantize(x.data_ptr(), _DTYPES[x.dtype], x.shape[:-1].numel(), I, ldx, _dp(rows), N, _dp(count), codes.data_ptr(),
+                                    ldc, scales.data_ptr(), _dp(values), ldv, _stream_ptr(stream)), where)
+
+
+def _int8_product(where: str, desc: Int8Desc, codes, scales, xq, sx, bias, y, offsets) -> int:
+    """Checks what both products take alike; the pitch of the weights."""
+    E, O, N = desc.experts, desc.out_features, xq.shape[0] if xq.dim() else -1
+    i8, f32, h = torch.int8, torch.float32, y.dtype
+    if codes.dtype != i8 or xq.dtype != i8 or scales.dtype != f32 or sx.dtype != f32 or _DTYPES.get(h) != desc.dtype:
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: int8 codes, float32 scales and outputs of the layer's type are needed")
+    if codes.shape[:-1].numel() != E * O or not _laid_out(scales, E, O):
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: codes and scales are not the descriptor's arrays")
+    if y.dim() != 2 or y.shape[0] != N or sx.numel() != N or not sx.is_contiguous():
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: xq, sx and y differ in rows")
+    if bias is not None and (bias.dtype != h or not _laid_out(bias, E, O)):
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: the bias is not [E, O] in the layer's type")
+    _on_current(where, codes, scales, xq, sx, bias, y, offsets)
+    return _pitch_of(where, codes, desc.in_features)
+
+
+def pipe_int8_linear(desc: Int8Desc, codes: torch.Tensor, scales: torch.Tensor, xq: torch.Tensor, sx: torch.Tensor, y: torch.Tensor,
+                     bias: torch.Tensor | None = None, activation: int = ACT_IDENTITY, stream=None) -> None:
+    """codes: cuda int8 [O, I] (or [1, O, I]), scales: float32 [O]; xq: int8 [T, I], sx: float32 [T]; y: [T, O], bias: [O], in the layer's
+    type.  Rows of codes and xq lie at multiples of 16 bytes."""
+    where = "pipe_int8_linear"
+    ldw = _int8_product(where, desc, codes, scales, xq, sx, bias, y, None)
+    _check(lib().pipe_int8_linear(C.byref(desc), codes.data_ptr(), ldw, scales.data_ptr(), xq.data_ptr(), xq.shape[0],
+                                  _pitch_of(where, xq, desc.in_features), sx.data_ptr(), _dp(bias), activation, y.data_ptr(),
+                                  _pitch_of(where, y, desc.out_features), _stream_ptr(stream)), where)
+
+
+def pipe_int8_expert_linear(desc: Int8Desc, codes: torch.Tensor, scales: torch.Tensor, xq: torch.Tensor, sx: torch.Tensor,
+                            offsets: torch.Tensor, y: torch.Tensor, bias: torch.Tensor | None = None, activation: int = ACT_IDENTITY,
+                            stream=None) -> None:
+    """codes: cuda int8 [E, O, I], scales: float32 [E, O]; xq: int8 [N, I], sx: float32 [N]; offsets: int32 [E + 1]; y: [N, O];
+    bias: [E, O] or None."""
+    where = "pipe_int8_expert_linear"
+    ldw = _int8_product(where, desc, codes, scales, xq, sx, bias, y, offsets)
+    _wants(where, offsets.dtype == torch.int32 and offsets.numel() == desc.experts + 1 and offsets.is_contiguous(), "offsets")
+    _check(lib().pipe_int8_expert_linear(C.byref(desc), codes.data_ptr(), ldw, scales.data_ptr(), xq.data_ptr(),
+                                         _pitch_of(where, xq, desc.in_features), sx.data_ptr(), offsets.data_ptr(), xq.shape[0], _dp(bias),
+                                         activation, y.data_ptr(), _pitch_of(where, y, desc.out_features), _stream_ptr(stream)), where)
+
+
+def alloc_int8(rows: int, I: int, device="cuda", experts: int | None = None):
+    """codes ([rows, I], or [experts, rows, I]) at the pitch that the products want, and scales; unset."""
+    lead = (rows,) if experts is None else (experts, rows)
+    codes = torch.empty((*lead, I + 15 & ~15), dtype=torch.int8, device=device)[..., :I]
+    return codes, torch.empty(lead, dtype=torch.float32, device=device)
+
+
+def pipe_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, logprobs: torch.Tensor | None = None,
+                        entropy: torch.Tensor | None = None, top: torch.Tensor | None = None, top_logprobs: torch.Tensor | None = None,
+                        scale: float = 1.0, stream=None) -> None:
+    """logits: cuda float32 / bfloat16 / float16 [T, V]; tokens: int32 [T, n], logprobs: float32 [T, n] (or both [T]); entropy: float32
+    [T]; top: int32 [T, k], top_logprobs: float32 [T, k]."""
+    where = "pipe_token_logprobs"
+    _wants(where, logits.dim() == 2 and logits.dtype in _DTYPES, "logits [T, V] in float32, bfloat16 or float16")
+    T, V = logits.shape
+    n = k = 0
+    if tokens is not None or logprobs is not None:
+        _wants(where, tokens is not None and logprobs is not None and tokens.dtype == torch.int32 and logprobs.dtype == torch.float32 and
+               tokens.shape == logprobs.shape and tokens.dim() in (1, 2) and tokens.shape[0] == T and tokens.is_contiguous() and
+               logprobs.is_contiguous(), "tokens int32 [T, n] and logprobs float32 [T, n]")
+        n = tokens.shape[1] if tokens.dim() == 2 else 1
+    _wants(where, entropy is None or (entropy.dtype == torch.float32 and entropy.shape == (T,) and entropy.is_contiguous()), "entropy float32 [T]")
+    for t, kind in ((top, torch.int32), (top_logprobs, torch.float32)):
+        if t is not None:
+            _wants(where, t.dtype == kind and t.dim() == 2 and t.shape[0] == T and t.is_contiguous() and k in (0, t.shape[1]), "top int32 [T, k], top_logprobs float32 [T, k]")
+            k = t.shape[1]
+    _on_current(where, logits, tokens, logprobs, entropy, top, top_logprobs)
+    _check(lib().pipe_token_logprobs(logits.data_ptr(), _DTYPES[logits.dtype], T, V, _pitch_of(where, logits, V), scale, _dp(tokens), n, _dp(logprobs), _dp(entropy), k, _dp(top),
+                                     _dp(top_logprobs), _stream_ptr(stream)), where)
 
 
 def pipe_diag_select_kernel(which: int) -> None:

@@ -10,20 +10,21 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libpipe.so")
+_FOLDERS = ("", "group", "int8", "logprob")   # of CSRC
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 
 
 def _sources() -> list[str]:
-    return sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "group", "*.cu")))
+    return sorted(s for d in _FOLDERS for s in glob.glob(os.path.join(CSRC, d, "*.cu")))
 
 
 def _stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = _sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "group", "*.cuh")) + glob.glob(os.path.join(CSRC, "group", "*.h")) + glob.glob(os.path.join(_ROOT, "include", "*.h"))
+    deps = _sources() + [h for d in _FOLDERS for e in ("*.cuh", "*.h") for h in glob.glob(os.path.join(CSRC, d, e))] + glob.glob(os.path.join(_ROOT, "include", "*.h"))
     return any(os.path.getmtime(d) > t for d in deps)
 
 

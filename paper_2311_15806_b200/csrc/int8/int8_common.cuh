@@ -1,0 +1,41 @@
+// What the kernels of the 8-bit integer layers share (formats and entry points: include/pipe.h).
+#pragma once
+
+#include "../group/group_common.cuh"
+
+namespace pipe {
+namespace i8 {
+
+// One call of pipe_int8_linear (c.offsets = nullptr: one expert that owns all N rows) or pipe_int8_expert_linear.
+struct Call {
+  grp::Call c;          // E, O, I; x: int8 [T, I] with T = N, ldx in bytes; offsets, N; bias, act, y, ldy; status
+  const int8_t* w;      // E * O rows of I, pitch ldw
+  int64_t ldw;
+  const float* sw;      // [E * O]
+  const float* sx;      // [N]
+  int dtype;            // of bias and y
+};
+
+// The types of bias and outputs.
+struct Fp32 {
+  using T = float;
+  static __device__ __forceinline__ float load(const void* p, int64_t i) { return __ldcg(static_cast<const float*>(p) + i); }
+  static __device__ __forceinline__ void store(void* p, int64_t i, float v) { static_cast<float*>(p)[i] = v; }
+};
+template <class H>
+struct Half {
+  using T = uint16_t;
+  static __device__ __forceinline__ float load(const void* p, int64_t i) { return H::to_float(__ldcg(static_cast<const uint16_t*>(p) + i)); }
+  static __device__ __forceinline__ void store(void* p, int64_t i, float v) { static_cast<uint16_t*>(p)[i] = H::from_float(v); }
+};
+using Bf16 = Half<grp::Bf16>;
+using Fp16 = Half<grp::Fp16>;
+
+// The output from an exact sum: one rounding each of the sum, its product with the channel's scale, and (fused with the bias) that with
+// the token's.
+__device__ __forceinline__ float scaled(int acc, float sw, float sx, float bias) { return fmaf(__fmul_rn(static_cast<float>(acc), sw), sx, bias); }
+
+pipe_status linear_simple(const Call& c, cudaStream_t stream);
+
+}  // namespace i8
+}  // namespace pipe
