@@ -18,13 +18,15 @@ struct Call {
 
 // The types of bias and outputs.
 struct Fp32 {
-  using T = float;
+  static constexpr int kBytes = 4;
+  static __device__ __forceinline__ uint32_t pack(float, float) { return 0; }   // (of 16-bit types only)
   static __device__ __forceinline__ float load(const void* p, int64_t i) { return __ldcg(static_cast<const float*>(p) + i); }
   static __device__ __forceinline__ void store(void* p, int64_t i, float v) { static_cast<float*>(p)[i] = v; }
 };
 template <class H>
 struct Half {
-  using T = uint16_t;
+  static constexpr int kBytes = 2;
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return H::pack(lo, hi); }
   static __device__ __forceinline__ float load(const void* p, int64_t i) { return H::to_float(__ldcg(static_cast<const uint16_t*>(p) + i)); }
   static __device__ __forceinline__ void store(void* p, int64_t i, float v) { static_cast<uint16_t*>(p)[i] = H::from_float(v); }
 };
@@ -35,7 +37,7 @@ using Fp16 = Half<grp::Fp16>;
 // the token's.
 __device__ __forceinline__ float scaled(int acc, float sw, float sx, float bias) { return fmaf(__fmul_rn(static_cast<float>(acc), sw), sx, bias); }
 
-pipe_status linear_simple(const Call& c, cudaStream_t stream);
+pipe_status linear_tc(const Call& c, cudaStream_t stream);
 
 }  // namespace i8
 }  // namespace pipe

@@ -42,7 +42,7 @@ static pipe_status product(const pipe_int8_desc* desc, const int8_t* codes, int6
   c.dtype = desc->dtype;
   c.c.status = device_status_word();
   if (!c.c.status) return grp::runtime_failed();
-  const pipe_status st = linear_simple(c, stream);
+  const pipe_status st = linear_tc(c, stream);
   if (st == PIPE_OK) take_expansion_mark(stream);
   return st;
 }
