@@ -6,7 +6,7 @@
 // read as zeros.  Sums are int32 in tensor memory, exact, in two accumulators, so that the drain of a tile overlaps the next one's
 // products.  The drain applies the channel's scale, the token's, bias and sigma; 16-bit outputs are turned in shared memory to rows of
 // y, 32-bit ones are stored as they come, 32 neighbouring channels at a time.
-//   warp 0 copies   warp 1 MMAs, tensor memory   warps 2-5 drain
+//   warp 0 copies   warp 1 MMAs, tensor memory   warps 2-9 drain, two for every 32 lanes of tensor memory, which take 32 rows in turn
 // Few tiles: the CTAs of a cluster share a tile's reduction axis and add their sums through distributed shared memory (integers: in any
 // order the same).  Such a CTA gives its tensor memory back before it waits for the others: one that held it could wait for a CTA
 // that waits for tensor memory on another SM.
@@ -25,11 +25,10 @@ using grp::cluster_rank;
 using grp::cluster_sync;
 using grp::Unit;
 
-constexpr int kThreads = 192;
+constexpr int kThreads = 64 + 32 * kDrainWarps;
 struct TcArgs : TcPlan {
   Call call;
   int wide_y;      // rows of y are 16-byte aligned
-  int ahead;       // stages of the first tile's weights that are asked for early
 };
 
 __device__ __forceinline__ void tma_pair_2d(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
@@ -90,21 +89,6 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(pred));
   return pred != 0;
 }
-// Whether all four warps of the drain may go on: behind it they meet at barriers without a limit, so that one that has given up must
-// not leave the others waiting.
-__device__ __forceinline__ bool drain_agrees(bool ok) {
-  uint32_t all;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
-      "bar.red.and.pred q, 1, 128, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(all)
-      : "r"(ok ? 1u : 0u)
-      : "memory");
-  return all != 0;
-}
-__device__ __forceinline__ void drain_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
-
 // Eight neighbouring outputs of a row of y, `room` of them inside the layer.
 template <class H>
 __device__ __forceinline__ void store_y8(void* y, int64_t at, const float (&v)[8], int wide, int room) {
@@ -123,16 +107,23 @@ __device__ __forceinline__ void store_y8(void* y, int64_t at, const float (&v)[8
   }
 }
 
-// Tile t of the launch: a unit's rows, 128 CG channels from 128 CG m on.
+// Tile t of the launch: a unit's rows, TM channels of every CTA.
 struct Tile : Unit {
-  int m;
+  int o0;  // this CTA's first channel
   int n;   // columns of its MMAs: the rows rounded up to what the MMA takes
 };
 template <int CG>
-__device__ __forceinline__ Tile tile_of(const TcArgs& p, const int32_t* table, int t) {
+__device__ __forceinline__ Tile tile_of(const TcArgs& p, const int32_t* table, int t, int rank) {
   Tile r;
-  static_cast<Unit&>(r) = grp::unit_at(table, p.call.c.E, p.TN, t / p.mtiles);
-  r.m = t % p.mtiles;
+  const int u = t / p.mtiles;
+  if (p.call.c.offsets) {
+    static_cast<Unit&>(r) = grp::unit_at(table, p.call.c.E, p.TN, u);
+  } else {   // (N and the tile's end are below 2^31)
+    r.e = 0;
+    r.lo = u * p.TN;
+    r.hi = min(r.lo + p.TN, static_cast<int>(p.call.c.N));
+  }
+  r.o0 = (t % p.mtiles * CG + rank) * p.TM;
   constexpr int kStep = CG == 2 ? 32 : 16;
   r.n = (r.hi - r.lo + kStep - 1) & ~(kStep - 1);
   return r;
@@ -158,7 +149,8 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
   const int part = CG == 1 && p.split > 1 ? crank : 0;  // of the reduction axis
   const int team = blockIdx.x / (CG * p.split), teams = gridDim.x / (CG * p.split);
   const int st0 = p.stages * part / p.split, st1 = p.stages * (part + 1) / p.split;   // (stages <= 1024)
-  const uint32_t x_bytes = static_cast<uint32_t>(p.TN / CG) * kStage, stage_bytes = kWBytes + x_bytes;
+  const uint32_t w_block = static_cast<uint32_t>(p.TM) * kBlock, x_block = static_cast<uint32_t>(p.TN / CG) * kBlock;
+  const uint32_t stage_bytes = p.KS * (w_block + x_block);
   const uint32_t ring = p.ring;
   const int acc_pitch = p.TN < 32 ? 32 : p.TN;
 
@@ -170,12 +162,14 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(d_full + 8 * b, 1);
-      mbar_init(d_empty + 8 * b, 4 * CG);
+      mbar_init(d_empty + 8 * b, kDrainWarps * CG);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&wmap)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&xmap)) : "memory");
     if (!c.offsets && team < p.tiles) {
-      const int o0 = ((team % p.mtiles) * CG + rank) * 128;
-      for (int st = st0; st < st1 && st < st0 + p.ahead; ++st) ask_l2(&wmap, st * kStage, o0);
+      const int o0 = (team % p.mtiles * CG + rank) * p.TM;
+      for (int b = st0 * p.KS; b < st1 * p.KS && b < st0 * p.KS + p.ahead; ++b) ask_l2(&wmap, b * kBlock, o0);
     }
   }
   if (warp == 1) {
@@ -189,13 +183,13 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
   }
   grid_wait();
   grid_release();
-  grp::build_units<kThreads>(c, p.TN, table);
+  if (c.offsets) grp::build_units<kThreads>(c, p.TN, table);   // (one expert needs no table: 0.7 us)
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   if (CG == 2) cluster_sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_slot;
-  const int tiles = table[c.E] * p.mtiles;   // (below 2^31: the host has looked; of a cluster that shares the axis one at most)
+  const int tiles = c.offsets ? table[c.E] * p.mtiles : static_cast<int>(p.tiles);   // (below 2^31: the host has looked; of a cluster that shares the axis one at most)
 
   if (warp == 0) {
     // ---- copies: one thread
@@ -205,18 +199,21 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
       const uint32_t lead = CG == 2 ? cluster_address(bars, 0) : bar0;   // the first CTA's barriers
       bool ok = true;
       for (int64_t t = team; ok && t < tiles; t += teams) {
-        const Tile tl = tile_of<CG>(p, table, static_cast<int>(t));
-        const int row0 = tl.lo + rank * (tl.n / CG), w0 = tl.e * c.O + (tl.m * CG + rank) * 128;
+        const Tile tl = tile_of<CG>(p, table, static_cast<int>(t), rank);
+        const int row0 = tl.lo + rank * (tl.n / CG), w0 = tl.e * c.O + tl.o0;
         for (int st = st0; st < st1; ++st, ++it, rp.advance(1, ring)) {
           if (!mbar_wait(done + 8 * rp.slot, rp.phase ^ 1, abort_flag, c.status)) { ok = false; break; }
           if (rank == 0) mbar_expect_tx(full + 8 * rp.slot, CG * stage_bytes);
-          const uint32_t dst = base + rp.slot * stage_bytes;
-          if (CG == 2) {
-            tma_pair_2d(dst, &wmap, st * kStage, w0, lead + 8 * rp.slot);
-            tma_pair_2d(dst + kWBytes, &xmap, st * kStage, row0, lead + 8 * rp.slot);
-          } else {
-            tma_load_2d(dst, &wmap, st * kStage, w0, full + 8 * rp.slot);
-            tma_load_2d(dst + kWBytes, &xmap, st * kStage, row0, full + 8 * rp.slot);
+          const uint32_t w = base + rp.slot * stage_bytes, x = w + p.KS * w_block;
+          for (int b = 0; b < p.KS; ++b) {
+            const int k = (st * p.KS + b) * kBlock;
+            if (CG == 2) {
+              tma_pair_2d(w + b * w_block, &wmap, k, w0, lead + 8 * rp.slot);
+              tma_pair_2d(x + b * x_block, &xmap, k, row0, lead + 8 * rp.slot);
+            } else {
+              tma_load_2d(w + b * w_block, &wmap, k, w0, full + 8 * rp.slot);
+              tma_load_2d(x + b * x_block, &xmap, k, row0, full + 8 * rp.slot);
+            }
           }
         }
       }
@@ -235,7 +232,7 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
       bool ok = true;
       for (int64_t t = team; ok && t < tiles; t += teams, ++n) {
         const uint32_t buf = n & 1, use = n >> 1;
-        const uint32_t idesc = idesc_i8(128 * CG, tile_of<CG>(p, table, static_cast<int>(t)).n);
+        const uint32_t idesc = idesc_i8(128 * CG, tile_of<CG>(p, table, static_cast<int>(t), rank).n);
         ok = CG == 2 ? mbar_wait<true>(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status) : mbar_wait(d_empty + 8 * buf, (use & 1) ^ 1, abort_flag, c.status);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -244,9 +241,11 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
           ok = mbar_wait(full + 8 * rp.slot, rp.phase, abort_flag, c.status);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t al = lo + rp.slot * (stage_bytes >> 4), xl = al + (kWBytes >> 4);
+          const uint32_t al = lo + rp.slot * (stage_bytes >> 4), xl = al + p.KS * (w_block >> 4);
+          for (int b = 0; b < p.KS; ++b) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) mma<CG>(d, hi | (al + 2u * k), hi | (xl + 2u * k), idesc, k > 0 || st > st0);
+            for (int k = 0; k < 4; ++k) mma<CG>(d, hi | (al + b * (w_block >> 4) + 2u * k), hi | (xl + b * (x_block >> 4) + 2u * k), idesc, k > 0 || b > 0 || st > st0);
+          }
           commit<CG>(done + 8 * rp.slot);
           ++issued;
         }
@@ -257,16 +256,15 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
     __syncwarp();   // (one thread may have been alone)
   } else if (p.split == 1) {
     // ---- drain
-    const int q = warp & 3, tid = (q << 5) | lane;   // this warp's 32 lanes of tensor memory
+    const int q = warp & 3, half = (warp - 2) >> 2;   // this warp's 32 lanes of tensor memory, and its turn
     const uint32_t from = tmem + (static_cast<uint32_t>(q * 32) << 16);
     const uint32_t lead_e = (CG == 2 ? cluster_address(bars, 0) : bar0) + (d_empty - bar0);
-    float* sx = reinterpret_cast<float*>(gen + p.off_sx) + q * acc_pitch;   // this warp's copy of the rows' scales
-    uint8_t* turn = gen + p.off_turn;
-    const int piece = tid & 15, r0 = tid >> 4;
-    uint32_t n = 0, chunk = 0;
+    float* sx = reinterpret_cast<float*>(gen + p.off_sx) + (4 * half + q) * acc_pitch;   // this warp's copy of the rows' scales
+    uint8_t* turn = gen + p.off_turn + (4 * half + q) * kTurnBytes;
+    uint32_t n = 0;
     for (int64_t t = team; t < tiles; t += teams, ++n) {
-      const Tile tl = tile_of<CG>(p, table, static_cast<int>(t));
-      const int o0 = (tl.m * CG + rank) * 128, count = tl.hi - tl.lo;
+      const Tile tl = tile_of<CG>(p, table, static_cast<int>(t), rank);
+      const int o0 = tl.o0, end = min(c.O, o0 + p.TM), count = tl.hi - tl.lo;
       const int64_t ch0 = static_cast<int64_t>(tl.e) * c.O;
       const uint32_t buf = n & 1, use = n >> 1;
       constexpr int kMine = H::kBytes == 4 ? 1 : 4;   // this thread's channels: 32 q + lane, or 32 q + lane / 4 + 8 h
@@ -274,42 +272,37 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
 #pragma unroll
       for (int h = 0; h < kMine; ++h) {
         const int o = o0 + 32 * q + (kMine == 1 ? lane : 8 * h + (lane >> 2));
-        sw[h] = o < c.O ? __ldcg(p.call.sw + ch0 + o) : 0.f;
-        bias[h] = c.bias && o < c.O ? H::load(c.bias, ch0 + o) : 0.f;
+        sw[h] = o < end ? __ldcg(p.call.sw + ch0 + o) : 0.f;
+        bias[h] = c.bias && o < end ? H::load(c.bias, ch0 + o) : 0.f;
       }
-      for (int i = lane; i < acc_pitch; i += 32) sx[i] = i < count ? __ldcg(p.call.sx + tl.lo + i) : 0.f;
+      for (int i = 32 * half + lane; i < acc_pitch; i += 64) sx[i] = i < count ? __ldcg(p.call.sx + tl.lo + i) : 0.f;
       __syncwarp();
-      const bool ok = mbar_wait<CG == 2, 64>(d_full + 8 * buf, use & 1, abort_flag, c.status);
-      if (!drain_agrees(ok)) break;
+      if (!__all_sync(0xffffffffu, mbar_wait<CG == 2, 64>(d_full + 8 * buf, use & 1, abort_flag, c.status))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      for (int n0 = 0; n0 < count; n0 += 32, ++chunk) {   // rows of y, 32 at a time
-        const bool last = n0 + 32 >= count;
-        auto free_accumulator = [&]() {   // the accumulator is read
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) arrive_lead(lead_e + 8 * buf);
-        };
+      for (int n0 = 32 * half; n0 < count; n0 += 64) {   // rows of y, 32 at a time
         if constexpr (H::kBytes == 4) {
           const int o = o0 + 32 * q + lane;
           float* y = static_cast<float*>(c.y) + (static_cast<int64_t>(tl.lo) + n0) * c.ldy + o;
+          int v[2][16];   // 16 rows each
+          tmem_ld16(from + buf * acc_pitch + n0, v[0]);
+          tmem_ld16(from + buf * acc_pitch + n0 + 16, v[1]);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {   // 16 rows each
-            int v[16];
-            tmem_ld16(from + buf * acc_pitch + n0 + 16 * g, v);
-            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-            if (g == 1 && last) free_accumulator();
+          for (int g = 0; g < 2; ++g) {
             float u[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) u[i] = scaled(v[i], sw[0], sx[n0 + 16 * g + i], bias[0]);
+            for (int i = 0; i < 16; ++i) u[i] = scaled(v[g][i], sw[0], sx[n0 + 16 * g + i], bias[0]);
             grp::quick_activation(u, c.act);
-            if (o < c.O) {
+            if (o < end) {
 #pragma unroll
               for (int i = 0; i < 16; ++i)
                 if (n0 + 16 * g + i < count) y[(16 * g + i) * c.ldy] = u[i];
             }
           }
         } else {
-          uint8_t* to = turn + (chunk & 1) * kTurnBytes;
+          int v[2][16];   // 16 channels each
+          tmem_ld_16x32(from + buf * acc_pitch + n0, v[0]);
+          tmem_ld_16x32(from + (16u << 16) + buf * acc_pitch + n0, v[1]);
           float sc[8];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -317,31 +310,26 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
             sc[2 * j] = two.x;
             sc[2 * j + 1] = two.y;
           }
+          __syncwarp();   // the turn of the rows before has been read
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          // 8 channels at a time: four blocks of 8 rows; a row is 64 bytes, its 16-byte pieces permuted by its number
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {   // 16 channels each
-            int v[16];
-            tmem_ld_16x32(from + (static_cast<uint32_t>(16 * g) << 16) + buf * acc_pitch + n0, v);
-            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-            if (g == 1 && last) free_accumulator();
+          for (int h = 0; h < 4; ++h) {
+            float u[8];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {   // 8 channels: four blocks of 8 rows; a row's 16-byte pieces lie permuted by its number
-              float u[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i) u[i] = scaled(v[4 * (i >> 1) + 2 * h + (i & 1)], sw[2 * g + h], sc[i], bias[2 * g + h]);
-              grp::quick_activation(u, c.act);
-              const int at = (4 * q + 2 * g + h) ^ (lane & 7);
-              turn_store(smem_u32(to) + lane * 256 + at * 16, H::pack(u[0], u[1]), H::pack(u[2], u[3]), H::pack(u[4], u[5]), H::pack(u[6], u[7]));
-            }
+            for (int i = 0; i < 8; ++i) u[i] = scaled(v[h >> 1][4 * (i >> 1) + 2 * (h & 1) + (i & 1)], sw[h], sc[i], bias[h]);
+            grp::quick_activation(u, c.act);
+            turn_store(smem_u32(turn) + lane * 64 + ((h ^ ((lane >> 1) & 3)) * 16), H::pack(u[0], u[1]), H::pack(u[2], u[3]), H::pack(u[4], u[5]), H::pack(u[6], u[7]));
           }
-          drain_sync();
-          const int col = o0 + 8 * piece;
+          __syncwarp();
+          const int piece = lane & 3, r0 = lane >> 2, col = o0 + 32 * q + 8 * piece;
           uint16_t* y = static_cast<uint16_t*>(c.y) + (static_cast<int64_t>(tl.lo) + n0 + r0) * c.ldy + col;
           uint4 w[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const uint4*>(to + (r0 + 8 * i) * 256 + ((piece ^ (r0 & 7)) * 16));
+          for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const uint4*>(turn + (r0 + 8 * i) * 64 + ((piece ^ ((r0 >> 1) & 3)) * 16));
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (n0 + r0 + 8 * i < count && col < c.O) {
+            if (n0 + r0 + 8 * i < count && col < end) {
               uint16_t* at = y + static_cast<int64_t>(8 * i) * c.ldy;
               if (p.wide_y && c.O - col >= 8) {
                 *reinterpret_cast<uint4*>(at) = w[i];
@@ -354,12 +342,16 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
             }
         }
       }
+      // the accumulator is read
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) arrive_lead(lead_e + 8 * buf);
     }
-  } else if (team < tiles) {
+  } else if (warp < 6 && team < tiles) {
     // ---- a split's sums go to shared memory (behind the last product nothing else lives there)
     const int q = warp & 3, row = 32 * q + lane;
     int32_t* sums = reinterpret_cast<int32_t*>(gen);   // [TN][128]
-    const Tile tl = tile_of<CG>(p, table, team);
+    const Tile tl = tile_of<CG>(p, table, team, rank);
     const bool ok = __all_sync(0xffffffffu, mbar_wait<false, 64>(d_full, 0, abort_flag, c.status)) != 0;
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     if (ok)
@@ -384,12 +376,11 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
     cluster_sync();
     if (team < tiles) {
       const int32_t* sums = reinterpret_cast<const int32_t*>(gen);
-      const Tile tl = tile_of<CG>(p, table, team);
-      const int o0 = tl.m * 128;
+      const Tile tl = tile_of<CG>(p, table, team, rank);
       const int64_t ch0 = static_cast<int64_t>(tl.e) * c.O;
       for (int i = crank * kThreads + threadIdx.x; i < (tl.hi - tl.lo) * 16; i += p.split * kThreads) {
-        const int r = i >> 4, col = o0 + (i & 15) * 8;
-        if (col >= c.O) continue;
+        const int r = i >> 4, col = tl.o0 + (i & 15) * 8;
+        if (col >= min(c.O, tl.o0 + p.TM)) continue;
         int acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
         for (int q = 0; q < 8; ++q)   // (all loads in flight at once)
@@ -429,7 +420,7 @@ static bool encode(CUtensorMap* map, const void* base, int64_t rows, int cols, i
   EncodeFn fn = encode_fn();
   if (!fn) return false;
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(pitch)};
-  const cuuint32_t box[2] = {kStage, static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
+  const cuuint32_t box[2] = {kBlock, static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -440,9 +431,8 @@ pipe_status linear_tc(const Call& call, cudaStream_t stream) {
   if (!plan_tc(TcShape{c.E, c.O, c.I, c.offsets != nullptr, c.N}, &p)) return PIPE_ERR_UNSUPPORTED;
   p.call = call;
   p.wide_y = !(reinterpret_cast<uintptr_t>(c.y) & 15) && c.ldy % (call.dtype == PIPE_DTYPE_FP32 ? 4 : 8) == 0;
-  p.ahead = 16;
   CUtensorMap wmap, xmap;
-  if (!encode(&wmap, call.w, static_cast<int64_t>(c.E) * c.O, c.I, call.ldw, 128) || !encode(&xmap, c.x, c.N, c.I, c.ldx, p.TN / p.cg)) return grp::runtime_failed();
+  if (!encode(&wmap, call.w, static_cast<int64_t>(c.E) * c.O, c.I, call.ldw, p.TM) || !encode(&xmap, c.x, c.N, c.I, c.ldx, p.TN / p.cg)) return grp::runtime_failed();
   void (*k)(TcArgs, CUtensorMap, CUtensorMap) =
       call.dtype == PIPE_DTYPE_FP32 ? tc_kernel<Fp32>(p.cg) : (call.dtype == PIPE_DTYPE_BF16 ? tc_kernel<Bf16>(p.cg) : tc_kernel<Fp16>(p.cg));
   if (!grp::allow_dynamic_smem(reinterpret_cast<const void*>(k), kMaxSmem)) return grp::runtime_failed();
