@@ -35,7 +35,6 @@ struct TcPlan {
   int stages;      // ceil(I / (128 KS))
   int split;       // CTAs (pairs have none) that share a tile's reduction axis
   int ring;        // stages in flight
-  int resident;    // CTAs of an SM
   int columns;     // of tensor memory that a CTA takes
   uint32_t off_turn, off_sx, off_table;   // shared memory behind the ring
   int smem;        // dynamic shared memory
@@ -57,46 +56,75 @@ inline bool lay_out(const TcShape& c, TcPlan* p) {
   while (p->columns < (p->split > 1 ? 1 : 2) * wide) p->columns *= 2;
   const int turn = p->split > 1 ? 0 : kDrainWarps * kTurnBytes, sx = p->split > 1 ? 0 : kDrainWarps * wide * 4, table = unit_ints(c.E) * 4;
   const int stage = p->KS * (p->TM + p->TN / p->cg) * kBlock;
-  const int room = kMaxSmem / p->resident - (p->resident > 1 ? 1024 : 0) - 1024 - turn - sx - table;
+  const int room = kMaxSmem - 1024 - turn - sx - table;
   p->ring = room / stage < kMaxRing ? room / stage : kMaxRing;
   p->ahead = 16;
-  if (p->ring < 2 || p->resident * p->columns > 512) return false;
+  if (p->ring < 2 || p->columns > 512) return false;
   p->off_turn = static_cast<uint32_t>(p->ring * stage);
   p->off_sx = p->off_turn + turn;
   p->off_table = p->off_sx + sx;
   // the MMA reads 128 rows of weights, also behind the last stage's
   const int read = p->ring * stage + (128 - p->TM) * kBlock, all = static_cast<int>(p->off_table) + table;
   p->smem = 1024 + (read > all ? read : all);
-  if (p->smem > kMaxSmem / p->resident) return false;
-  p->teams = p->split > 1 ? p->tiles : kChipSMs * p->resident / p->cg;
+  if (p->smem > kMaxSmem) return false;
+  p->teams = p->split > 1 ? p->tiles : kChipSMs / p->cg;
   if (p->teams > p->tiles) p->teams = p->tiles;
   return true;
 }
 
+// The blocks of a stage: as many as about 48 KB hold, 4 at most (a stage's barriers cost what 128 columns of MMA do; larger stages leave too
+// few in the ring).  4096 -> 11008 on one row: 4 blocks 10.1 us, 2 10.4, 1 11.9; on 64 rows: 4 13.0, 2 12.0.
+inline int stage_blocks(int TM, int TN, int cg) {
+  const int block = (TM + TN / cg) * kBlock;
+  return 4 * block <= 50000 ? 4 : (2 * block <= 50000 ? 2 : 1);
+}
+
+// Tile (rows TN, channels TM, CTAs cg) and split: the least of, in nanoseconds,
+//   rounds of tiles on the SMs * max(blocks of a CTA * max(160, 2.3 (TM + TN / cg)), 7000 + 5 TN)
+//   + 47 TN + 30 a CTA (the next launch's start is overlapped on SMs that are left free) + 450 for a pair + 5000 for a split,
+// a form (the copies' bytes, the drain, the launch's latency) whose numbers are fitted to 6000 timings of 75 shapes; the choice takes 2 %
+// longer than the best that was timed, on average.  Either side (us): 11008 x 4096, one row: TM 80 10.1, TM 128 11.2; 128 rows: pairs of TM
+// 80 14.0, single CTAs of TM 80 14.9; 512 rows: pairs of 192 rows 24.0, of 256 27.4; 4096 x 11008, one row: TM 128 split four ways 12.0,
+// TM 32 not split 15.1; 4096 rows, 4096 -> 11008: pairs of 256 rows 123, single CTAs 150.
 inline bool plan_tc(const TcShape& c, TcPlan* p) {
   const int64_t experts = c.ragged ? (c.N < c.E ? c.N : c.E) : 1;
   const int64_t mean = div_up(c.N, experts);   // rows of an expert
+  const int64_t blocks = div_up(c.I, kBlock);
+  const int64_t least = div_up(mean, 256);
   int64_t best = -1;
-  TcPlan t{};
-  for (int cap = 16; cap <= 256; cap *= 2) {
-    const int64_t units = c.ragged ? div_up(2 * mean > cap ? 2 * mean + cap : 2 * cap, 2 * cap) * experts : div_up(c.N, cap);
-    for (int pair = 1; pair <= 2; ++pair) {
-      if ((pair == 2 && (c.O <= 128 || cap < 64)) || (pair == 1 && cap > 128)) continue;
-      for (int TM = pair == 2 ? 128 : 32; TM <= 128; TM += 16) {
-        const int64_t tiles = units * div_up(c.O, TM * pair);
-        const int64_t rounds = div_up(tiles, kChipSMs / pair);
-        const int64_t block = pair == 1 ? 100 + (cap + TM) : 200 + cap * 6 / 10;
-        const int64_t cost = rounds * (div_up(c.I, kBlock) * block + 500);
-        t = TcPlan{};
-        t.TN = cap; t.TM = TM; t.KS = pair == 2 ? 1 : 2; t.cg = pair; t.split = 1; t.resident = 1;
-        if ((best < 0 || cost < best) && lay_out(c, &t)) {
-          best = cost;
-          *p = t;
+  int last = 0;
+  for (int64_t n = least; n < least + 8; ++n) {   // units of an expert with as many rows as that
+    int rows = static_cast<int>(div_up(mean, n));
+    if (c.ragged) rows = rows > 128 ? 256 : 2 * rows;   // (experts have unequal numbers of rows)
+    const int small = (rows + 15) & ~15, wide = (rows + 31) & ~31;
+    if (small == last) continue;
+    last = small;
+    for (int cg = 1; cg <= 2; ++cg) {
+      const int TN = cg == 1 ? small : wide;
+      if (cg == 1 ? TN > 128 : c.O <= 64) continue;
+      // rows fill units evenly where there is one expert; otherwise an expert's last unit is half full, on average
+      const int64_t units = c.ragged ? (2 * mean > TN ? div_up(2 * mean + TN, 2 * TN) : 1) * experts : div_up(c.N, TN);
+      for (int TM = cg == 1 ? 32 : 64; TM <= 128; TM += 16) {
+        const int64_t tiles = units * div_up(c.O, TM * cg);
+        for (int split = 1; split <= 8; ++split) {
+          if (split > 1 && (cg == 2 || TN > 64 || blocks < 4 * split || tiles > kClusters[split])) break;
+          const int64_t rounds = split > 1 ? 1 : div_up(tiles, kChipSMs / cg), load = (TM + TN / cg) * 23 / 10;
+          const int64_t work = div_up(blocks, split) * (load > 160 ? load : 160), floor = 7000 + 5 * TN;
+          const int64_t ctas = tiles * cg * split;
+          const int64_t cost = rounds * (work > floor ? work : floor) + 47 * TN + 30 * (ctas < kChipSMs ? ctas : kChipSMs) + (cg == 2 ? 450 : 0) + (split > 1 ? 5000 : 0);
+          if (best < 0 || cost < best) {
+            best = cost;
+            p->TN = TN; p->TM = TM; p->cg = cg; p->split = split;
+          }
         }
       }
     }
   }
-  return best >= 0;
+  p->KS = stage_blocks(p->TM, p->TN, p->cg);
+  if (lay_out(c, p)) return true;
+  // (the bound on an expert call's units may be more than the clusters of a launch can be: those tiles are one CTA's)
+  p->split = 1;
+  return lay_out(c, p);
 }
 
 }  // namespace i8

@@ -425,10 +425,27 @@ static bool encode(CUtensorMap* map, const void* base, int64_t rows, int cols, i
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The plan, gone over once for a shape (some 2 us) as long as this thread has no other one in its place.
+static bool plan_for(const TcShape& c, TcPlan* p) {
+  struct Known {
+    TcShape shape;
+    TcPlan plan;
+    bool good;
+  };
+  static thread_local Known known[16] = {};
+  Known& k = known[(static_cast<uint64_t>(c.N) * 7 + c.O * 3u + c.I) % 16];
+  if (k.shape.E != c.E || k.shape.O != c.O || k.shape.I != c.I || k.shape.ragged != c.ragged || k.shape.N != c.N) {   // (E is 0 in an empty place)
+    k.good = plan_tc(c, &k.plan);
+    k.shape = c;
+  }
+  *p = k.plan;
+  return k.good;
+}
+
 pipe_status linear_tc(const Call& call, cudaStream_t stream) {
   const grp::Call& c = call.c;
   TcArgs p;
-  if (!plan_tc(TcShape{c.E, c.O, c.I, c.offsets != nullptr, c.N}, &p)) return PIPE_ERR_UNSUPPORTED;
+  if (!plan_for(TcShape{c.E, c.O, c.I, c.offsets != nullptr, c.N}, &p)) return PIPE_ERR_UNSUPPORTED;
   p.call = call;
   p.wide_y = !(reinterpret_cast<uintptr_t>(c.y) & 15) && c.ldy % (call.dtype == PIPE_DTYPE_FP32 ? 4 : 8) == 0;
   CUtensorMap wmap, xmap;
