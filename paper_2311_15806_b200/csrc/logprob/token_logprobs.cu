@@ -1,16 +1,26 @@
-// Log probabilities of given tokens, entropy and top alternatives (definition: pipe_token_logprobs in include/pipe.h), the simplest form:
-// a block per row that reads it once for the largest logit, once for the sums and once for every alternative.
+// Log probabilities of given tokens, entropy and top alternatives (definition: pipe_token_logprobs in include/pipe.h).
+//
+// One pass over the logits: a thread keeps the largest logit it has met, m, and under it the sums of exp(z - z_m) and of
+// (l - m) exp(z - z_m), scaled anew when m grows; threads, warps and the CTAs of a row's cluster are joined likewise.  Bound by HBM, closely
+// followed by the exponentials (one a logit) and the issue slots.
+// The alternatives cost no work in that pass: the k-th largest of the threads' own largest logits is not above the row's k-th
+// largest, so only threads with one at least as large can hold an alternative, some k of them, and their logits alone are looked at
+// again, a warp at a time, in L2.  What is found (some more than k) is ranked by counting.  Where too many are found, as among equal
+// logits, the k-th largest logit is settled by halving and the first of those equal to it are taken in the row's order.
 #include "../group/group_common.cuh"
 
 namespace pipe {
 namespace lpb {
 
-constexpr int kThreads = 256;
-constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
+constexpr float kLog2e = 1.44269504f;
+constexpr float kFar = -1e30f;     // differences below have probability 0 at every scale (2^-20 at least)
+constexpr int kFound = 512;        // most logits that are ranked: no less than a cluster's PIPE_MAX_TOP each
+constexpr int kCluster = 8;
+static_assert(kFound >= kCluster * PIPE_MAX_TOP, "");
 
 struct Args {
   const void* logits;
-  int64_t T, ldl;
+  int64_t ldl;
   int V;
   float scale;
   const int32_t* tokens;
@@ -23,85 +33,449 @@ struct Args {
   int* status;
 };
 
-template <int SRC>
-__device__ __forceinline__ float logit(const void* row, int64_t i) {
-  if (SRC == PIPE_DTYPE_FP32) return __ldcg(static_cast<const float*>(row) + i);
-  const uint16_t h = __ldcg(static_cast<const uint16_t*>(row) + i);
-  return SRC == PIPE_DTYPE_BF16 ? grp::Bf16::to_float(h) : grp::Fp16::to_float(h);
-}
-// Keys that order like the numbers, -0 and 0 alike.
+// Keys that order like the numbers, -0 and 0 alike (adding 0 makes them one).
 __device__ __forceinline__ uint32_t key_of(float v) {
   const uint32_t u = __float_as_uint(v + 0.f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float number_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
+constexpr uint32_t kNoneKey = 0x007FFFFFu;   // of -Inf
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 
+// 16 bytes of logits.
 template <int SRC>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(const Args a) {
-  __shared__ unsigned long long best_s;
-  __shared__ float red[2][kThreads / 32];
-  __shared__ int bad_s;
+struct Vec {
+  static constexpr int kLogits = SRC == PIPE_DTYPE_FP32 ? 4 : 8, kSize = SRC == PIPE_DTYPE_FP32 ? 4 : 2;
+  uint32_t u[4];
+  __device__ __forceinline__ void load(const uint8_t* p) {
+    const uint4 a = __ldcg(reinterpret_cast<const uint4*>(p));
+    u[0] = a.x; u[1] = a.y; u[2] = a.z; u[3] = a.w;
+  }
+  __device__ __forceinline__ void fill() {   // -Inf: not there
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = SRC == PIPE_DTYPE_FP32 ? 0xFF800000u : (SRC == PIPE_DTYPE_BF16 ? 0xFF80FF80u : 0xFC00FC00u);
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (SRC == PIPE_DTYPE_FP32) return __uint_as_float(u[i]);
+    else if constexpr (SRC == PIPE_DTYPE_BF16) return __uint_as_float(i & 1 ? u[i >> 1] & 0xFFFF0000u : u[i >> 1] << 16);
+    else return grp::Fp16::to_float(static_cast<uint16_t>(i & 1 ? u[i >> 1] >> 16 : u[i >> 1]));
+  }
+  // the largest of these, a NaN if there is one
+  static __device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    if constexpr (SRC == PIPE_DTYPE_BF16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+  }
+  template <int N>
+  static __device__ __forceinline__ float largest(const Vec (&v)[N]) {
+    if constexpr (SRC == PIPE_DTYPE_FP32) {
+      float m = v[0].at(0);
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i + j) m = max_nan(m, v[j].at(i));
+      return m;
+    } else {
+      uint32_t m = v[0].u[0];
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i + j) m = larger2(m, v[j].u[i]);
+      Vec one;
+      one.u[0] = m;
+      return max_nan(one.at(0), one.at(1));
+    }
+  }
+};
+template <int SRC>
+__device__ __forceinline__ float logit(const uint8_t* row, int64_t i) {
+  if constexpr (SRC == PIPE_DTYPE_FP32) return __ldcg(reinterpret_cast<const float*>(row) + i);
+  const uint16_t h = __ldcg(reinterpret_cast<const uint16_t*>(row) + i);
+  return SRC == PIPE_DTYPE_BF16 ? grp::Bf16::to_float(h) : grp::Fp16::to_float(h);
+}
+
+// The sums over some logits: m the largest (-Inf: none; a NaN or +Inf: no distribution), s = sum exp(scale (l - m)), h = sum (l - m)
+// exp(scale (l - m)).
+struct Sums {
+  float m, s, h;
+};
+// Those of N neighbouring lanes joined, the same in all of them (c: scale log2 e).
+template <int N>
+__device__ __forceinline__ Sums joined(const Sums& own, float c) {
+  Sums r = own;
+#pragma unroll
+  for (int o = N / 2; o; o >>= 1) r.m = max_nan(r.m, __shfl_xor_sync(0xffffffffu, r.m, o));
+  const float d = fmaxf(own.m - fmaxf(r.m, -3.402823466e38f), kFar), f = ex2(d * c);
+  r.s = own.s * f;
+  r.h = (own.h + own.s * d) * f;
+#pragma unroll
+  for (int o = N / 2; o; o >>= 1) {
+    r.s += __shfl_xor_sync(0xffffffffu, r.s, o);
+    r.h += __shfl_xor_sync(0xffffffffu, r.h, o);
+  }
+  return r;
+}
+
+// What of a row this CTA reads: `head` logits before the first 16-byte boundary (the first CTA's), vectors first .. end - 1 of those that
+// begin there, and `tail` logits behind the last (the last CTA's).  Thread t has vectors first + t, first + t + B, .. and the t-th logit
+// of head and tail.
+struct Part {
+  const uint8_t* row;
+  const uint8_t* vectors;
+  int head, tail, first, end, tail_at, head_all;
+};
+
+// A logit and its place as one number, larger for what is listed first: the key above, the place's complement below.  0: none.
+using Entry = unsigned long long;
+__device__ __forceinline__ Entry entry_of(float l, int i) { return (static_cast<Entry>(key_of(l)) << 32) | (0xFFFFFFFFu - static_cast<uint32_t>(i)); }
+__device__ __forceinline__ uint32_t key_in(Entry e) { return static_cast<uint32_t>(e >> 32); }
+__device__ __forceinline__ int place_in(Entry e) { return static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(e)); }
+
+constexpr int kGroups = 256;
+
+// Shared memory of the search for the alternatives.
+template <int B>
+struct Search {
+  alignas(16) Entry entry[kFound + 2];
+  uint32_t group[kGroups];               // the largest logits of groups of threads, as keys
+  int found;
+  uint32_t least;
+  int run[2][B / 32];
+};
+
+// f(logit, index) for the logits of this CTA's part that are not below `least` (of the key of a number), of threads whose largest, `own`,
+// is not.  Whole warps look at a thread's vectors, those of four threads at a time.
+template <int SRC, int B, class F>
+__device__ __forceinline__ void look_again(const Part& p, uint32_t own, uint32_t least, F f) {
+  constexpr int kLogits = Vec<SRC>::kLogits;
+  const int lane = threadIdx.x & 31;
+  const float bound = number_of(least);
+  uint32_t which = __ballot_sync(0xffffffffu, own >= least);
+  while (which) {
+    int t[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      t[j] = which ? static_cast<int>(threadIdx.x & ~31u) + __ffs(which) - 1 : -1;
+      which &= which - 1;
+    }
+    for (int v0 = p.first + lane * B; v0 < p.end; v0 += 32 * B) {
+      Vec<SRC> w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (t[j] >= 0 && v0 + t[j] < p.end) w[j].load(p.vectors + (v0 + t[j]) * int64_t{16});
+        else w[j].fill();
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const Vec<SRC> one[1] = {w[j]};
+        if (Vec<SRC>::largest(one) >= bound) {
+#pragma unroll
+          for (int i = 0; i < kLogits; ++i)
+            if (w[j].at(i) >= bound) f(w[j].at(i), p.head_all + (v0 + t[j]) * kLogits + i);
+        }
+      }
+    }
+    if (lane < 8) {   // their logits of head and tail
+      const int j = lane & 3, u = j & 2 ? (j & 1 ? t[3] : t[2]) : (j & 1 ? t[1] : t[0]), at = lane & 4 ? p.tail_at + u : u;
+      if (u >= 0 && u < (lane & 4 ? p.tail : p.head)) {
+        const float l = logit<SRC>(p.row, at);
+        if (l >= bound) f(l, at);
+      }
+    }
+  }
+}
+
+// The `count` entries ranked: out[i], i < k, with zeros where there are none.
+template <int B>
+__device__ __forceinline__ void rank(Search<B>& s, int count, int k, Entry* out) {
+  for (int i = threadIdx.x; i < k; i += B) out[i] = 0;
+  if (threadIdx.x == 0) s.entry[count] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < count; i += B) {
+    const Entry e = s.entry[i];
+    int above = 0;
+#pragma unroll 4
+    for (int j = 0; j < count; j += 2) {
+      const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(s.entry + j);
+      above += (two.x > e) + (two.y > e);
+    }
+    if (e != 0 && above < k) out[above] = e;
+  }
+}
+
+// Fills s.entry with logits of this CTA's part, in any order, the k first of them among these or all that there are; returns their number,
+// kFound at most.  m: the largest of this thread's.
+template <int SRC, int B>
+__device__ int search(Search<B>& s, const Part& p, float m, int k) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t own = key_of(m);
+  if (threadIdx.x == 0) s.found = 0;
+  // A bound for the k-th largest: of disjoint groups of threads at least k have one as large, by halving until those are few enough (or down
+  // to kNoneKey + 1, the least that is not masked, where there are fewer than k).
+  int size = 1;
+  uint32_t most = own;
+  if (B > kGroups) {
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    size = 2;
+    if (k <= 32) {
+      most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      size = 4;
+    }
+  }
+  for (int i = threadIdx.x; i < kGroups; i += B)
+    if (i >= B / size) s.group[i] = 0;
+  if (threadIdx.x % size == 0) s.group[threadIdx.x / size] = most;
+  __syncthreads();
+  if (warp == 0) {
+    uint32_t mine[kGroups / 32], lo = kNoneKey + 1, hi = 0;
+#pragma unroll
+    for (int i = 0; i < kGroups / 32; ++i) {
+      mine[i] = s.group[32 * i + lane];
+      hi = max(hi, mine[i]);
+    }
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    int n = B;
+    while (lo < hi && n > k + (k >> 1) + 4) {
+      const uint32_t mid = lo + (hi - lo + 1) / 2;
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < kGroups / 32; ++i) c += mine[i] >= mid;
+      c = __reduce_add_sync(0xffffffffu, c);
+      if (c >= k) {
+        lo = mid;
+        n = c;
+      } else {
+        hi = mid - 1;
+      }
+    }
+    if (lane == 0) s.least = lo;
+  }
+  __syncthreads();
+  uint32_t least = s.least;
+  look_again<SRC, B>(p, own, least, [&](float l, int i) {
+    const int at = atomicAdd(&s.found, 1);
+    if (at < kFound) s.entry[at] = entry_of(l, i);
+  });
+  __syncthreads();
+  if (s.found <= kFound) return s.found;
+
+  // Too many.  The key of the k-th largest, by halving between that bound and the largest.
+  uint32_t hi = 0;
+  for (int g = lane; g < kGroups; g += 32) hi = max(hi, s.group[g]);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  for (int turn = 0; least < hi; turn ^= 1) {   // (the same in all threads; at least k logits reach `least`)
+    const uint32_t mid = least + (hi - least + 1) / 2;
+    int c = 0;
+    look_again<SRC, B>(p, own, mid, [&](float, int) { ++c; });
+    c = __reduce_add_sync(0xffffffffu, c);
+    if (lane == 0) s.run[turn][warp] = c;
+    __syncthreads();
+    c = 0;
+#pragma unroll
+    for (int w = 0; w < B / 32; ++w) c += s.run[turn][w];
+    if (c >= k) least = mid;
+    else hi = mid - 1;
+  }
+  // Those above it, fewer than k, in any order; then the first that are equal to it, in the row's order.
+  __syncthreads();
+  if (threadIdx.x == 0) s.found = 0;
+  __syncthreads();
+  look_again<SRC, B>(p, own, least, [&](float l, int i) {
+    if (key_of(l) > least) s.entry[atomicAdd(&s.found, 1)] = entry_of(l, i);
+  });
+  __syncthreads();
+  int have = s.found;
+  constexpr int kLogits = Vec<SRC>::kLogits;
+  const float bound = number_of(least);
+  const int steps = (p.end - p.first + B - 1) / B;   // of the block through its vectors; the head before, the tail behind
+  for (int st = -1; st <= steps && have < k; ++st) {
+    uint32_t equal = 0;
+    int base = 0;
+    if (st < 0 || st == steps) {
+      base = st < 0 ? static_cast<int>(threadIdx.x) : p.tail_at + static_cast<int>(threadIdx.x);
+      if (static_cast<int>(threadIdx.x) < (st < 0 ? p.head : p.tail)) equal = logit<SRC>(p.row, base) == bound;
+    } else {
+      const int v = p.first + st * B + static_cast<int>(threadIdx.x);
+      base = p.head_all + v * kLogits;
+      if (v < p.end) {
+        Vec<SRC> w;
+        w.load(p.vectors + v * int64_t{16});
+#pragma unroll
+        for (int i = 0; i < kLogits; ++i) equal |= static_cast<uint32_t>(w.at(i) == bound) << i;
+      }
+    }
+    int upto = __popc(equal);
+    const int mine = upto;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += v;
+    }
+    if (lane == 31) s.run[0][warp] = upto;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < B / 32; ++w) {
+      if (w < warp) before += s.run[0][w];
+      all += s.run[0][w];
+    }
+    int at = have + before + upto - mine;
+    for (; equal && at < k; equal &= equal - 1, ++at) s.entry[at] = entry_of(bound, base + __ffs(equal) - 1);
+    have = min(have + all, k);
+    __syncthreads();
+  }
+  return have;
+}
+
+// B threads a CTA; a cluster of CTAs a row.  ENT: the entropy is wanted.
+template <int SRC, int B, bool ENT>
+__global__ void __launch_bounds__(B, 1536 / B) logprobs_kernel(const Args a) {
+  constexpr int kLogits = Vec<SRC>::kLogits, kSize = Vec<SRC>::kSize, kAhead = 4;
+  __shared__ Search<B> search_s;
+  __shared__ Sums warp_s[B / 32];
+  __shared__ Sums own_s;                     // this CTA's
+  __shared__ Entry top_s[PIPE_MAX_TOP];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int ctas = grp::cluster_ctas(), crank = grp::cluster_rank();
+  const int64_t t = blockIdx.x / ctas;
+  Part p;
+  p.row = static_cast<const uint8_t*>(a.logits) + t * a.ldl * kSize;
+  p.head_all = min(a.V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(p.row) & 15)) & 15) / kSize);
+  p.vectors = p.row + p.head_all * kSize;
+  const int all = (a.V - p.head_all) / kLogits;
+  p.first = static_cast<int>(static_cast<int64_t>(all) * crank / ctas);
+  p.end = static_cast<int>(static_cast<int64_t>(all) * (crank + 1) / ctas);
+  p.head = crank == 0 ? p.head_all : 0;
+  p.tail_at = p.head_all + all * kLogits;
+  p.tail = crank == ctas - 1 ? a.V - p.tail_at : 0;
+  const float c = a.scale * kLog2e;
   grid_wait();
   grid_release();
-  const int64_t t = blockIdx.x;
-  const void* row = static_cast<const uint8_t*>(a.logits) + t * a.ldl * (SRC == PIPE_DTYPE_FP32 ? 4 : 2);
-  if (threadIdx.x == 0) bad_s = 0, best_s = 0;
-  __syncthreads();
-  float m = -INFINITY;
-  bool bad = false;
-  for (int i = threadIdx.x; i < a.V; i += kThreads) {
-    const float l = logit<SRC>(row, i);
-    if (!(l <= 3.402823466e38f)) bad = true;
-    m = fmaxf(m, l);
-  }
-  if (bad) bad_s = 1;
-  m = number_of(__reduce_max_sync(0xffffffffu, key_of(m)));
-  if ((threadIdx.x & 31) == 0) red[0][threadIdx.x >> 5] = m;
-  __syncthreads();
-  for (int w = 0; w < kThreads / 32; ++w) m = fmaxf(m, red[0][w]);
-  bad = bad_s != 0;
-  const bool none = m == -INFINITY;
-  if (bad && threadIdx.x == 0) raise_status(a.status, PIPE_ERR_NONFINITE);
-  const float c = a.scale * kLog2e;
-  float s = 0.f, h = 0.f;
-  for (int i = threadIdx.x; i < a.V; i += kThreads) {
-    const float d = fmaxf(logit<SRC>(row, i) - m, -1e30f), e = exp2f(d * c);
-    s += e;
-    h += d * e;
-  }
-  __syncthreads();
-  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o), h += __shfl_xor_sync(0xffffffffu, h, o);
-  if ((threadIdx.x & 31) == 0) red[0][threadIdx.x >> 5] = s, red[1][threadIdx.x >> 5] = h;
-  __syncthreads();
-  s = h = 0.f;
-  for (int w = 0; w < kThreads / 32; ++w) s += red[0][w], h += red[1][w];
-  const float logs = logf(s), nan = __int_as_float(0x7FC00000);
-  auto logprob = [&](float l) { return bad ? nan : (none || l == -INFINITY ? -INFINITY : (0.5f * l - 0.5f * m) * a.scale * 2.f - logs); };
-  for (int j = threadIdx.x; j < a.n; j += kThreads) {
-    const int tok = __ldcg(a.tokens + t * a.n + j);
-    a.logprobs[t * a.n + j] = tok >= 0 && tok < a.V ? logprob(logit<SRC>(row, tok)) : 0.f;
-  }
-  if (a.entropy && threadIdx.x == 0) a.entropy[t] = bad ? nan : (none ? 0.f : logs - a.scale * h / s);
-  unsigned long long last = ~0ull;
-  for (int j = 0; j < a.k; ++j) {
-    unsigned long long best = 0;
-    for (int i = threadIdx.x; i < a.V; i += kThreads) {
-      const float l = logit<SRC>(row, i);
-      const unsigned long long k = (static_cast<unsigned long long>(key_of(l)) << 32) | (0xFFFFFFFFu - i);
-      if (l != -INFINITY && k < last && k > best) best = k;
+
+  Sums own = {-INFINITY, 0.f, 0.f};
+  f32x2 s2 = both_f2(0.f), h2 = both_f2(0.f);
+  auto grow = [&](float m) {   // a new largest logit
+    const float base = fmaxf(m, -3.402823466e38f), d = fmaxf(own.m - base, kFar), f = ex2(d * c);
+    if (ENT) h2 = mul_f2(fma_f2(s2, both_f2(d), h2), both_f2(f));
+    s2 = mul_f2(s2, both_f2(f));
+    own.m = m;
+  };
+  for (int v0 = p.first + static_cast<int>(threadIdx.x); v0 < p.end; v0 += kAhead * B) {   // (at most 2^28 vectors)
+    Vec<SRC> v[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (v0 + j * B < p.end) v[j].load(p.vectors + (v0 + j * B) * int64_t{16});
+      else v[j].fill();
     }
-    atomicMax(&best_s, best);
-    __syncthreads();
-    last = best_s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      best_s = 0;
-      const bool some = last != 0 && !bad;
-      if (a.top) a.top[t * a.k + j] = some ? static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(last)) : -1;
-      if (a.top_logprobs) a.top_logprobs[t * a.k + j] = some ? logprob(number_of(static_cast<uint32_t>(last >> 32))) : (bad ? nan : -INFINITY);
-    }
-    __syncthreads();
+    const float m = max_nan(own.m, Vec<SRC>::largest(v));
+    if (!(m <= own.m)) grow(m);
+    const f32x2 minus = both_f2(-fmaxf(own.m, -3.402823466e38f)), c2 = both_f2(c);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+      for (int i = 0; i < kLogits; i += 2) {
+        f32x2 d = add_f2(pack_f2(v[j].at(i), v[j].at(i + 1)), minus);
+        float d0, d1;
+        if (ENT) {   // (an infinite difference times its exponential would be no number)
+          unpack_f2(d, d0, d1);
+          d = pack_f2(fmaxf(d0, kFar), fmaxf(d1, kFar));
+        }
+        unpack_f2(mul_f2(d, c2), d0, d1);
+        const f32x2 e = pack_f2(ex2(d0), ex2(d1));
+        s2 = add_f2(s2, e);
+        if (ENT) h2 = fma_f2(d, e, h2);
+      }
   }
+#pragma unroll
+  for (int which = 0; which < 2; ++which)
+    if (static_cast<int>(threadIdx.x) < (which ? p.tail : p.head)) {
+      const float l = logit<SRC>(p.row, (which ? p.tail_at : 0) + static_cast<int>(threadIdx.x)), m = max_nan(own.m, l);
+      if (!(m <= own.m)) grow(m);
+      const float d = fmaxf(l - fmaxf(own.m, -3.402823466e38f), kFar), e = ex2(d * c);
+      s2 = add_f2(s2, pack_f2(e, 0.f));
+      h2 = fma_f2(both_f2(d), pack_f2(e, 0.f), h2);
+    }
+  const float mine = own.m;
+  {
+    float x, y;
+    unpack_f2(s2, x, y);
+    own.s = x + y;
+    unpack_f2(h2, x, y);
+    own.h = x + y;
+  }
+  own = joined<32>(own, c);
+  if (lane == 0) warp_s[warp] = own;
+  __syncthreads();
+  own = joined<B / 32>(warp_s[lane & (B / 32 - 1)], c);   // (in every lane)
+  if (threadIdx.x == 0) own_s = own;
+  if (a.k > 0) {
+    // (a row that is no distribution has no alternatives, in whichever CTA that shows)
+    const int count = own.m <= 3.402823466e38f ? search<SRC, B>(search_s, p, mine, a.k) : 0;
+    __syncthreads();
+    rank<B>(search_s, count, a.k, top_s);
+  }
+  if (ctas > 1) {
+    grp::cluster_sync();
+    if (crank == 0) {
+      Sums others = {-INFINITY, 0.f, 0.f};
+      const int from = lane & (kCluster - 1);
+      if (from < ctas) others = Sums{grp::cluster_load(&own_s.m, from), grp::cluster_load(&own_s.s, from), grp::cluster_load(&own_s.h, from)};
+      own = joined<kCluster>(others, c);
+      for (int i = threadIdx.x; i < ctas * a.k; i += B) {
+        const int from = i / a.k;
+        asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(search_s.entry[i]) : "r"(grp::cluster_address(top_s + (i - from * a.k), from)) : "memory");
+      }
+    }
+    grp::cluster_sync();   // (no CTA leaves, and none ranks anew, while another one's memory is read)
+    if (crank != 0) return;
+    if (a.k > 0) rank<B>(search_s, ctas * a.k, a.k, top_s);
+  }
+  const bool bad = !(own.m <= 3.402823466e38f), none = own.m == -INFINITY;
+  const float logs = logf(own.s), nan = __int_as_float(0x7FC00000);
+  // (halves: the difference of two logits may be beyond the type's range where its product with the scale is not)
+  auto logprob = [&](float l) { return bad ? nan : (none || l == -INFINITY ? -INFINITY : (0.5f * l - 0.5f * own.m) * a.scale * 2.f - logs); };
+  if (threadIdx.x == 0) {
+    if (bad) raise_status(a.status, PIPE_ERR_NONFINITE);
+    if (ENT) a.entropy[t] = bad ? nan : (none ? 0.f : logs - a.scale * own.h / own.s);
+  }
+  for (int j = threadIdx.x; j < a.n; j += B) {
+    const int token = __ldcg(a.tokens + t * a.n + j);
+    a.logprobs[t * a.n + j] = token >= 0 && token < a.V ? logprob(logit<SRC>(p.row, token)) : 0.f;
+  }
+  if (a.k > 0) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.k; i += B) {
+      const Entry e = top_s[i];
+      if (a.top) a.top[t * a.k + i] = bad || e == 0 ? -1 : place_in(e);
+      if (a.top_logprobs) a.top_logprobs[t * a.k + i] = bad ? nan : (e == 0 ? -INFINITY : logprob(number_of(key_in(e))));
+    }
+  }
+}
+
+using Kernel = void (*)(Args);
+template <int SRC>
+static Kernel logprobs_of(bool wide, bool entropy) {
+  if (wide) return entropy ? logprobs_kernel<SRC, 512, true> : logprobs_kernel<SRC, 512, false>;
+  return entropy ? logprobs_kernel<SRC, 128, true> : logprobs_kernel<SRC, 128, false>;
+}
+
+// Threads of a CTA and CTAs of a row.
+static void choose(int64_t T, int V, int size, int* threads, int* ctas) {
+  const int64_t bytes = static_cast<int64_t>(V) * size;
+  *threads = bytes <= 32768 ? 128 : 512;
+  *ctas = 1;
+  while (*ctas < kCluster && bytes / *ctas > 16384 && T * *ctas * 2 <= 3 * kPlanSMs) *ctas *= 2;
 }
 
 }  // namespace lpb
@@ -125,12 +499,16 @@ extern "C" pipe_status pipe_token_logprobs(const void* d_logits, int32_t dtype, 
       misaligned(d_top, 4) || misaligned(d_top_logprobs, 4))
     return PIPE_ERR_ALIGNMENT;
   if (T == 0) return PIPE_OK;
-  lpb::Args a = {d_logits, T, ldl, V, scale, d_tokens, n, d_logprobs, d_entropy, k, d_top, d_top_logprobs, device_status_word()};
+  lpb::Args a = {d_logits, ldl, V, scale, d_tokens, n, d_logprobs, d_entropy, k, d_top, d_top_logprobs, device_status_word()};
   if (!a.status) return grp::runtime_failed();
-  const auto kern = dtype == PIPE_DTYPE_FP32 ? lpb::logprobs_kernel<PIPE_DTYPE_FP32>
-                                             : (dtype == PIPE_DTYPE_BF16 ? lpb::logprobs_kernel<PIPE_DTYPE_BF16> : lpb::logprobs_kernel<PIPE_DTYPE_FP16>);
+  int threads, ctas;
+  lpb::choose(T, V, dtype == PIPE_DTYPE_FP32 ? 4 : 2, &threads, &ctas);
+  const bool wide = threads == 512;
+  const lpb::Kernel kern = dtype == PIPE_DTYPE_FP32 ? lpb::logprobs_of<PIPE_DTYPE_FP32>(wide, d_entropy != nullptr)
+                                                    : (dtype == PIPE_DTYPE_BF16 ? lpb::logprobs_of<PIPE_DTYPE_BF16>(wide, d_entropy != nullptr)
+                                                                                : lpb::logprobs_of<PIPE_DTYPE_FP16>(wide, d_entropy != nullptr));
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (launch_overlapped(kern, dim3(static_cast<unsigned>(T)), lpb::kThreads, 1, true, s, a) != cudaSuccess) return grp::runtime_failed();
+  if (launch_overlapped(kern, dim3(static_cast<unsigned>(T * ctas)), threads, ctas, true, s, a) != cudaSuccess) return grp::runtime_failed();
   count_launch(1);
   take_expansion_mark(s);
   return launch_status();
