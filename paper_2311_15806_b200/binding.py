@@ -652,49 +652,70 @@ def make_int8_desc(O: int, I: int, dtype=torch.bfloat16, experts: int = 1) -> In
 def _pitch_of(where: str, t: torch.Tensor, cols: int) -> int:
     """Row pitch of a [.., cols] array, [rows, cols] with leading dimensions joined, whose rows are contiguous and at one distance."""
     shape, stride = t.shape, t.stride()
-    if len(shape) == 2 and shape[1] == cols and (stride[1] == 1 or cols <= 1):
-        return stride[0] if shape[0] > 1 else max(cols + 15 & ~15, stride[0] & ~15)
-    if len(shape) == 3 and shape[2] == cols and (stride[2] == 1 or cols <= 1) and (shape[0] <= 1 or shape[1] <= 1 or stride[0] == shape[1] * stride[1]):
+    if len(shape) == 2:
+        if shape[1] == cols and (stride[1] == 1 or cols <= 1):
+            return stride[0] if shape[0] > 1 else max(cols + 15 & ~15, stride[0] & ~15)
+    elif len(shape) == 3 and shape[2] == cols and (stride[2] == 1 or cols <= 1) and (shape[0] <= 1 or shape[1] <= 1 or stride[0] == shape[1] * stride[1]):
         if shape[0] * shape[1] > 1:
             return stride[1] if shape[1] > 1 else stride[0]
         return max(cols + 15 & ~15, stride[1] & ~15)
     raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: an array of shape {tuple(shape)} and strides {stride}, rows of {cols} at one distance are needed")
 
 
+_i8, _i32, _f32 = torch.int8, torch.int32, torch.float32
+
+
+# (What follows is written for few calls into torch: each takes some 0.1 us, a call of the library 4.)
 def pipe_int8_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, rows: torch.Tensor | None = None,
                        count: torch.Tensor | None = None, values: torch.Tensor | None = None, stream=None) -> None:
     """x: cuda float32 / bfloat16 / float16 [T, I] (weights also [E, O, I]); codes: int8 [N, I] (or x's shape); scales: float32, N of
     them; rows: int32 [N] or None (N = T); count: one int32 or None; values: float32 of codes' shape or None."""
     where = "pipe_int8_quantize"
-    I = x.shape[-1] if x.dim() else 0
-    _wants(where, codes.dtype == torch.int8 and scales.dtype == torch.float32 and x.dtype in _DTYPES, "types")
-    ldx, ldc, ldv = _pitch_of(where, x, I), _pitch_of(where, codes, I), 0
-    N = scales.numel()
-    _wants(where, scales.is_contiguous() and N == codes.shape[:-1].numel(), "a scale for every row of codes")
-    _wants(where, rows is None or (rows.dtype == torch.int32 and rows.numel() == N and rows.is_contiguous()), "rows")
-    _wants(where, count is None or (count.dtype == torch.int32 and count.numel() == 1), "count")
+    lead, x_dtype = x.shape, _DTYPES.get(x.dtype)
+    if x_dtype is None or codes.dtype != _i8 or scales.dtype != _f32:
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: x in float32, bfloat16 or float16, int8 codes and float32 scales are needed")
+    I = lead[-1] if lead else 0
+    ldx, ldc, ldv, v = _pitch_of(where, x, I), _pitch_of(where, codes, I), 0, None
+    T, N, n = lead[0] if len(lead) == 2 else lead[0] * lead[1], scales.numel(), codes.shape
+    if N != (n[0] if len(n) == 2 else n[0] * n[1]) or not scales.is_contiguous():
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: a scale for every row of codes is needed")
+    if rows is not None:
+        _wants(where, rows.dtype == _i32 and rows.numel() == N and rows.is_contiguous(), "rows")
+    if count is not None:
+        _wants(where, count.dtype == _i32 and count.numel() == 1, "count")
     if values is not None:
-        _wants(where, values.dtype == torch.float32 and values.shape == codes.shape, "values are float32 of the codes' shape")
-        ldv = _pitch_of(where, values, I)
-    _on_current(where, x, codes, scales, rows, count, values)
-    _check(lib().pipe_int8_quantize(x.data_ptr(), _DTYPES[x.dtype], x.shape[:-1].numel(), I, ldx, _dp(rows), N, _dp(count), codes.data_ptr(),
-                                    ldc, scales.data_ptr(), _dp(values), ldv, _stream_ptr(stream)), where)
+        _wants(where, values.dtype == _f32 and values.shape == n, "values are float32 of the codes' shape")
+        ldv, v = _pitch_of(where, values, I), values.data_ptr()
+    dev = x.get_device()
+    if dev < 0 or dev != _current_device() or codes.get_device() != dev or scales.get_device() != dev:
+        _on_current(where, x, codes, scales)
+    if rows is not None or count is not None or v is not None:
+        _on_current(where, x, rows, count, values)
+    status = lib().pipe_int8_quantize(x.data_ptr(), x_dtype, T, I, ldx, _dp(rows), N, _dp(count), codes.data_ptr(), ldc, scales.data_ptr(), v,
+                                      ldv, _raw_stream(dev) if stream is None else _stream_ptr(stream))
+    if status != PIPE_OK:
+        raise PipeError(status, where)
 
 
-def _int8_product(where: str, desc: Int8Desc, codes, scales, xq, sx, bias, y, offsets) -> int:
-    """Checks what both products take alike; the pitch of the weights."""
-    E, O, N = desc.experts, desc.out_features, xq.shape[0] if xq.dim() else -1
-    i8, f32, h = torch.int8, torch.float32, y.dtype
-    if codes.dtype != i8 or xq.dtype != i8 or scales.dtype != f32 or sx.dtype != f32 or _DTYPES.get(h) != desc.dtype:
+def _int8_product(where: str, desc: Int8Desc, codes, scales, xq, sx, bias, y) -> tuple[int, int, int, int]:
+    """Checks what both products take alike; the pitches of the weights, of xq and of y, and the rows."""
+    E, O, I, h = desc.experts, desc.out_features, desc.in_features, y.dtype
+    if codes.dtype != _i8 or xq.dtype != _i8 or scales.dtype != _f32 or sx.dtype != _f32 or _DTYPES.get(h) != desc.dtype:
         raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: int8 codes, float32 scales and outputs of the layer's type are needed")
-    if codes.shape[:-1].numel() != E * O or not _laid_out(scales, E, O):
+    ldw, ldx, ldy = _pitch_of(where, codes, I), _pitch_of(where, xq, I), _pitch_of(where, y, O)
+    w, N = codes.shape, y.shape[0]
+    if (w[0] if len(w) == 2 else w[0] * w[1]) != E * O or not _laid_out(scales, E, O):
         raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: codes and scales are not the descriptor's arrays")
-    if y.dim() != 2 or y.shape[0] != N or sx.numel() != N or not sx.is_contiguous():
+    if y.dim() != 2 or xq.dim() != 2 or xq.shape[0] != N or sx.numel() != N or not sx.is_contiguous():
         raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: xq, sx and y differ in rows")
-    if bias is not None and (bias.dtype != h or not _laid_out(bias, E, O)):
-        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: the bias is not [E, O] in the layer's type")
-    _on_current(where, codes, scales, xq, sx, bias, y, offsets)
-    return _pitch_of(where, codes, desc.in_features)
+    dev = codes.get_device()
+    if dev < 0 or dev != _current_device() or scales.get_device() != dev or xq.get_device() != dev or sx.get_device() != dev or y.get_device() != dev:
+        _on_current(where, codes, scales, xq, sx, y)
+    if bias is not None:
+        if bias.dtype != h or not _laid_out(bias, E, O):
+            raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: the bias is not [E, O] in the layer's type")
+        _on_current(where, codes, bias)
+    return ldw, ldx, ldy, N
 
 
 def pipe_int8_linear(desc: Int8Desc, codes: torch.Tensor, scales: torch.Tensor, xq: torch.Tensor, sx: torch.Tensor, y: torch.Tensor,
@@ -702,10 +723,11 @@ def pipe_int8_linear(desc: Int8Desc, codes: torch.Tensor, scales: torch.Tensor, 
     """codes: cuda int8 [O, I] (or [1, O, I]), scales: float32 [O]; xq: int8 [T, I], sx: float32 [T]; y: [T, O], bias: [O], in the layer's
     type.  Rows of codes and xq lie at multiples of 16 bytes."""
     where = "pipe_int8_linear"
-    ldw = _int8_product(where, desc, codes, scales, xq, sx, bias, y, None)
-    _check(lib().pipe_int8_linear(C.byref(desc), codes.data_ptr(), ldw, scales.data_ptr(), xq.data_ptr(), xq.shape[0],
-                                  _pitch_of(where, xq, desc.in_features), sx.data_ptr(), _dp(bias), activation, y.data_ptr(),
-                                  _pitch_of(where, y, desc.out_features), _stream_ptr(stream)), where)
+    ldw, ldx, ldy, T = _int8_product(where, desc, codes, scales, xq, sx, bias, y)
+    status = lib().pipe_int8_linear(C.byref(desc), codes.data_ptr(), ldw, scales.data_ptr(), xq.data_ptr(), T, ldx, sx.data_ptr(), _dp(bias),
+                                    activation, y.data_ptr(), ldy, _stream_ptr(stream))
+    if status != PIPE_OK:
+        raise PipeError(status, where)
 
 
 def pipe_int8_expert_linear(desc: Int8Desc, codes: torch.Tensor, scales: torch.Tensor, xq: torch.Tensor, sx: torch.Tensor,
@@ -714,11 +736,15 @@ def pipe_int8_expert_linear(desc: Int8Desc, codes: torch.Tensor, scales: torch.T
     """codes: cuda int8 [E, O, I], scales: float32 [E, O]; xq: int8 [N, I], sx: float32 [N]; offsets: int32 [E + 1]; y: [N, O];
     bias: [E, O] or None."""
     where = "pipe_int8_expert_linear"
-    ldw = _int8_product(where, desc, codes, scales, xq, sx, bias, y, offsets)
-    _wants(where, offsets.dtype == torch.int32 and offsets.numel() == desc.experts + 1 and offsets.is_contiguous(), "offsets")
-    _check(lib().pipe_int8_expert_linear(C.byref(desc), codes.data_ptr(), ldw, scales.data_ptr(), xq.data_ptr(),
-                                         _pitch_of(where, xq, desc.in_features), sx.data_ptr(), offsets.data_ptr(), xq.shape[0], _dp(bias),
-                                         activation, y.data_ptr(), _pitch_of(where, y, desc.out_features), _stream_ptr(stream)), where)
+    ldw, ldx, ldy, N = _int8_product(where, desc, codes, scales, xq, sx, bias, y)
+    if offsets.dtype != _i32 or offsets.numel() != desc.experts + 1 or not offsets.is_contiguous():
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: offsets are int32 [experts + 1]")
+    if offsets.get_device() != codes.get_device():
+        _on_current(where, codes, offsets)
+    status = lib().pipe_int8_expert_linear(C.byref(desc), codes.data_ptr(), ldw, scales.data_ptr(), xq.data_ptr(), ldx, sx.data_ptr(),
+                                           offsets.data_ptr(), N, _dp(bias), activation, y.data_ptr(), ldy, _stream_ptr(stream))
+    if status != PIPE_OK:
+        raise PipeError(status, where)
 
 
 def alloc_int8(rows: int, I: int, device="cuda", experts: int | None = None):
@@ -734,22 +760,41 @@ def pipe_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None
     """logits: cuda float32 / bfloat16 / float16 [T, V]; tokens: int32 [T, n], logprobs: float32 [T, n] (or both [T]); entropy: float32
     [T]; top: int32 [T, k], top_logprobs: float32 [T, k]."""
     where = "pipe_token_logprobs"
-    _wants(where, logits.dim() == 2 and logits.dtype in _DTYPES, "logits [T, V] in float32, bfloat16 or float16")
-    T, V = logits.shape
+    shape, dtype = logits.shape, _DTYPES.get(logits.dtype)
+    if len(shape) != 2 or dtype is None:
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: logits [T, V] in float32, bfloat16 or float16 are needed")
+    T, V = shape
     n = k = 0
+    a = b = c = d = e = None
+    dev = logits.get_device()
+    ok = dev >= 0 and dev == _current_device()
     if tokens is not None or logprobs is not None:
-        _wants(where, tokens is not None and logprobs is not None and tokens.dtype == torch.int32 and logprobs.dtype == torch.float32 and
-               tokens.shape == logprobs.shape and tokens.dim() in (1, 2) and tokens.shape[0] == T and tokens.is_contiguous() and
+        s = tokens.shape if tokens is not None and logprobs is not None else ()
+        _wants(where, len(s) in (1, 2) and s[0] == T and logprobs.shape == s and tokens.dtype == _i32 and logprobs.dtype == _f32 and tokens.is_contiguous() and
                logprobs.is_contiguous(), "tokens int32 [T, n] and logprobs float32 [T, n]")
-        n = tokens.shape[1] if tokens.dim() == 2 else 1
-    _wants(where, entropy is None or (entropy.dtype == torch.float32 and entropy.shape == (T,) and entropy.is_contiguous()), "entropy float32 [T]")
-    for t, kind in ((top, torch.int32), (top_logprobs, torch.float32)):
-        if t is not None:
-            _wants(where, t.dtype == kind and t.dim() == 2 and t.shape[0] == T and t.is_contiguous() and k in (0, t.shape[1]), "top int32 [T, k], top_logprobs float32 [T, k]")
-            k = t.shape[1]
-    _on_current(where, logits, tokens, logprobs, entropy, top, top_logprobs)
-    _check(lib().pipe_token_logprobs(logits.data_ptr(), _DTYPES[logits.dtype], T, V, _pitch_of(where, logits, V), scale, _dp(tokens), n, _dp(logprobs), _dp(entropy), k, _dp(top),
-                                     _dp(top_logprobs), _stream_ptr(stream)), where)
+        n = s[1] if len(s) == 2 else 1
+        a, b, ok = tokens.data_ptr(), logprobs.data_ptr(), ok and tokens.get_device() == dev and logprobs.get_device() == dev
+        if n == 0:
+            a = b = None
+    if entropy is not None:
+        _wants(where, entropy.dtype == _f32 and entropy.shape == (T,) and entropy.is_contiguous(), "entropy float32 [T]")
+        c, ok = entropy.data_ptr(), ok and entropy.get_device() == dev
+    if top is not None:
+        s = top.shape
+        _wants(where, len(s) == 2 and s[0] == T and top.dtype == _i32 and top.is_contiguous(), "top int32 [T, k]")
+        k, d, ok = s[1], top.data_ptr(), ok and top.get_device() == dev
+    if top_logprobs is not None:
+        s = top_logprobs.shape
+        _wants(where, len(s) == 2 and s[0] == T and (top is None or s[1] == k) and top_logprobs.dtype == _f32 and top_logprobs.is_contiguous(),
+               "top_logprobs float32 [T, k]")
+        k, e, ok = s[1], top_logprobs.data_ptr(), ok and top_logprobs.get_device() == dev
+    if k == 0:
+        d = e = None
+    if not ok:
+        raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: all tensors have to be on the current device")
+    status = lib().pipe_token_logprobs(logits.data_ptr(), dtype, T, V, _pitch_of(where, logits, V), scale, a, n, b, c, k, d, e, _stream_ptr(stream))
+    if status != PIPE_OK:
+        raise PipeError(status, where)
 
 
 def pipe_diag_select_kernel(which: int) -> None:

@@ -12,11 +12,13 @@
 namespace pipe {
 namespace lpb {
 
-constexpr float kLog2e = 1.44269504f;
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 constexpr float kFar = -1e30f;     // differences below have probability 0 at every scale (2^-20 at least)
-constexpr int kFound = 512;        // most logits that are ranked: no less than a cluster's PIPE_MAX_TOP each
+constexpr int kFound = 544;        // most logits that are ranked: no less than a cluster's PIPE_MAX_TOP each
 constexpr int kCluster = 8;
-static_assert(kFound >= kCluster * PIPE_MAX_TOP, "");
+constexpr int kWide = 512, kNarrow = 128, kResident = 1536;   // threads of a CTA, and of an SM
+constexpr int kAhead = 4;                                      // vectors that a thread has in flight
+static_assert(kFound >= kCluster * PIPE_MAX_TOP && kFound % 2 == 0, "");
 
 struct Args {
   const void* logits;
@@ -69,6 +71,13 @@ struct Vec {
     else if constexpr (SRC == PIPE_DTYPE_BF16) return __uint_as_float(i & 1 ? u[i >> 1] & 0xFFFF0000u : u[i >> 1] << 16);
     else return grp::Fp16::to_float(static_cast<uint16_t>(i & 1 ? u[i >> 1] >> 16 : u[i >> 1]));
   }
+  // (bf16: what is below -1e30 made that, a NaN kept)
+  __device__ __forceinline__ void raise() {
+    if constexpr (SRC == PIPE_DTYPE_BF16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = larger2(u[i], 0xF14AF14Au);   // (-1.00025e30, no more than kFar)
+    }
+  }
   // the largest of these, a NaN if there is one
   static __device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
     uint32_t d;
@@ -106,8 +115,8 @@ __device__ __forceinline__ float logit(const uint8_t* row, int64_t i) {
   return SRC == PIPE_DTYPE_BF16 ? grp::Bf16::to_float(h) : grp::Fp16::to_float(h);
 }
 
-// The sums over some logits: m the largest (-Inf: none; a NaN or +Inf: no distribution), s = sum exp(scale (l - m)), h = sum (l - m)
-// exp(scale (l - m)).
+// The sums over some logits: m the largest (-Inf: none; a NaN or +Inf: no distribution), s = sum 2^z and h = sum z 2^z with
+// z = c (l - m), c = scale log2 e.
 struct Sums {
   float m, s, h;
 };
@@ -117,9 +126,9 @@ __device__ __forceinline__ Sums joined(const Sums& own, float c) {
   Sums r = own;
 #pragma unroll
   for (int o = N / 2; o; o >>= 1) r.m = max_nan(r.m, __shfl_xor_sync(0xffffffffu, r.m, o));
-  const float d = fmaxf(own.m - fmaxf(r.m, -3.402823466e38f), kFar), f = ex2(d * c);
+  const float z = fmaxf(fmaxf(own.m - fmaxf(r.m, -3.402823466e38f), kFar) * c, kFar), f = ex2(z);
   r.s = own.s * f;
-  r.h = (own.h + own.s * d) * f;
+  r.h = (own.h + own.s * z) * f;
 #pragma unroll
   for (int o = N / 2; o; o >>= 1) {
     r.s += __shfl_xor_sync(0xffffffffu, r.s, o);
@@ -200,6 +209,40 @@ __device__ __forceinline__ void look_again(const Part& p, uint32_t own, uint32_t
 // The `count` entries ranked: out[i], i < k, with zeros where there are none.
 template <int B>
 __device__ __forceinline__ void rank(Search<B>& s, int count, int k, Entry* out) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (count > 2 * k + 64) {
+    // first brought down to some more than k by one warp: halving between none and the largest (entries are different, but for zeros)
+    if (warp == 0) {
+      Entry lo = 0, hi = 0;
+      for (int i = lane; i < count; i += 32) hi = max(hi, s.entry[i]);
+      hi = static_cast<Entry>(__reduce_max_sync(0xffffffffu, static_cast<uint32_t>(hi >> 32))) << 32 | 0xFFFFFFFFu;
+      int n = count;
+      while (lo < hi && n > k + 16) {
+        const Entry half = lo + (hi - lo + 1) / 2;
+        int c = 0;
+        for (int i = lane; i < count; i += 32) c += s.entry[i] >= half;
+        c = __reduce_add_sync(0xffffffffu, c);
+        if (c >= k) {
+          lo = half;
+          n = c;
+        } else {
+          hi = half - 1;
+        }
+      }
+      int kept = 0;
+      for (int i0 = 0; i0 < count; i0 += 32) {
+        const Entry e = i0 + lane < count ? s.entry[i0 + lane] : 0;
+        const bool in = e != 0 && e >= lo;
+        const uint32_t m = __ballot_sync(0xffffffffu, in);   // (these have been read: what is written lies at or before them)
+        if (in) s.entry[kept + __popc(m & ((1u << lane) - 1))] = e;
+        kept += __popc(m);
+        __syncwarp();
+      }
+      if (lane == 0) s.found = kept;
+    }
+    __syncthreads();
+    count = s.found;
+  }
   for (int i = threadIdx.x; i < k; i += B) out[i] = 0;
   if (threadIdx.x == 0) s.entry[count] = 0;
   __syncthreads();
@@ -245,8 +288,9 @@ __device__ int search(Search<B>& s, const Part& p, float m, int k) {
       mine[i] = s.group[32 * i + lane];
       hi = max(hi, mine[i]);
     }
+    if (k <= 32) lo = max(lo, __reduce_min_sync(0xffffffffu, hi));   // (every lane has a group as large as that)
     hi = __reduce_max_sync(0xffffffffu, hi);
-    int n = B;
+    int n = kGroups;
     while (lo < hi && n > k + (k >> 1) + 4) {
       const uint32_t mid = lo + (hi - lo + 1) / 2;
       int c = 0;
@@ -340,8 +384,8 @@ __device__ int search(Search<B>& s, const Part& p, float m, int k) {
 
 // B threads a CTA; a cluster of CTAs a row.  ENT: the entropy is wanted.
 template <int SRC, int B, bool ENT>
-__global__ void __launch_bounds__(B, 1536 / B) logprobs_kernel(const Args a) {
-  constexpr int kLogits = Vec<SRC>::kLogits, kSize = Vec<SRC>::kSize, kAhead = 4;
+__global__ void __launch_bounds__(B, kResident / B) logprobs_kernel(const Args a) {
+  constexpr int kLogits = Vec<SRC>::kLogits, kSize = Vec<SRC>::kSize;
   __shared__ Search<B> search_s;
   __shared__ Sums warp_s[B / 32];
   __shared__ Sums own_s;                     // this CTA's
@@ -363,15 +407,26 @@ __global__ void __launch_bounds__(B, 1536 / B) logprobs_kernel(const Args a) {
   grid_wait();
   grid_release();
 
+  // a given token and its logit, on their way while the row is read
+  int token = -1;
+  float given = 0.f;
+  if (crank == 0 && static_cast<int>(threadIdx.x) < a.n) {
+    token = __ldcg(a.tokens + t * a.n + threadIdx.x);
+    if (token >= 0 && token < a.V) given = logit<SRC>(p.row, token);
+  }
+  // The pass.  z is formed by one fused operation, c l - ref with ref = c m rounded: the same ref for all, so that what its rounding adds to
+  // every z cancels in the end.  For that the largest logit may not be beyond 1e29 (see below), and smaller logits than -1e30 count as that.
   Sums own = {-INFINITY, 0.f, 0.f};
+  float ref = kFar * c;
   f32x2 s2 = both_f2(0.f), h2 = both_f2(0.f);
   auto grow = [&](float m) {   // a new largest logit
-    const float base = fmaxf(m, -3.402823466e38f), d = fmaxf(own.m - base, kFar), f = ex2(d * c);
-    if (ENT) h2 = mul_f2(fma_f2(s2, both_f2(d), h2), both_f2(f));
+    const float to = fminf(fmaxf(m, kFar), -kFar) * c, z = fmaxf(ref - to, kFar), f = ex2(z);
+    if (ENT) h2 = mul_f2(fma_f2(s2, both_f2(z), h2), both_f2(f));
     s2 = mul_f2(s2, both_f2(f));
     own.m = m;
+    ref = to;
   };
-  for (int v0 = p.first + static_cast<int>(threadIdx.x); v0 < p.end; v0 += kAhead * B) {   // (at most 2^28 vectors)
+  for (int v0 = p.first + static_cast<int>(threadIdx.x); v0 - lane < p.end; v0 += kAhead * B) {   // (at most 2^28 vectors)
     Vec<SRC> v[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
@@ -380,31 +435,34 @@ __global__ void __launch_bounds__(B, 1536 / B) logprobs_kernel(const Args a) {
     }
     const float m = max_nan(own.m, Vec<SRC>::largest(v));
     if (!(m <= own.m)) grow(m);
-    const f32x2 minus = both_f2(-fmaxf(own.m, -3.402823466e38f)), c2 = both_f2(c);
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j)
+    for (int j = 0; j < kAhead; ++j) {
+      if (v0 - lane + j * B >= p.end) break;   // (whole warps)
+      if (ENT) v[j].raise();
 #pragma unroll
       for (int i = 0; i < kLogits; i += 2) {
-        f32x2 d = add_f2(pack_f2(v[j].at(i), v[j].at(i + 1)), minus);
-        float d0, d1;
-        if (ENT) {   // (an infinite difference times its exponential would be no number)
-          unpack_f2(d, d0, d1);
-          d = pack_f2(fmaxf(d0, kFar), fmaxf(d1, kFar));
+        f32x2 z = fma_f2(pack_f2(v[j].at(i), v[j].at(i + 1)), both_f2(c), both_f2(-ref));
+        float z0, z1;
+        unpack_f2(z, z0, z1);
+        if (ENT && SRC != PIPE_DTYPE_BF16) {   // (an infinite z times its power would be no number)
+          z0 = fmaxf(z0, kFar);
+          z1 = fmaxf(z1, kFar);
+          z = pack_f2(z0, z1);
         }
-        unpack_f2(mul_f2(d, c2), d0, d1);
-        const f32x2 e = pack_f2(ex2(d0), ex2(d1));
+        const f32x2 e = pack_f2(ex2(z0), ex2(z1));
         s2 = add_f2(s2, e);
-        if (ENT) h2 = fma_f2(d, e, h2);
+        if (ENT) h2 = fma_f2(z, e, h2);
       }
+    }
   }
 #pragma unroll
   for (int which = 0; which < 2; ++which)
     if (static_cast<int>(threadIdx.x) < (which ? p.tail : p.head)) {
       const float l = logit<SRC>(p.row, (which ? p.tail_at : 0) + static_cast<int>(threadIdx.x)), m = max_nan(own.m, l);
       if (!(m <= own.m)) grow(m);
-      const float d = fmaxf(l - fmaxf(own.m, -3.402823466e38f), kFar), e = ex2(d * c);
+      const float z = fmaxf(fmaf(l, c, -ref), kFar), e = ex2(z);
       s2 = add_f2(s2, pack_f2(e, 0.f));
-      h2 = fma_f2(both_f2(d), pack_f2(e, 0.f), h2);
+      h2 = fma_f2(both_f2(z), pack_f2(e, 0.f), h2);
     }
   const float mine = own.m;
   {
@@ -413,6 +471,28 @@ __global__ void __launch_bounds__(B, 1536 / B) logprobs_kernel(const Args a) {
     own.s = x + y;
     unpack_f2(h2, x, y);
     own.h = x + y;
+  }
+  if (fabsf(mine) <= 1e29f) {   // from ref to c m
+    const float z = fmaf(mine, c, -ref), f = ex2(-z);
+    own.h = (own.h - own.s * z) * f;
+    own.s *= f;
+  } else if (fabsf(mine) <= 3.402823466e38f) {
+    // logits of a size at which c l may be beyond the type's range (masked by its lowest number, all that this thread has): once more, by
+    // differences
+    own.s = own.h = 0.f;
+    auto add = [&](float l) {
+      const float z = fmaxf(fmaxf(l - mine, kFar) * c, kFar), e = ex2(z);
+      own.s += e;
+      own.h += z * e;
+    };
+    for (int v = p.first + static_cast<int>(threadIdx.x); v < p.end; v += B) {
+      Vec<SRC> w;
+      w.load(p.vectors + v * int64_t{16});
+#pragma unroll
+      for (int i = 0; i < kLogits; ++i) add(w.at(i));
+    }
+    if (static_cast<int>(threadIdx.x) < p.head) add(logit<SRC>(p.row, threadIdx.x));
+    if (static_cast<int>(threadIdx.x) < p.tail) add(logit<SRC>(p.row, p.tail_at + static_cast<int>(threadIdx.x)));
   }
   own = joined<32>(own, c);
   if (lane == 0) warp_s[warp] = own;
@@ -447,11 +527,14 @@ __global__ void __launch_bounds__(B, 1536 / B) logprobs_kernel(const Args a) {
   auto logprob = [&](float l) { return bad ? nan : (none || l == -INFINITY ? -INFINITY : (0.5f * l - 0.5f * own.m) * a.scale * 2.f - logs); };
   if (threadIdx.x == 0) {
     if (bad) raise_status(a.status, PIPE_ERR_NONFINITE);
-    if (ENT) a.entropy[t] = bad ? nan : (none ? 0.f : logs - a.scale * own.h / own.s);
+    if (ENT) a.entropy[t] = bad ? nan : (none ? 0.f : logs - kLn2 * own.h / own.s);
   }
   for (int j = threadIdx.x; j < a.n; j += B) {
-    const int token = __ldcg(a.tokens + t * a.n + j);
-    a.logprobs[t * a.n + j] = token >= 0 && token < a.V ? logprob(logit<SRC>(p.row, token)) : 0.f;
+    if (j >= B) {
+      token = __ldcg(a.tokens + t * a.n + j);
+      if (token >= 0 && token < a.V) given = logit<SRC>(p.row, token);
+    }
+    a.logprobs[t * a.n + j] = token >= 0 && token < a.V ? logprob(given) : 0.f;
   }
   if (a.k > 0) {
     __syncthreads();
@@ -466,16 +549,16 @@ __global__ void __launch_bounds__(B, 1536 / B) logprobs_kernel(const Args a) {
 using Kernel = void (*)(Args);
 template <int SRC>
 static Kernel logprobs_of(bool wide, bool entropy) {
-  if (wide) return entropy ? logprobs_kernel<SRC, 512, true> : logprobs_kernel<SRC, 512, false>;
-  return entropy ? logprobs_kernel<SRC, 128, true> : logprobs_kernel<SRC, 128, false>;
+  if (wide) return entropy ? logprobs_kernel<SRC, kWide, true> : logprobs_kernel<SRC, kWide, false>;
+  return entropy ? logprobs_kernel<SRC, kNarrow, true> : logprobs_kernel<SRC, kNarrow, false>;
 }
 
 // Threads of a CTA and CTAs of a row.
 static void choose(int64_t T, int V, int size, int* threads, int* ctas) {
   const int64_t bytes = static_cast<int64_t>(V) * size;
-  *threads = bytes <= 32768 ? 128 : 512;
+  *threads = bytes <= 32768 ? kNarrow : kWide;
   *ctas = 1;
-  while (*ctas < kCluster && bytes / *ctas > 16384 && T * *ctas * 2 <= 3 * kPlanSMs) *ctas *= 2;
+  while (*ctas < kCluster && bytes / *ctas > 16384 && T * *ctas * 2 <= kResident / *threads * kPlanSMs) *ctas *= 2;
 }
 
 }  // namespace lpb
@@ -503,7 +586,7 @@ extern "C" pipe_status pipe_token_logprobs(const void* d_logits, int32_t dtype, 
   if (!a.status) return grp::runtime_failed();
   int threads, ctas;
   lpb::choose(T, V, dtype == PIPE_DTYPE_FP32 ? 4 : 2, &threads, &ctas);
-  const bool wide = threads == 512;
+  const bool wide = threads == lpb::kWide;
   const lpb::Kernel kern = dtype == PIPE_DTYPE_FP32 ? lpb::logprobs_of<PIPE_DTYPE_FP32>(wide, d_entropy != nullptr)
                                                     : (dtype == PIPE_DTYPE_BF16 ? lpb::logprobs_of<PIPE_DTYPE_BF16>(wide, d_entropy != nullptr)
                                                                                 : lpb::logprobs_of<PIPE_DTYPE_FP16>(wide, d_entropy != nullptr));
