@@ -22,7 +22,7 @@ static_assert(kFound >= kCluster * PIPE_MAX_TOP && kFound % 2 == 0, "");
 
 struct Args {
   const void* logits;
-  int64_t ldl;
+  int64_t T, ldl;
   int V;
   float scale;
   const int32_t* tokens;
@@ -145,6 +145,21 @@ struct Part {
   const uint8_t* vectors;
   int head, tail, first, end, tail_at, head_all;
 };
+template <int SRC>
+__device__ __forceinline__ Part part_of(const Args& a, int64_t t, int crank, int ctas) {
+  constexpr int kLogits = Vec<SRC>::kLogits, kSize = Vec<SRC>::kSize;
+  Part p;
+  p.row = static_cast<const uint8_t*>(a.logits) + t * a.ldl * kSize;
+  p.head_all = min(a.V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(p.row) & 15)) & 15) / kSize);
+  p.vectors = p.row + p.head_all * kSize;
+  const int all = (a.V - p.head_all) / kLogits;
+  p.first = static_cast<int>(static_cast<int64_t>(all) * crank / ctas);
+  p.end = static_cast<int>(static_cast<int64_t>(all) * (crank + 1) / ctas);
+  p.head = crank == 0 ? p.head_all : 0;
+  p.tail_at = p.head_all + all * kLogits;
+  p.tail = crank == ctas - 1 ? a.V - p.tail_at : 0;
+  return p;
+}
 
 // A logit and its place as one number, larger for what is listed first: the key above, the place's complement below.  0: none.
 using Entry = unsigned long long;
@@ -153,6 +168,7 @@ __device__ __forceinline__ uint32_t key_in(Entry e) { return static_cast<uint32_
 __device__ __forceinline__ int place_in(Entry e) { return static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(e)); }
 
 constexpr int kGroups = 256;
+
 
 // Shared memory of the search for the alternatives.
 template <int B>
@@ -385,7 +401,7 @@ __device__ int search(Search<B>& s, const Part& p, float m, int k) {
 // B threads a CTA; a cluster of CTAs a row.  ENT: the entropy is wanted.
 template <int SRC, int B, bool ENT>
 __global__ void __launch_bounds__(B, kResident / B) logprobs_kernel(const Args a) {
-  constexpr int kLogits = Vec<SRC>::kLogits, kSize = Vec<SRC>::kSize;
+  constexpr int kLogits = Vec<SRC>::kLogits;
   __shared__ Search<B> search_s;
   __shared__ Sums warp_s[B / 32];
   __shared__ Sums own_s;                     // this CTA's
@@ -393,16 +409,7 @@ __global__ void __launch_bounds__(B, kResident / B) logprobs_kernel(const Args a
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int ctas = grp::cluster_ctas(), crank = grp::cluster_rank();
   const int64_t t = blockIdx.x / ctas;
-  Part p;
-  p.row = static_cast<const uint8_t*>(a.logits) + t * a.ldl * kSize;
-  p.head_all = min(a.V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(p.row) & 15)) & 15) / kSize);
-  p.vectors = p.row + p.head_all * kSize;
-  const int all = (a.V - p.head_all) / kLogits;
-  p.first = static_cast<int>(static_cast<int64_t>(all) * crank / ctas);
-  p.end = static_cast<int>(static_cast<int64_t>(all) * (crank + 1) / ctas);
-  p.head = crank == 0 ? p.head_all : 0;
-  p.tail_at = p.head_all + all * kLogits;
-  p.tail = crank == ctas - 1 ? a.V - p.tail_at : 0;
+  const Part p = part_of<SRC>(a, t, crank, ctas);
   const float c = a.scale * kLog2e;
   grid_wait();
   grid_release();
@@ -426,18 +433,12 @@ __global__ void __launch_bounds__(B, kResident / B) logprobs_kernel(const Args a
     own.m = m;
     ref = to;
   };
-  for (int v0 = p.first + static_cast<int>(threadIdx.x); v0 - lane < p.end; v0 += kAhead * B) {   // (at most 2^28 vectors)
-    Vec<SRC> v[kAhead];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      if (v0 + j * B < p.end) v[j].load(p.vectors + (v0 + j * B) * int64_t{16});
-      else v[j].fill();
-    }
+  auto take = [&](Vec<SRC> (&v)[kAhead], int some) {   // `some` of these are there: the same number in a whole warp
     const float m = max_nan(own.m, Vec<SRC>::largest(v));
     if (!(m <= own.m)) grow(m);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      if (v0 - lane + j * B >= p.end) break;   // (whole warps)
+      if (j >= some) break;
       if (ENT) v[j].raise();
 #pragma unroll
       for (int i = 0; i < kLogits; i += 2) {
@@ -454,6 +455,24 @@ __global__ void __launch_bounds__(B, kResident / B) logprobs_kernel(const Args a
         if (ENT) h2 = fma_f2(z, e, h2);
       }
     }
+  };
+  // whole batches first: loads at fixed distances, nothing to be asked for each (with conditions: 8 instructions a logit, of which 4 its own)
+  int v0 = p.first + static_cast<int>(threadIdx.x);
+  const uint8_t* from = p.vectors + v0 * int64_t{16};
+  for (; v0 - lane + 31 + (kAhead - 1) * B < p.end; v0 += kAhead * B, from += kAhead * B * 16) {   // (at most 2^28 vectors)
+    Vec<SRC> v[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) v[j].load(from + j * B * 16);
+    take(v, kAhead);
+  }
+  if (v0 - lane < p.end) {
+    Vec<SRC> v[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (v0 + j * B < p.end) v[j].load(from + j * B * 16);
+      else v[j].fill();
+    }
+    take(v, (p.end - (v0 - lane) + B - 1) / B);
   }
 #pragma unroll
   for (int which = 0; which < 2; ++which)
@@ -553,14 +572,6 @@ static Kernel logprobs_of(bool wide, bool entropy) {
   return entropy ? logprobs_kernel<SRC, kNarrow, true> : logprobs_kernel<SRC, kNarrow, false>;
 }
 
-// Threads of a CTA and CTAs of a row.
-static void choose(int64_t T, int V, int size, int* threads, int* ctas) {
-  const int64_t bytes = static_cast<int64_t>(V) * size;
-  *threads = bytes <= 32768 ? kNarrow : kWide;
-  *ctas = 1;
-  while (*ctas < kCluster && bytes / *ctas > 16384 && T * *ctas * 2 <= kResident / *threads * kPlanSMs) *ctas *= 2;
-}
-
 }  // namespace lpb
 }  // namespace pipe
 
@@ -582,16 +593,18 @@ extern "C" pipe_status pipe_token_logprobs(const void* d_logits, int32_t dtype, 
       misaligned(d_top, 4) || misaligned(d_top_logprobs, 4))
     return PIPE_ERR_ALIGNMENT;
   if (T == 0) return PIPE_OK;
-  lpb::Args a = {d_logits, ldl, V, scale, d_tokens, n, d_logprobs, d_entropy, k, d_top, d_top_logprobs, device_status_word()};
+  lpb::Args a = {d_logits, T, ldl, V, scale, d_tokens, n, d_logprobs, d_entropy, k, d_top, d_top_logprobs, device_status_word()};
   if (!a.status) return grp::runtime_failed();
-  int threads, ctas;
-  lpb::choose(T, V, dtype == PIPE_DTYPE_FP32 ? 4 : 2, &threads, &ctas);
-  const bool wide = threads == lpb::kWide;
+  // Rows of more than 32 KB go to CTAs of 512 threads, few of them to several each; shorter ones to CTAs of 128.
+  const int64_t bytes = static_cast<int64_t>(V) * (dtype == PIPE_DTYPE_FP32 ? 4 : 2);
+  const bool wide = bytes > 32768;
+  int ctas = 1;
+  while (wide && ctas < lpb::kCluster && bytes / ctas > 16384 && T * ctas * 2 <= lpb::kResident / lpb::kWide * kPlanSMs) ctas *= 2;
   const lpb::Kernel kern = dtype == PIPE_DTYPE_FP32 ? lpb::logprobs_of<PIPE_DTYPE_FP32>(wide, d_entropy != nullptr)
                                                     : (dtype == PIPE_DTYPE_BF16 ? lpb::logprobs_of<PIPE_DTYPE_BF16>(wide, d_entropy != nullptr)
                                                                                 : lpb::logprobs_of<PIPE_DTYPE_FP16>(wide, d_entropy != nullptr));
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (launch_overlapped(kern, dim3(static_cast<unsigned>(T * ctas)), threads, ctas, true, s, a) != cudaSuccess) return grp::runtime_failed();
+  if (launch_overlapped(kern, dim3(static_cast<unsigned>(T * ctas)), wide ? lpb::kWide : lpb::kNarrow, ctas, true, s, a) != cudaSuccess) return grp::runtime_failed();
   count_launch(1);
   take_expansion_mark(s);
   return launch_status();
