@@ -180,63 +180,82 @@ struct Search {
   int run[2][B / 32];
 };
 
-// f(logit, index) for the logits of this CTA's part that are not below `least` (of the key of a number), of threads whose largest, `own`,
-// is not.  Whole warps look at a thread's vectors, those of four threads at a time.
+// take(in, logit, place), by whole warps, for the logits of this CTA's part that may be not below `least` (of the key of a number; in: one
+// that is not), of threads whose largest, `own`, is not.  Where a thread has many vectors its warp looks at them, those of four threads at
+// a time; otherwise it looks itself.
 template <int SRC, int B, class F>
-__device__ __forceinline__ void look_again(const Part& p, uint32_t own, uint32_t least, F f) {
+__device__ __forceinline__ void look_again(const Part& p, uint32_t own, uint32_t least, F take) {
   constexpr int kLogits = Vec<SRC>::kLogits;
   const int lane = threadIdx.x & 31;
   const float bound = number_of(least);
-  uint32_t which = __ballot_sync(0xffffffffu, own >= least);
-  while (which) {
-    int t[4];
+  const bool mine = own >= least;
+  uint32_t which = __ballot_sync(0xffffffffu, mine);
+  if (!which) return;
+  auto look = [&](int v0, int v1, int v2, int v3) {   // at these vectors (p.end: none)
+    const int v[4] = {v0, v1, v2, v3};
+    Vec<SRC> w[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      t[j] = which ? static_cast<int>(threadIdx.x & ~31u) + __ffs(which) - 1 : -1;
-      which &= which - 1;
+      if (v[j] < p.end) w[j].load(p.vectors + v[j] * int64_t{16});
+      else w[j].fill();
     }
-    for (int v0 = p.first + lane * B; v0 < p.end; v0 += 32 * B) {
-      Vec<SRC> w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const Vec<SRC> one[1] = {w[j]};
+      if (!__any_sync(0xffffffffu, Vec<SRC>::largest(one) >= bound)) continue;
+#pragma unroll
+      for (int i = 0; i < kLogits; ++i) take(w[j].at(i) >= bound, w[j].at(i), p.head_all + v[j] * kLogits + i);
+    }
+  };
+  if (p.end - p.first <= 4 * B) {
+    const int v = mine ? p.first + static_cast<int>(threadIdx.x) : p.end;
+    look(v, min(v + B, p.end), min(v + 2 * B, p.end), min(v + 3 * B, p.end));
+  } else {
+    while (which) {
+      int t[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (t[j] >= 0 && v0 + t[j] < p.end) w[j].load(p.vectors + (v0 + t[j]) * int64_t{16});
-        else w[j].fill();
+        t[j] = which ? p.first + static_cast<int>(threadIdx.x & ~31u) + __ffs(which) - 1 : p.end;
+        which &= which - 1;
       }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const Vec<SRC> one[1] = {w[j]};
-        if (Vec<SRC>::largest(one) >= bound) {
-#pragma unroll
-          for (int i = 0; i < kLogits; ++i)
-            if (w[j].at(i) >= bound) f(w[j].at(i), p.head_all + (v0 + t[j]) * kLogits + i);
-        }
+      for (int at = 0; p.first + at < p.end; at += 32 * B) {   // (at most 2^28 vectors)
+        const int more = at + lane * B;
+        look(min(t[0] + more, p.end), min(t[1] + more, p.end), min(t[2] + more, p.end), min(t[3] + more, p.end));
       }
     }
-    if (lane < 8) {   // their logits of head and tail
-      const int j = lane & 3, u = j & 2 ? (j & 1 ? t[3] : t[2]) : (j & 1 ? t[1] : t[0]), at = lane & 4 ? p.tail_at + u : u;
-      if (u >= 0 && u < (lane & 4 ? p.tail : p.head)) {
-        const float l = logit<SRC>(p.row, at);
-        if (l >= bound) f(l, at);
-      }
+  }
+#pragma unroll
+  for (int of = 0; of < 2; ++of) {
+    const int n = of ? p.tail : p.head, at = (of ? p.tail_at : 0) + static_cast<int>(threadIdx.x);
+    if (static_cast<int>(threadIdx.x & ~31u) < n) {
+      const float l = static_cast<int>(threadIdx.x) < n ? logit<SRC>(p.row, at) : -INFINITY;
+      take(l >= bound, l, at);
     }
   }
 }
 
-// The `count` entries ranked: out[i], i < k, with zeros where there are none.
+// The `count` entries ranked: out[i], i < k, with zeros where there are none.  (A barrier has to stand before and behind.)
 template <int B>
 __device__ __forceinline__ void rank(Search<B>& s, int count, int k, Entry* out) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (count > 2 * k + 64) {
-    // first brought down to some more than k by one warp: halving between none and the largest (entries are different, but for zeros)
+    // first brought down to some more than k by one warp, by halving between the least and the largest of their keys
     if (warp == 0) {
-      Entry lo = 0, hi = 0;
-      for (int i = lane; i < count; i += 32) hi = max(hi, s.entry[i]);
-      hi = static_cast<Entry>(__reduce_max_sync(0xffffffffu, static_cast<uint32_t>(hi >> 32))) << 32 | 0xFFFFFFFFu;
+      const uint32_t* key = reinterpret_cast<const uint32_t*>(s.entry) + 1;   // (of entry i: key[2 i])
+      uint32_t lo = ~0u, hi = 0;
+      for (int i = lane; i < count; i += 32) {
+        const uint32_t v = key[2 * i];
+        hi = max(hi, v);
+        lo = min(lo, v);
+      }
+      lo = __reduce_min_sync(0xffffffffu, lo);
+      hi = __reduce_max_sync(0xffffffffu, hi);
       int n = count;
       while (lo < hi && n > k + 16) {
-        const Entry half = lo + (hi - lo + 1) / 2;
+        const uint32_t half = lo + (hi - lo + 1) / 2;
         int c = 0;
-        for (int i = lane; i < count; i += 32) c += s.entry[i] >= half;
+#pragma unroll 4
+        for (int i = lane; i < count; i += 32) c += key[2 * i] >= half;
         c = __reduce_add_sync(0xffffffffu, c);
         if (c >= k) {
           lo = half;
@@ -248,7 +267,7 @@ __device__ __forceinline__ void rank(Search<B>& s, int count, int k, Entry* out)
       int kept = 0;
       for (int i0 = 0; i0 < count; i0 += 32) {
         const Entry e = i0 + lane < count ? s.entry[i0 + lane] : 0;
-        const bool in = e != 0 && e >= lo;
+        const bool in = e != 0 && key_in(e) >= lo;
         const uint32_t m = __ballot_sync(0xffffffffu, in);   // (these have been read: what is written lies at or before them)
         if (in) s.entry[kept + __popc(m & ((1u << lane) - 1))] = e;
         kept += __popc(m);
@@ -307,7 +326,7 @@ __device__ int search(Search<B>& s, const Part& p, float m, int k) {
     if (k <= 32) lo = max(lo, __reduce_min_sync(0xffffffffu, hi));   // (every lane has a group as large as that)
     hi = __reduce_max_sync(0xffffffffu, hi);
     int n = kGroups;
-    while (lo < hi && n > k + (k >> 1) + 4) {
+    while (lo < hi && n > k + (k >> 2) + 2) {
       const uint32_t mid = lo + (hi - lo + 1) / 2;
       int c = 0;
 #pragma unroll
@@ -324,10 +343,16 @@ __device__ int search(Search<B>& s, const Part& p, float m, int k) {
   }
   __syncthreads();
   uint32_t least = s.least;
-  look_again<SRC, B>(p, own, least, [&](float l, int i) {
-    const int at = atomicAdd(&s.found, 1);
-    if (at < kFound) s.entry[at] = entry_of(l, i);
-  });
+  // (the places of a warp's finds at once)
+  auto keep = [&](bool in, float l, int i) {
+    const uint32_t m = __ballot_sync(0xffffffffu, in);
+    if (!m) return;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&s.found, __popc(m));
+    at = __shfl_sync(0xffffffffu, at, 0) + __popc(m & ((1u << lane) - 1));
+    if (in && at < kFound) s.entry[at] = entry_of(l, i);
+  };
+  look_again<SRC, B>(p, own, least, keep);
   __syncthreads();
   if (s.found <= kFound) return s.found;
 
@@ -338,7 +363,7 @@ __device__ int search(Search<B>& s, const Part& p, float m, int k) {
   for (int turn = 0; least < hi; turn ^= 1) {   // (the same in all threads; at least k logits reach `least`)
     const uint32_t mid = least + (hi - least + 1) / 2;
     int c = 0;
-    look_again<SRC, B>(p, own, mid, [&](float, int) { ++c; });
+    look_again<SRC, B>(p, own, mid, [&](bool in, float, int) { c += in; });
     c = __reduce_add_sync(0xffffffffu, c);
     if (lane == 0) s.run[turn][warp] = c;
     __syncthreads();
@@ -352,9 +377,7 @@ __device__ int search(Search<B>& s, const Part& p, float m, int k) {
   __syncthreads();
   if (threadIdx.x == 0) s.found = 0;
   __syncthreads();
-  look_again<SRC, B>(p, own, least, [&](float l, int i) {
-    if (key_of(l) > least) s.entry[atomicAdd(&s.found, 1)] = entry_of(l, i);
-  });
+  look_again<SRC, B>(p, own, least + 1, keep);
   __syncthreads();
   int have = s.found;
   constexpr int kLogits = Vec<SRC>::kLogits;
