@@ -1,15 +1,16 @@
 // Rows to int8 by a scale of their own (definition: pipe_int8_quantize in include/pipe.h).
 //
-// One pass, bound by HBM: a row's values stay in registers between the search for the largest magnitude and the codes.  P threads take
-// a row, four neighbouring values at a time, so that every load and store of a warp is of whole neighbouring lines; the largest
-// magnitude is found on the values' bits, which order like the magnitudes, a NaN above all.  Rows beyond what the registers hold are
-// read a second time.
+// One pass: a row's values stay in registers between the search for the largest magnitude and the codes.  P threads take a row,
+// neighbouring values W at a time, every load and store of a warp of whole neighbouring lines: eight of 16 bits, four where values are
+// written too (their 16-byte stores would leave half-written sectors otherwise).  The largest magnitude is found on the values' bits,
+// which order like the magnitudes, a NaN above all.  Rows beyond what the registers hold are read a second time.  Bound by HBM where
+// values are written, otherwise by the issue slots: some 7 instructions a value and 100 a thread and row.
 #include "int8_common.cuh"
 
 namespace pipe {
 namespace i8 {
 
-constexpr int kQHeld = 8;   // fours of values that a thread holds
+constexpr int kQHeld = 32;   // values that a thread holds
 
 struct QuantArgs {
   const void* x;
@@ -22,7 +23,7 @@ struct QuantArgs {
   float* scales;
   float* values;
   int64_t ldv;
-  int wide_x, wide_c, wide_v;   // fours of values, codes, values behind the codes are aligned to their size
+  int wide_x, wide_c, wide_v;   // W values, W codes, four values behind the codes are aligned to their size
   int* status;
 };
 
@@ -32,31 +33,29 @@ __device__ __noinline__ float exact_code(float x, float s) {
   return fminf(fmaxf(static_cast<float>(rint(static_cast<double>(x) / static_cast<double>(s))), -127.f), 127.f);
 }
 
-// Four neighbouring values as they lie in memory.
-template <int SRC>
-struct Four {
-  static constexpr int kWords = SRC == PIPE_DTYPE_FP32 ? 4 : 2;
+// W neighbouring values as they lie in memory.
+template <int SRC, int W>
+struct Run {
+  static constexpr int kWords = SRC == PIPE_DTYPE_FP32 ? W : W / 2;
   uint32_t u[kWords];
-  __device__ __forceinline__ void load(const uint8_t* row, int i, int I, bool wide) {   // values i .. i + 3 of a row of I; zeros behind it
-    if constexpr (SRC == PIPE_DTYPE_FP32) {
-      const uint32_t* p = reinterpret_cast<const uint32_t*>(row) + i;
-      if (wide && i + 4 <= I) {
-        const uint4 a = __ldcg(reinterpret_cast<const uint4*>(p));
+  __device__ __forceinline__ void load(const uint8_t* row, int i, int I, bool wide) {   // values i .. of a row of I; zeros behind it
+    const uint8_t* at = row + static_cast<int64_t>(i) * (SRC == PIPE_DTYPE_FP32 ? 4 : 2);
+    if (wide && i + W <= I) {
+      if constexpr (kWords == 4) {
+        const uint4 a = __ldcg(reinterpret_cast<const uint4*>(at));
         u[0] = a.x; u[1] = a.y; u[2] = a.z; u[3] = a.w;
       } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) u[j] = i + j < I ? __ldcg(p + j) : 0u;
-      }
-    } else {
-      const uint16_t* p = reinterpret_cast<const uint16_t*>(row) + i;
-      if (wide && i + 4 <= I) {
-        const uint2 a = __ldcg(reinterpret_cast<const uint2*>(p));
+        const uint2 a = __ldcg(reinterpret_cast<const uint2*>(at));
         u[0] = a.x; u[1] = a.y;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          u[j] = (i + 2 * j < I ? __ldcg(p + 2 * j) : 0u) | (i + 2 * j + 1 < I ? static_cast<uint32_t>(__ldcg(p + 2 * j + 1)) << 16 : 0u);
       }
+    } else if constexpr (SRC == PIPE_DTYPE_FP32) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) u[j] = i + j < I ? __ldcg(reinterpret_cast<const uint32_t*>(at) + j) : 0u;
+    } else {
+      const uint16_t* p = reinterpret_cast<const uint16_t*>(at);
+#pragma unroll
+      for (int j = 0; j < W / 2; ++j)
+        u[j] = (i + 2 * j < I ? __ldcg(p + 2 * j) : 0u) | (i + 2 * j + 1 < I ? static_cast<uint32_t>(__ldcg(p + 2 * j + 1)) << 16 : 0u);
     }
   }
   __device__ __forceinline__ void zero() {
@@ -65,26 +64,30 @@ struct Four {
   }
   // the larger of `most` and the magnitudes (16-bit types: in both halves)
   __device__ __forceinline__ uint32_t magnitude(uint32_t most) const {
-    if constexpr (SRC == PIPE_DTYPE_FP32) return max(max(most, max(u[0] & 0x7FFFFFFFu, u[1] & 0x7FFFFFFFu)), max(u[2] & 0x7FFFFFFFu, u[3] & 0x7FFFFFFFu));
-    else return __vmaxu2(most, __vmaxu2(u[0] & 0x7FFF7FFFu, u[1] & 0x7FFF7FFFu));
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) {
+      if constexpr (SRC == PIPE_DTYPE_FP32) most = max(most, u[j] & 0x7FFFFFFFu);
+      else most = __vmaxu2(most, u[j] & 0x7FFF7FFFu);
+    }
+    return most;
   }
   __device__ __forceinline__ float value(int j) const {
     if constexpr (SRC == PIPE_DTYPE_FP32) return __uint_as_float(u[j]);
-    const uint16_t h = static_cast<uint16_t>(u[j >> 1] >> (16 * (j & 1)));
-    return SRC == PIPE_DTYPE_BF16 ? grp::Bf16::to_float(h) : grp::Fp16::to_float(h);
+    else if constexpr (SRC == PIPE_DTYPE_BF16) return __uint_as_float(j & 1 ? u[j >> 1] & 0xFFFF0000u : u[j >> 1] << 16);
+    else return grp::Fp16::to_float(static_cast<uint16_t>(u[j >> 1] >> (16 * (j & 1))));
   }
 };
 template <int SRC>
-__device__ __forceinline__ float as_number(uint32_t magnitude) {   // of Four::magnitude, over a whole row
+__device__ __forceinline__ float as_number(uint32_t magnitude) {   // of Run::magnitude, over a whole row
   if constexpr (SRC == PIPE_DTYPE_FP32) return __uint_as_float(magnitude);
   const uint16_t h = static_cast<uint16_t>(max(magnitude & 0xFFFFu, magnitude >> 16));
   return SRC == PIPE_DTYPE_BF16 ? grp::Bf16::to_float(h) : grp::Fp16::to_float(h);
 }
 
 // P threads of a row; a block of 256 threads, or of P where that is more.
-template <int SRC, int P>
+template <int SRC, int W, int P>
 __global__ void __launch_bounds__(P > 256 ? P : 256) int8_quantize_kernel(const QuantArgs a) {
-  constexpr int kThreads = P > 256 ? P : 256, kRows = kThreads / P;
+  constexpr int kThreads = P > 256 ? P : 256, kRows = kThreads / P, kRuns = kQHeld / W;
   constexpr int kSize = SRC == PIPE_DTYPE_FP32 ? 4 : 2;
   __shared__ uint32_t most_s[kThreads / 32];
   grid_wait();
@@ -98,32 +101,29 @@ __global__ void __launch_bounds__(P > 256 ? P : 256) int8_quantize_kernel(const 
   const int I = mine && r >= 0 && r < a.T ? a.I : 0;   // values to be read
   const uint8_t* row = static_cast<const uint8_t*>(a.x) + (I ? r * a.ldx * kSize : 0);
 
-  Four<SRC> held[kQHeld];
-  uint32_t most = 0;
+  Run<SRC, W> held[kRuns];
 #pragma unroll
-  for (int k = 0; k < kQHeld; ++k) {
-    const int i = 4 * (k * P + l);
+  for (int k = 0; k < kRuns; ++k) {
+    const int i = W * (k * P + l);
     if (i < I) held[k].load(row, i, I, a.wide_x);
     else held[k].zero();
   }
+  uint32_t most = 0;
 #pragma unroll
-  for (int k = 0; k < kQHeld; ++k) most = held[k].magnitude(most);
-  for (int i = 4 * (kQHeld * P + l); i < I; i += 4 * P) {
-    Four<SRC> f;
+  for (int k = 0; k < kRuns; ++k) most = held[k].magnitude(most);
+  for (int i = kQHeld * P + W * l; i < I; i += W * P) {   // (I is below 2^29 + 1)
+    Run<SRC, W> f;
     f.load(row, i, I, a.wide_x);
     most = f.magnitude(most);
   }
-  float top = as_number<SRC>(most);
-  most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+  most = __reduce_max_sync(0xffffffffu, __float_as_uint(as_number<SRC>(most)));
   if (P > 32) {
     if ((threadIdx.x & 31) == 0) most_s[threadIdx.x >> 5] = most;
     __syncthreads();
-    const int first = (threadIdx.x / P) * (P / 32);
-#pragma unroll
-    for (int w = 0; w < P / 32; ++w) most = max(most, most_s[first + w]);
+    most = __reduce_max_sync(0xffffffffu, most_s[(threadIdx.x / P) * (P / 32) + (threadIdx.x & 31) % (P / 32)]);
   }
   if (!mine) return;
-  top = __uint_as_float(most);
+  const float top = __uint_as_float(most);
   const bool finite = top <= 3.402823466e38f;
   const float s = __fdiv_rn(top, 127.f);
   if (l == 0) {
@@ -134,59 +134,86 @@ __global__ void __launch_bounds__(P > 256 ? P : 256) int8_quantize_kernel(const 
   const float inv = fast ? __frcp_rn(s) : 0.f;
   int8_t* codes = a.codes + slot * a.ldc;
   float* values = a.values ? a.values + slot * a.ldv : nullptr;
-  auto put = [&](const Four<SRC>& f, int i) {
-    float q[4] = {0.f, 0.f, 0.f, 0.f};
-    if (some) {
-      // An estimate rounded by an addition (1.5 * 2^23, where the spacing of binary32 is one) is off by one at most.  The remainder
-      // x - q s is exact: a multiple of the last place of s (of half of it where |x| < s), and at most s.  Where it reaches half a step,
-      // on a tie or where the estimate went wrong, the definition is evaluated.
-      float edge = fast ? 0.f : s;
-      if (fast) {
+  const f32x2 inv2 = both_f2(inv), less2 = both_f2(-s), magic2 = both_f2(12582912.f);
+  auto put = [&](const Run<SRC, W>& f, int i) {
+    // An estimate rounded by an addition (1.5 * 2^23, where the spacing of binary32 is one, and the code the low byte) is off by one at
+    // most.  The remainder x - q s is exact: a multiple of the last place of s (of half of it where |x| < s), and at most s.  Where it
+    // reaches half a step, on a tie or where the estimate went wrong, the definition is evaluated.
+    f32x2 q[W / 2];
+    uint32_t word[W / 4];
+    float u[W], edge = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          q[j] = __fsub_rn(__fmaf_rn(f.value(j), inv, 12582912.f), 12582912.f);
-          edge = fmaxf(edge, fabsf(fmaf(-q[j], s, f.value(j))));
-        }
-      }
-      if (2.f * edge >= s) {
+    for (int h = 0; h < W / 2; ++h) {
+      const f32x2 x = pack_f2(f.value(2 * h), f.value(2 * h + 1)), sum = fma_f2(x, inv2, magic2);
+      unpack_f2(sum, u[2 * h], u[2 * h + 1]);
+      q[h] = sub_f2(sum, magic2);
+      float r0, r1;
+      unpack_f2(fma_f2(q[h], less2, x), r0, r1);
+      edge = max3_abs(edge, r0, r1);
+    }
+    if (!fast || 2.f * edge >= s) {   // (a step without a usable reciprocal, zero and infinity among them: not fast)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q[j] = exact_code(f.value(j), s);
+      for (int h = 0; h < W / 2; ++h) {
+        const float e0 = some ? exact_code(f.value(2 * h), s) : 0.f, e1 = some ? exact_code(f.value(2 * h + 1), s) : 0.f;
+        q[h] = pack_f2(e0, e1);
+        u[2 * h] = e0 + 12582912.f;
+        u[2 * h + 1] = e1 + 12582912.f;
       }
     }
-    if (a.wide_c && i + 4 <= a.I) {
-      *reinterpret_cast<uint32_t*>(codes + i) = pack4_low_bytes(q[0] + 12582912.f, q[1] + 12582912.f, q[2] + 12582912.f, q[3] + 12582912.f);
+#pragma unroll
+    for (int h = 0; h < W / 4; ++h) word[h] = pack4_low_bytes(u[4 * h], u[4 * h + 1], u[4 * h + 2], u[4 * h + 3]);
+    if (a.wide_c && i + W <= a.I) {
+      if constexpr (W == 8) *reinterpret_cast<uint2*>(codes + i) = make_uint2(word[0], word[1]);
+      else *reinterpret_cast<uint32_t*>(codes + i) = word[0];
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (i + j < a.I) codes[i + j] = static_cast<int8_t>(static_cast<int>(q[j]));
+      for (int j = 0; j < W; ++j)
+        if (i + j < a.I) codes[i + j] = static_cast<int8_t>(word[j >> 2] >> (8 * (j & 3)));
     }
-    if (values) {
-      if (a.wide_v && i + 4 <= a.I) {
-        __stcg(reinterpret_cast<float4*>(values + i), make_float4(q[0] * s, q[1] * s, q[2] * s, q[3] * s));
-      } else {
+    if constexpr (W == 4) {
+      if (values) {
+        float v[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (i + j < a.I) values[i + j] = q[j] * s;
+        for (int h = 0; h < 2; ++h) unpack_f2(mul_f2(q[h], both_f2(s)), v[2 * h], v[2 * h + 1]);
+        if (a.wide_v && i + 4 <= a.I) {
+          __stcg(reinterpret_cast<float4*>(values + i), make_float4(v[0], v[1], v[2], v[3]));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (i + j < a.I) values[i + j] = v[j];
+        }
       }
     }
   };
 #pragma unroll
-  for (int k = 0; k < kQHeld; ++k) {
-    const int i = 4 * (k * P + l);
+  for (int k = 0; k < kRuns; ++k) {
+    const int i = W * (k * P + l);
     if (i < a.I) put(held[k], i);
   }
-  for (int64_t i = 4 * (static_cast<int64_t>(kQHeld) * P + l); i < a.I; i += 4 * P) {
-    Four<SRC> f;
-    if (I) f.load(row, static_cast<int>(i), I, a.wide_x);
+  for (int i = kQHeld * P + W * l; i < a.I; i += W * P) {
+    Run<SRC, W> f;
+    if (I) f.load(row, i, a.I, a.wide_x);
     else f.zero();
-    put(f, static_cast<int>(i));
+    put(f, i);
   }
 }
 
 using QuantKernel = void (*)(QuantArgs);
-template <int SRC>
+template <int SRC, int W>
 static QuantKernel quantize_kernel(int P) {
-  return P == 32 ? int8_quantize_kernel<SRC, 32> : (P == 128 ? int8_quantize_kernel<SRC, 128> : int8_quantize_kernel<SRC, 512>);
+  switch (P) {
+    case 32: return int8_quantize_kernel<SRC, W, 32>;
+    case 64: return int8_quantize_kernel<SRC, W, 64>;
+    case 128: return int8_quantize_kernel<SRC, W, 128>;
+    case 256: return int8_quantize_kernel<SRC, W, 256>;
+    default: return int8_quantize_kernel<SRC, W, 512>;
+  }
+}
+template <int SRC>
+static QuantKernel quantize_kernel(int P, bool values) {
+  if constexpr (SRC != PIPE_DTYPE_FP32)
+    if (!values) return quantize_kernel<SRC, 8>(P);
+  return quantize_kernel<SRC, 4>(P);
 }
 
 }  // namespace i8
@@ -215,15 +242,17 @@ extern "C" pipe_status pipe_int8_quantize(const void* d_x, int32_t x_dtype, int6
   a.codes = d_codes; a.ldc = ldc;
   a.scales = d_scales;
   a.values = d_values; a.ldv = ldv;
-  a.wide_x = !misaligned(d_x, 4 * size) && ldx % 4 == 0;
-  a.wide_c = !misaligned(d_codes, 4) && ldc % 4 == 0;
+  const int W = d_values || size == 4 ? 4 : 8;
+  a.wide_x = !misaligned(d_x, W * size) && ldx % W == 0;
+  a.wide_c = !misaligned(d_codes, W) && ldc % W == 0;
   a.wide_v = !misaligned(d_values, 16) && ldv % 4 == 0;
   a.status = device_status_word();
   if (!a.status) return grp::runtime_failed();
   // the fewest threads whose registers hold a row
-  const int P = I <= 4 * i8::kQHeld * 32 ? 32 : (I <= 4 * i8::kQHeld * 128 ? 128 : 512);
-  const i8::QuantKernel k = x_dtype == PIPE_DTYPE_FP32 ? i8::quantize_kernel<PIPE_DTYPE_FP32>(P)
-                                                       : (x_dtype == PIPE_DTYPE_BF16 ? i8::quantize_kernel<PIPE_DTYPE_BF16>(P) : i8::quantize_kernel<PIPE_DTYPE_FP16>(P));
+  int P = 32;
+  while (P < 512 && I > i8::kQHeld * P) P *= 2;
+  const i8::QuantKernel k = x_dtype == PIPE_DTYPE_FP32 ? i8::quantize_kernel<PIPE_DTYPE_FP32>(P, d_values)
+                                                       : (x_dtype == PIPE_DTYPE_BF16 ? i8::quantize_kernel<PIPE_DTYPE_BF16>(P, d_values) : i8::quantize_kernel<PIPE_DTYPE_FP16>(P, d_values));
   const int threads = P > 256 ? P : 256;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (launch_overlapped(k, dim3(static_cast<unsigned>(ceil_div<int64_t>(N, threads / P))), threads, 1, true, s, a) != cudaSuccess) return grp::runtime_failed();
