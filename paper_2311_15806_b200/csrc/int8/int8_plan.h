@@ -100,8 +100,8 @@ inline bool plan_tc(const TcShape& c, TcPlan* p) {
     if (small == last) continue;
     last = small;
     for (int cg = 1; cg <= 2; ++cg) {
-      const int TN = cg == 1 ? small : wide;
-      if (cg == 1 ? TN > 128 : c.O <= 64) continue;
+      if (cg == 2 && c.O <= 64) continue;
+      const int TN = cg == 2 ? wide : (small < 128 ? small : 128);
       // rows fill units evenly where there is one expert; otherwise an expert's last unit is half full, on average
       const int64_t units = c.ragged ? (2 * mean > TN ? div_up(2 * mean + TN, 2 * TN) : 1) * experts : div_up(c.N, TN);
       for (int TM = cg == 1 ? 32 : 64; TM <= 128; TM += 16) {

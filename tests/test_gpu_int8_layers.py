@@ -328,3 +328,117 @@ def test_a_layer_of_experts_from_router_to_sum():
                 room[t] += float(mix[t, j]) * (tol[0] + 2.0 ** -22 * v[0].abs())
     room = room + 2.0 ** -8 * (want.abs() + room) + 1e-30
     assert ((out.cpu().double() - want).abs() <= room).all()
+
+
+# ---- streams, captures, offsets past 31 bits ----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("T,O,I", [(3, 2048, 4096), (5, 300, 11008), (90, 1000, 640), (700, 2048, 512)])
+def test_captured_and_replayed_and_on_two_streams_at_once(T, O, I):
+    """One token's form, a split axis, single CTAs and pairs: the same bits from a graph, from another stream, from both streams at once."""
+    gen = _gen(T)
+    _, sw, wd = _layer(gen, 1, O, I)
+    sw = sw.cuda()
+    d = B.make_int8_desc(O, I)
+    x = [torch.randn((T, I), generator=gen).to(torch.bfloat16).cuda() for _ in range(2)]
+    q = [B.alloc_int8(T, I) for _ in range(2)]
+    y = [torch.empty((T, O), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+
+    def forward(i, stream=None):
+        B.pipe_int8_quantize(x[i], *q[i], stream=stream)
+        B.pipe_int8_linear(d, wd, sw, *q[i], y[i], activation=2, stream=stream)
+
+    want = []
+    for i in range(2):
+        forward(i)
+        want.append(y[i].clone())
+        y[i].zero_()
+    _ok()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            forward(i, streams[i])
+    _ok()
+    assert torch.equal(y[0], want[0]) and torch.equal(y[1], want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        forward(0)
+        forward(0)
+    x[0].copy_(x[1])
+    for _ in range(3):
+        graph.replay()
+    _ok()
+    assert torch.equal(y[0], want[1])
+
+
+def test_weights_and_outputs_beyond_31_bits():
+    gen = _gen(21)
+    # rows of weights, and of an expert, that begin beyond 2^31 bytes
+    O, I = 530000, 4112
+    codes = torch.empty((O, I), dtype=torch.int8, device="cuda")
+    codes.random_(-128, 128)
+    sw = torch.rand(O, device="cuda") * 0.01
+    for T in (2, 70):
+        x = torch.randint(-128, 128, (T, I), generator=gen, dtype=torch.int8)
+        sx = torch.rand((T,), generator=gen)
+        y = torch.empty((T, O), dtype=torch.bfloat16, device="cuda")
+        B.pipe_int8_linear(B.make_int8_desc(O, I), codes, sw, x.cuda(), sx.cuda(), y)
+        _ok()
+        for part in (slice(0, 300), slice(O - 300, O)):
+            R.check_product(y[:, part], x, sx, codes[part], sw[part], None, 0, "bf16")
+        half = torch.empty((T, O // 2), dtype=torch.float32, device="cuda")
+        B.pipe_int8_expert_linear(B.make_int8_desc(O // 2, I, dtype=torch.float32, experts=2), codes.view(2, O // 2, I), sw, x.cuda(), sx.cuda(),
+                                  torch.tensor([0, 1, T], dtype=torch.int32, device="cuda"), half)
+        _ok()
+        R.check_product(half[1:, -300:], x[1:], sx[1:], codes[-300:], sw[-300:], None, 0, "fp32")
+    del codes, y, half
+    # outputs beyond 2^31 values
+    T, O, I = 70000, 32000, 16
+    w, sw, wd = _layer(gen, 1, O, I)
+    x = torch.randint(-128, 128, (T, I), generator=gen, dtype=torch.int8)
+    sx = torch.rand((T,), generator=gen)
+    y = torch.empty((T, O), dtype=torch.bfloat16, device="cuda")
+    B.pipe_int8_linear(B.make_int8_desc(O, I), wd, sw.cuda(), x.cuda(), sx.cuda(), y)
+    _ok()
+    for part in (slice(0, 40), slice(T - 40, T)):
+        R.check_product(y[part], x[part], sx[part], w[0], sw[0], None, 0, "bf16")
+
+
+def test_rows_to_int8_far_apart():
+    gen = _gen(22)
+    I, pitch = 1003, (1 << 31) + 8
+    flat = torch.empty(pitch + I, dtype=torch.bfloat16, device="cuda")
+    x = torch.randn((2, I), generator=gen).to(torch.bfloat16)
+    at = flat.as_strided((2, I), (pitch, 1))
+    at.copy_(x)
+    raw = torch.empty(pitch + I, dtype=torch.int8, device="cuda")
+    codes, scales = raw.as_strided((2, I), (pitch, 1)), torch.empty(2, device="cuda")
+    B.pipe_int8_quantize(at, codes, scales)
+    _ok()
+    s, q = R.quantized(x)
+    assert torch.equal(codes.cpu(), q) and torch.equal(scales.cpu(), s)
+
+
+def test_ties_of_16_bit_values():
+    """Rows whose quotients come to halves by the few bits of their values: every multiple of a half up to the largest."""
+    for dtype in ("bf16", "fp16"):
+        x = torch.stack([torch.arange(-254, 255) * 0.5 * 2.0 ** e for e in range(-6, 4)])
+        x = torch.cat([x, torch.arange(509).double().repeat(3, 1) * torch.tensor([[1.0], [0.375], [3.0]])]).to(R.TYPES[dtype])
+        codes, scales = B.alloc_int8(x.shape[0], x.shape[1])
+        values = torch.empty(x.shape, device="cuda")
+        s, q = R.quantized(x)
+        B.pipe_int8_quantize(x.cuda(), codes, scales)
+        _ok()
+        assert torch.equal(codes.cpu(), q) and torch.equal(scales.cpu(), s)
+        B.pipe_int8_quantize(x.cuda(), codes, scales, values=values)
+        _ok()
+        assert torch.equal(codes.cpu(), q) and torch.equal(values.cpu(), (q.double() * s.double()[:, None]).float())
+
+
+@pytest.mark.parametrize("T,O,I", [(5000, 50, 200), (3000, 64, 130), (2600, 1, 16), (9000, 65, 48)])
+def test_narrow_layers_on_many_rows(T, O, I):
+    _linear(T, O, I, "bf16", 1, True, T)
+
+
+def test_narrow_experts_on_many_rows():
+    _expert(3, 40, 96, "fp16", [700, 0, 2000], True, 2, 30)
+    _expert(5, 8, 300, "fp32", [150, 151, 0, 149, 600], False, 0, 31)
