@@ -43,15 +43,17 @@ struct TcPlan {
   int64_t teams;   // CTAs, pairs or clusters of the launch
 };
 
+constexpr int accumulator_columns(int TN) { return (TN + 31) & ~31; }
+
 // Shared memory, tensor memory and launch of a chosen tile.  False: it does not fit.
 inline bool lay_out(const TcShape& c, TcPlan* p) {
   p->stages = static_cast<int>(div_up(c.I, kBlock * p->KS));
   p->mtiles = static_cast<int>(div_up(c.O, p->TM * p->cg));
   p->tiles = most_units(c.ragged, c.N, c.E, p->TN) * p->mtiles;
   if (p->tiles * p->split * p->cg >= (int64_t{1} << 31)) return false;
-  // Accumulators: two of TN columns, 32 at least (what a drain reads at once); of a split one.  CTAs that wait for one another while they
+  // Accumulators: two of TN columns, rounded up to what a drain reads at once; of a split one.  CTAs that wait for one another while they
   // hold tensor memory, the pairs, take so much shared memory that no two of them meet on an SM.
-  const int wide = p->TN < 32 ? 32 : p->TN;
+  const int wide = accumulator_columns(p->TN);
   p->columns = 32;
   while (p->columns < (p->split > 1 ? 1 : 2) * wide) p->columns *= 2;
   const int turn = p->split > 1 ? 0 : kDrainWarps * kTurnBytes, sx = p->split > 1 ? 0 : kDrainWarps * wide * 4, table = unit_ints(c.E) * 4;

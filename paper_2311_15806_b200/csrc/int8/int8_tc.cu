@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
   const uint32_t w_block = static_cast<uint32_t>(p.TM) * kBlock, x_block = static_cast<uint32_t>(p.TN / CG) * kBlock;
   const uint32_t stage_bytes = p.KS * (w_block + x_block);
   const uint32_t ring = p.ring;
-  const int acc_pitch = p.TN < 32 ? 32 : p.TN;
+  const int acc_pitch = accumulator_columns(p.TN);
 
   if (threadIdx.x == 0) {
     abort_s = 0;
@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
     for (int64_t t = team; t < tiles; t += teams, ++n) {
       const Tile tl = tile_of<CG>(p, table, static_cast<int>(t), rank);
       const int o0 = tl.o0, end = min(c.O, o0 + p.TM), count = tl.hi - tl.lo;
-      const int64_t ch0 = static_cast<int64_t>(tl.e) * c.O;
+      const int64_t ch0 = static_cast<int64_t>(tl.e) * c.O, row0 = tl.lo;
       const uint32_t buf = n & 1, use = n >> 1;
       constexpr int kMine = H::kBytes == 4 ? 1 : 4;   // this thread's channels: 32 q + lane, or 32 q + lane / 4 + 8 h
       float sw[kMine], bias[kMine];
@@ -279,30 +279,39 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
       __syncwarp();
       if (!__all_sync(0xffffffffu, mbar_wait<CG == 2, 64>(d_full + 8 * buf, use & 1, abort_flag, c.status))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t acc = from + buf * acc_pitch;
       for (int n0 = 32 * half; n0 < count; n0 += 64) {   // rows of y, 32 at a time
+        int v[2][16];
         if constexpr (H::kBytes == 4) {
           const int o = o0 + 32 * q + lane;
-          float* y = static_cast<float*>(c.y) + (static_cast<int64_t>(tl.lo) + n0) * c.ldy + o;
-          int v[2][16];   // 16 rows each
-          tmem_ld16(from + buf * acc_pitch + n0, v[0]);
-          tmem_ld16(from + buf * acc_pitch + n0 + 16, v[1]);
+          float* y = static_cast<float*>(c.y) + (row0 + n0) * c.ldy + o;
+          tmem_ld16(acc + n0, v[0]);   // 16 rows each
+          tmem_ld16(acc + n0 + 16, v[1]);
           asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          float u[2][16];
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            float u[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) u[i] = scaled(v[g][i], sw[0], sx[n0 + 16 * g + i], bias[0]);
-            grp::quick_activation(u, c.act);
+            for (int i = 0; i < 16; i += 4) {
+              const float4 s = *reinterpret_cast<const float4*>(sx + n0 + 16 * g + i);
+              u[g][i] = scaled(v[g][i], sw[0], s.x, bias[0]);
+              u[g][i + 1] = scaled(v[g][i + 1], sw[0], s.y, bias[0]);
+              u[g][i + 2] = scaled(v[g][i + 2], sw[0], s.z, bias[0]);
+              u[g][i + 3] = scaled(v[g][i + 3], sw[0], s.w, bias[0]);
+            }
+          }
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            activate(u[g], c.act);
             if (o < end) {
 #pragma unroll
-              for (int i = 0; i < 16; ++i)
-                if (n0 + 16 * g + i < count) y[(16 * g + i) * c.ldy] = u[i];
+              for (int i = 0; i < 16; ++i, y += c.ldy)
+                if (n0 + 16 * g + i < count) *y = u[g][i];
             }
           }
         } else {
-          int v[2][16];   // 16 channels each
-          tmem_ld_16x32(from + buf * acc_pitch + n0, v[0]);
-          tmem_ld_16x32(from + (16u << 16) + buf * acc_pitch + n0, v[1]);
+          tmem_ld_16x32(acc + n0, v[0]);   // 16 channels each
+          tmem_ld_16x32(acc + (16u << 16) + n0, v[1]);
           float sc[8];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -318,26 +327,25 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
             float u[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) u[i] = scaled(v[h >> 1][4 * (i >> 1) + 2 * (h & 1) + (i & 1)], sw[h], sc[i], bias[h]);
-            grp::quick_activation(u, c.act);
+            activate(u, c.act);
             turn_store(smem_u32(turn) + lane * 64 + ((h ^ ((lane >> 1) & 3)) * 16), H::pack(u[0], u[1]), H::pack(u[2], u[3]), H::pack(u[4], u[5]), H::pack(u[6], u[7]));
           }
           __syncwarp();
           const int piece = lane & 3, r0 = lane >> 2, col = o0 + 32 * q + 8 * piece;
-          uint16_t* y = static_cast<uint16_t*>(c.y) + (static_cast<int64_t>(tl.lo) + n0 + r0) * c.ldy + col;
+          uint16_t* y = static_cast<uint16_t*>(c.y) + (row0 + n0 + r0) * c.ldy + col;
           uint4 w[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const uint4*>(turn + (r0 + 8 * i) * 64 + ((piece ^ ((r0 >> 1) & 3)) * 16));
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 4; ++i, y += 8 * c.ldy)
             if (n0 + r0 + 8 * i < count && col < end) {
-              uint16_t* at = y + static_cast<int64_t>(8 * i) * c.ldy;
               if (p.wide_y && c.O - col >= 8) {
-                *reinterpret_cast<uint4*>(at) = w[i];
+                *reinterpret_cast<uint4*>(y) = w[i];
               } else {
                 const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
-                  if (k < c.O - col) at[k] = static_cast<uint16_t>(u[k >> 1] >> (16 * (k & 1)));
+                  if (k < c.O - col) y[k] = static_cast<uint16_t>(u[k >> 1] >> (16 * (k & 1)));
               }
             }
         }
@@ -403,7 +411,7 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
           const bool real = col + k < c.O;
           v[k] = scaled(acc[k], real ? __ldcg(p.call.sw + ch0 + col + k) : 0.f, sx, real && c.bias ? H::load(c.bias, ch0 + col + k) : 0.f);
         }
-        grp::quick_activation(v, c.act);
+        activate(v, c.act);
         store_y8<H>(c.y, (static_cast<int64_t>(tl.lo) + r) * c.ldy + col, v, p.wide_y, c.O - col);
       }
     }

@@ -22,16 +22,16 @@ static void look(const TcShape& c) {
     CHECK(p.tiles * p.split * p.cg >= (int64_t{1} << 31));
     return;
   }
-  const int own = p.TN / p.cg, wide = p.TN < 32 ? 32 : p.TN;
+  const int own = p.TN / p.cg, wide = (p.TN + 31) / 32 * 32;
   // tiles: whole MMA widths, boxes and atoms of the swizzle
   CHECK(p.cg == 1 || p.cg == 2);
   CHECK(p.TN >= 16 && p.TN <= 256 && p.TN % (p.cg == 2 ? 32 : 16) == 0 && (p.cg == 2 || p.TN <= 128));
   CHECK(p.TM % 8 == 0 && p.TM >= 32 && p.TM <= 128 && own % 8 == 0);
   CHECK(p.KS == 1 || p.KS == 2 || p.KS == 4);
-  CHECK(p.TN <= 32 || (wide % 32 == 0) || p.cg == 1);
+  CHECK(accumulator_columns(p.TN) == wide);
   // accumulators: two, of a split one, what the drain reads at once inside of them
   CHECK(p.columns >= 32 && p.columns <= 512 && (p.columns & (p.columns - 1)) == 0);
-  CHECK((p.split > 1 ? p.TN : wide + ((p.TN + 31) / 32) * 32) <= p.columns);
+  CHECK((p.split > 1 ? 1 : 2) * wide <= p.columns);
   // ring and shared memory
   const int stage = p.KS * (p.TM + own) * 128;
   CHECK(p.ring >= 2 && p.ring <= kMaxRing);
