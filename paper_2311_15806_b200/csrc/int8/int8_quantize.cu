@@ -86,7 +86,7 @@ __device__ __forceinline__ float as_number(uint32_t magnitude) {   // of Run::ma
 
 // P threads of a row; a block of 256 threads, or of P where that is more.
 template <int SRC, int W, int P>
-__global__ void __launch_bounds__(P > 256 ? P : 256) int8_quantize_kernel(const QuantArgs a) {
+__global__ void __launch_bounds__(P > 256 ? P : 256, (W == 8 ? 1280 : 1024) / (P > 256 ? P : 256)) int8_quantize_kernel(const QuantArgs a) {
   constexpr int kThreads = P > 256 ? P : 256, kRows = kThreads / P, kRuns = kQHeld / W;
   constexpr int kSize = SRC == PIPE_DTYPE_FP32 ? 4 : 2;
   __shared__ uint32_t most_s[kThreads / 32];
