@@ -14,6 +14,7 @@ namespace lpb {
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 constexpr float kFar = -1e30f;     // differences below have probability 0 at every scale (2^-20 at least)
+constexpr float kExact = 16777216.f;   // numbers up to it are rounded by one at most
 constexpr int kFound = 544;        // most logits that are ranked: no less than a cluster's PIPE_MAX_TOP each
 constexpr int kCluster = 8;
 constexpr int kWide = 512, kNarrow = 128, kResident = 1536;   // threads of a CTA, and of an SM
@@ -71,7 +72,7 @@ struct Vec {
     else if constexpr (SRC == PIPE_DTYPE_BF16) return __uint_as_float(i & 1 ? u[i >> 1] & 0xFFFF0000u : u[i >> 1] << 16);
     else return grp::Fp16::to_float(static_cast<uint16_t>(i & 1 ? u[i >> 1] >> 16 : u[i >> 1]));
   }
-  // (bf16: what is below -1e30 made that, a NaN kept)
+  // (bf16: what is below kFar, -Inf among it, made that, a NaN kept)
   __device__ __forceinline__ void raise() {
     if constexpr (SRC == PIPE_DTYPE_BF16) {
 #pragma unroll
@@ -168,7 +169,6 @@ __device__ __forceinline__ uint32_t key_in(Entry e) { return static_cast<uint32_
 __device__ __forceinline__ int place_in(Entry e) { return static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(e)); }
 
 constexpr int kGroups = 256;
-
 
 // Shared memory of the search for the alternatives.
 template <int B>
@@ -445,12 +445,13 @@ __global__ void __launch_bounds__(B, kResident / B) logprobs_kernel(const Args a
     if (token >= 0 && token < a.V) given = logit<SRC>(p.row, token);
   }
   // The pass.  z is formed by one fused operation, c l - ref with ref = c m rounded: the same ref for all, so that what its rounding adds to
-  // every z cancels in the end.  For that the largest logit may not be beyond 1e29 (see below), and smaller logits than -1e30 count as that.
+  // every z, one at most as long as c m is within kExact, cancels in the end.  Beyond that ref stays at kExact: the sums are then no use, but
+  // nothing in them is infinite as long as m is negative, and they are made anew (below) should m stay there.
   Sums own = {-INFINITY, 0.f, 0.f};
-  float ref = kFar * c;
+  float ref = -kExact;
   f32x2 s2 = both_f2(0.f), h2 = both_f2(0.f);
   auto grow = [&](float m) {   // a new largest logit
-    const float to = fminf(fmaxf(m, kFar), -kFar) * c, z = fmaxf(ref - to, kFar), f = ex2(z);
+    const float to = fminf(fmaxf(m * c, -kExact), kExact), z = ref - to, f = ex2(z);
     if (ENT) h2 = mul_f2(fma_f2(s2, both_f2(z), h2), both_f2(f));
     s2 = mul_f2(s2, both_f2(f));
     own.m = m;
@@ -514,13 +515,12 @@ __global__ void __launch_bounds__(B, kResident / B) logprobs_kernel(const Args a
     unpack_f2(h2, x, y);
     own.h = x + y;
   }
-  if (fabsf(mine) <= 1e29f) {   // from ref to c m
+  if (fabsf(mine * c) <= kExact) {   // from ref to c m
     const float z = fmaf(mine, c, -ref), f = ex2(-z);
     own.h = (own.h - own.s * z) * f;
     own.s *= f;
   } else if (fabsf(mine) <= 3.402823466e38f) {
-    // logits of a size at which c l may be beyond the type's range (masked by its lowest number, all that this thread has): once more, by
-    // differences
+    // (a thread that has nothing but masked by large negative numbers, as a rule): once more, by differences
     own.s = own.h = 0.f;
     auto add = [&](float l) {
       const float z = fmaxf(fmaxf(l - mine, kFar) * c, kFar), e = ex2(z);

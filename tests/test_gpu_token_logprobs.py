@@ -232,3 +232,26 @@ def test_the_head_of_a_model_and_what_it_says():
     _ok()
     for a, b in zip(replayed, (logits, lp, ent, top, tlp)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("low", [-1e4, -1e7, -1e9, -1e20, -1e29, -1e30, -3e38])
+@pytest.mark.parametrize("scale", [1.0, 2.0 ** -20, 2.0 ** 20])
+def test_masks_of_any_large_number(dtype, low, scale):
+    """Tokens masked by adding or writing a large negative number, before others and behind, in parts of a row and in all of it."""
+    gen = _gen(11)
+    T, V = 8, 40009
+    l = torch.randn((T, V), generator=gen) * 3
+    l[0, :V - 50] = low
+    l[1, 50:] = low
+    l[2, torch.rand((V,), generator=gen) < 0.999] = low
+    l[3] = low
+    l[4] = low
+    l[4, 20000] = low * 0.5
+    l[5, ::2] = -math.inf
+    l[5, 1::4] = low
+    l[6, 8192:8192 * 4] = low
+    l[7] += -low * 2.0 ** -6                              # large positive ones
+    l = l.to(R.TYPES[dtype])
+    _check(l, torch.randint(0, V, (T, 2), generator=gen, dtype=torch.int32), 4, scale, tag=f"{low}")
+    _check(l[:, :3001].contiguous(), torch.randint(0, 3001, (T, 2), generator=gen, dtype=torch.int32), 4, scale, tag=f"{low} short")
