@@ -17,7 +17,7 @@ constexpr float kFar = -1e30f;     // differences below have probability 0 at ev
 constexpr float kExact = 16777216.f;   // numbers up to it are rounded by one at most
 constexpr int kFound = 544;        // most logits that are ranked: no less than a cluster's PIPE_MAX_TOP each
 constexpr int kCluster = 8;
-constexpr int kWide = 512, kNarrow = 128, kResident = 1536;   // threads of a CTA, and of an SM
+constexpr int kWide = 512, kMiddle = 256, kNarrow = 128, kResident = 1536;   // threads of a CTA, and of an SM
 constexpr int kAhead = 4;                                      // vectors that a thread has in flight
 static_assert(kFound >= kCluster * PIPE_MAX_TOP && kFound % 2 == 0, "");
 
@@ -590,8 +590,9 @@ __global__ void __launch_bounds__(B, kResident / B) logprobs_kernel(const Args a
 
 using Kernel = void (*)(Args);
 template <int SRC>
-static Kernel logprobs_of(bool wide, bool entropy) {
-  if (wide) return entropy ? logprobs_kernel<SRC, kWide, true> : logprobs_kernel<SRC, kWide, false>;
+static Kernel logprobs_of(int threads, bool entropy) {
+  if (threads == kWide) return entropy ? logprobs_kernel<SRC, kWide, true> : logprobs_kernel<SRC, kWide, false>;
+  if (threads == kMiddle) return entropy ? logprobs_kernel<SRC, kMiddle, true> : logprobs_kernel<SRC, kMiddle, false>;
   return entropy ? logprobs_kernel<SRC, kNarrow, true> : logprobs_kernel<SRC, kNarrow, false>;
 }
 
@@ -618,16 +619,22 @@ extern "C" pipe_status pipe_token_logprobs(const void* d_logits, int32_t dtype, 
   if (T == 0) return PIPE_OK;
   lpb::Args a = {d_logits, T, ldl, V, scale, d_tokens, n, d_logprobs, d_entropy, k, d_top, d_top_logprobs, device_status_word()};
   if (!a.status) return grp::runtime_failed();
-  // Rows of more than 32 KB go to CTAs of 512 threads, few of them to several each; shorter ones to CTAs of 128.
+  // Threads of a row: a CTA's joins, search and ranking take some 5 us whatever its size, so that many rows want many small CTAs on an SM,
+  // a long row one that reads it fast, and rows that are all on the chip at once as many threads as there are.  With 10 alternatives and the
+  // entropy (us; 128, 256 and 512 threads): 4000 rows of 16 KB 40, 43, 69, of 64 KB 77, 78, 99, of 128 KB 142, 118, 127, of 256 KB 258, 214,
+  // 198; 300 rows of 16 KB 9.4, 7.2, 8.5, of 64 KB 16.1, 12.7, 13.8; 100 rows of 64 KB 12.0, 9.7, 9.1.
   const int64_t bytes = static_cast<int64_t>(V) * (dtype == PIPE_DTYPE_FP32 ? 4 : 2);
-  const bool wide = bytes > 32768;
+  int threads = bytes <= 32768 ? lpb::kNarrow : (bytes <= 163840 ? lpb::kMiddle : lpb::kWide);
+  if (T <= 3 * kPlanSMs && bytes > 8192 && threads < lpb::kMiddle) threads = lpb::kMiddle;
+  if (T <= kPlanSMs && bytes > 16384) threads = lpb::kWide;
+  // and a few long rows several CTAs (1, 2, 4 and 8): a row of 256 KB 11.4, 10.4, 9.3, 8.6; 60 rows 15.3, 13.6, 15.4, 20.6
   int ctas = 1;
-  while (wide && ctas < lpb::kCluster && bytes / ctas > 16384 && T * ctas * 2 <= lpb::kResident / lpb::kWide * kPlanSMs) ctas *= 2;
-  const lpb::Kernel kern = dtype == PIPE_DTYPE_FP32 ? lpb::logprobs_of<PIPE_DTYPE_FP32>(wide, d_entropy != nullptr)
-                                                    : (dtype == PIPE_DTYPE_BF16 ? lpb::logprobs_of<PIPE_DTYPE_BF16>(wide, d_entropy != nullptr)
-                                                                                : lpb::logprobs_of<PIPE_DTYPE_FP16>(wide, d_entropy != nullptr));
+  while (threads == lpb::kWide && ctas < lpb::kCluster && bytes / ctas > 16384 && T * ctas * 2 <= lpb::kResident / lpb::kWide * kPlanSMs) ctas *= 2;
+  const lpb::Kernel kern = dtype == PIPE_DTYPE_FP32 ? lpb::logprobs_of<PIPE_DTYPE_FP32>(threads, d_entropy != nullptr)
+                                                    : (dtype == PIPE_DTYPE_BF16 ? lpb::logprobs_of<PIPE_DTYPE_BF16>(threads, d_entropy != nullptr)
+                                                                                : lpb::logprobs_of<PIPE_DTYPE_FP16>(threads, d_entropy != nullptr));
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (launch_overlapped(kern, dim3(static_cast<unsigned>(T * ctas)), wide ? lpb::kWide : lpb::kNarrow, ctas, true, s, a) != cudaSuccess) return grp::runtime_failed();
+  if (launch_overlapped(kern, dim3(static_cast<unsigned>(T * ctas)), threads, ctas, true, s, a) != cudaSuccess) return grp::runtime_failed();
   count_launch(1);
   take_expansion_mark(s);
   return launch_status();

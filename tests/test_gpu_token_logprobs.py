@@ -255,3 +255,37 @@ def test_masks_of_any_large_number(dtype, low, scale):
     l = l.to(R.TYPES[dtype])
     _check(l, torch.randint(0, V, (T, 2), generator=gen, dtype=torch.int32), 4, scale, tag=f"{low}")
     _check(l[:, :3001].contiguous(), torch.randint(0, 3001, (T, 2), generator=gen, dtype=torch.int32), 4, scale, tag=f"{low} short")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("k", [0, 10, 64])
+@pytest.mark.parametrize("T,V", [(460, 3001), (460, 12007), (460, 40009), (170, 90001), (46, 40009), (20, 12007)])
+def test_rows_for_every_number_of_threads(dtype, k, T, V):
+    """Few and many rows, short and long ones: CTAs of 128, 256 and 512 threads, one or more to a row.  Every row is one of ten kinds."""
+    gen = _gen(12)
+    kinds = 10
+    l = torch.randn((kinds, V), generator=gen) * 3
+    l[1, torch.rand((V,), generator=gen) < 0.99] = -math.inf
+    l[2] = -math.inf
+    l[3] = 1.5
+    l[4] = torch.randint(0, 4, (V,), generator=gen).float()
+    l[5] = torch.arange(V) / 64.0
+    l[6] = -torch.arange(V) / 64.0
+    l[7, :V - 3] = -math.inf
+    l[8, V // 2:V // 2 + 200] = 60.0
+    l[9, 5:] = -60000.0
+    l = l.to(R.TYPES[dtype])
+    tokens = torch.randint(-1, V + 1, (kinds, 3), generator=gen, dtype=torch.int32)
+    tokens[7, 0] = V - 1
+    on = torch.full((T, V + 5), math.nan, dtype=R.TYPES[dtype], device="cuda")[:, :V]
+    row = torch.arange(T) % kinds
+    on.copy_(l.cuda()[row.cuda()])
+    lp, ent, top, tlp = _call(on, tokens[row].contiguous(), k)
+    _ok()
+    w_lp, w_ent, w_ids, w_top, tol, ent_tol = (w[row] for w in R.logprobs(l, tokens, max(k, 1), 1.0))
+    size = lambda w: torch.where(torch.isinf(w), 0.0, w.abs()) + 1  # noqa: E731
+    R.close(lp, w_lp, tol, size(w_lp), f"{T} {V} lp")
+    R.close(ent, w_ent, ent_tol, 1 + w_ent.abs(), f"{T} {V} entropy")
+    if k:
+        assert torch.equal(top.cpu(), w_ids)
+        R.close(tlp, w_top, tol, size(w_top), f"{T} {V} top")
