@@ -15,6 +15,7 @@ namespace lpb {
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 constexpr float kFar = -1e30f;     // differences below have probability 0 at every scale (2^-20 at least)
 constexpr float kExact = 16777216.f;   // numbers up to it are rounded by one at most
+constexpr uint32_t kOutside = 0x7F800001u;   // a given token that is none (of NaNs there is one)
 constexpr int kFound = 544;        // most logits that are ranked: no less than a cluster's PIPE_MAX_TOP each
 constexpr int kCluster = 8;
 constexpr int kWide = 512, kMiddle = 256, kNarrow = 128, kResident = 1536;   // threads of a CTA, and of an SM
@@ -125,8 +126,12 @@ struct Sums {
 template <int N>
 __device__ __forceinline__ Sums joined(const Sums& own, float c) {
   Sums r = own;
+  if constexpr (N == 32) {
+    asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r.m) : "f"(own.m));
+  } else {
 #pragma unroll
-  for (int o = N / 2; o; o >>= 1) r.m = max_nan(r.m, __shfl_xor_sync(0xffffffffu, r.m, o));
+    for (int o = N / 2; o; o >>= 1) r.m = max_nan(r.m, __shfl_xor_sync(0xffffffffu, r.m, o));
+  }
   const float z = fmaxf(fmaxf(own.m - fmaxf(r.m, -3.402823466e38f), kFar) * c, kFar), f = ex2(z);
   r.s = own.s * f;
   r.h = (own.h + own.s * z) * f;
@@ -147,15 +152,16 @@ struct Part {
   int head, tail, first, end, tail_at, head_all;
 };
 template <int SRC>
-__device__ __forceinline__ Part part_of(const Args& a, int64_t t, int crank, int ctas) {
+__device__ __forceinline__ Part part_of(const Args& a, int64_t t, int crank, int ctas) {   // (ctas: a power of two)
   constexpr int kLogits = Vec<SRC>::kLogits, kSize = Vec<SRC>::kSize;
   Part p;
   p.row = static_cast<const uint8_t*>(a.logits) + t * a.ldl * kSize;
   p.head_all = min(a.V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(p.row) & 15)) & 15) / kSize);
   p.vectors = p.row + p.head_all * kSize;
   const int all = (a.V - p.head_all) / kLogits;
-  p.first = static_cast<int>(static_cast<int64_t>(all) * crank / ctas);
-  p.end = static_cast<int>(static_cast<int64_t>(all) * (crank + 1) / ctas);
+  const int shift = 31 - __clz(ctas);
+  p.first = static_cast<int>(static_cast<int64_t>(all) * crank >> shift);
+  p.end = static_cast<int>(static_cast<int64_t>(all) * (crank + 1) >> shift);
   p.head = crank == 0 ? p.head_all : 0;
   p.tail_at = p.head_all + all * kLogits;
   p.tail = crank == ctas - 1 ? a.V - p.tail_at : 0;
@@ -168,75 +174,100 @@ __device__ __forceinline__ Entry entry_of(float l, int i) { return (static_cast<
 __device__ __forceinline__ uint32_t key_in(Entry e) { return static_cast<uint32_t>(e >> 32); }
 __device__ __forceinline__ int place_in(Entry e) { return static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(e)); }
 
-constexpr int kGroups = 256;
+constexpr int kGroups = 256, kFewGroups = 32;
+constexpr int kFewAlternatives = 20;   // a bound from kFewGroups groups: 31 logits are found for the 20 largest, on average, 12 for 10
+constexpr int kFewFound = 64;          // that one warp ranks, or a CTA hands to its cluster's first
+static_assert(kFewFound >= PIPE_MAX_TOP && kCluster * kFewFound <= kFound, "");
 
 // Shared memory of the search for the alternatives.
 template <int B>
 struct Search {
   alignas(16) Entry entry[kFound + 2];
-  uint32_t group[kGroups];               // the largest logits of groups of threads, as keys
-  int found;
+  alignas(16) uint32_t group[kGroups];   // the largest logits of groups of threads, as keys
+  int found, kept;
   uint32_t least;
   int run[2][B / 32];
 };
 
-// take(in, logit, place), by whole warps, for the logits of this CTA's part that may be not below `least` (of the key of a number; in: one
-// that is not), of threads whose largest, `own`, is not.  Where a thread has many vectors its warp looks at them, those of four threads at
-// a time; otherwise it looks itself.
-template <int SRC, int B, class F>
-__device__ __forceinline__ void look_again(const Part& p, uint32_t own, uint32_t least, F take) {
+// The logits of this CTA's part that are not below `least` (the key of a number), of threads whose largest, `own`, is not: entered, as long
+// as there is room, and counted in s.found, or (COUNT) this thread's finds counted only.  Four vectors of a lane at a time: its own where no
+// thread has more, otherwise the warp's lanes share out those of four threads.
+// (All that follows the pass is written for few instructions: with 80 KB of them, as it was, every step waited for code.)
+template <int SRC, int B, bool COUNT>
+__device__ __forceinline__ int look_again(Search<B>& s, const Part& p, uint32_t own, uint32_t least) {
   constexpr int kLogits = Vec<SRC>::kLogits;
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, first = p.first + static_cast<int>(threadIdx.x);
   const float bound = number_of(least);
-  const bool mine = own >= least;
-  uint32_t which = __ballot_sync(0xffffffffu, mine);
-  if (!which) return;
-  auto look = [&](int v0, int v1, int v2, int v3) {   // at these vectors (p.end: none)
-    const int v[4] = {v0, v1, v2, v3};
-    Vec<SRC> w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (v[j] < p.end) w[j].load(p.vectors + v[j] * int64_t{16});
-      else w[j].fill();
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const Vec<SRC> one[1] = {w[j]};
-      if (!__any_sync(0xffffffffu, Vec<SRC>::largest(one) >= bound)) continue;
-#pragma unroll
-      for (int i = 0; i < kLogits; ++i) take(w[j].at(i) >= bound, w[j].at(i), p.head_all + v[j] * kLogits + i);
-    }
+  const bool mine = own >= least, few = p.end - p.first <= 4 * B;
+  int finds = 0;
+  auto enter = [&](int at, float l, int place) {
+    if (at < kFound) s.entry[at] = entry_of(l, place);
   };
-  if (p.end - p.first <= 4 * B) {
-    const int v = mine ? p.first + static_cast<int>(threadIdx.x) : p.end;
-    look(v, min(v + B, p.end), min(v + 2 * B, p.end), min(v + 3 * B, p.end));
-  } else {
-    while (which) {
-      int t[4];
+  uint32_t which = __ballot_sync(0xffffffffu, mine);
+  while (which) {
+    int from[4];   // a lane's vectors, one of each (p.end: none)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        t[j] = which ? p.first + static_cast<int>(threadIdx.x & ~31u) + __ffs(which) - 1 : p.end;
+    for (int j = 0; j < 4; ++j) {
+      if (few) {
+        from[j] = mine ? first + j * B : p.end;
+      } else {
+        from[j] = which ? first - lane + __ffs(which) - 1 + lane * B : p.end;
         which &= which - 1;
       }
-      for (int at = 0; p.first + at < p.end; at += 32 * B) {   // (at most 2^28 vectors)
-        const int more = at + lane * B;
-        look(min(t[0] + more, p.end), min(t[1] + more, p.end), min(t[2] + more, p.end), min(t[3] + more, p.end));
-      }
     }
-  }
+    if (few) which = 0;
+    for (int at = 0; p.first + at < p.end; at += 32 * B) {   // (at most 2^28 vectors)
+      Vec<SRC> w[4];
 #pragma unroll
-  for (int of = 0; of < 2; ++of) {
-    const int n = of ? p.tail : p.head, at = (of ? p.tail_at : 0) + static_cast<int>(threadIdx.x);
-    if (static_cast<int>(threadIdx.x & ~31u) < n) {
-      const float l = static_cast<int>(threadIdx.x) < n ? logit<SRC>(p.row, at) : -INFINITY;
-      take(l >= bound, l, at);
+      for (int j = 0; j < 4; ++j) {
+        if (from[j] + at < p.end) w[j].load(p.vectors + (from[j] + at) * int64_t{16});
+        else w[j].fill();
+      }
+      uint32_t hits = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < kLogits; ++i) hits |= w[j].at(i) >= bound ? 1u << (j * kLogits + i) : 0u;
+      if (COUNT) {
+        finds += __popc(hits);
+      } else if (hits) {
+        int to = atomicAdd(&s.found, __popc(hits));
+        for (; hits; hits &= hits - 1, ++to) {
+          const int bit = __ffs(hits) - 1, j = bit / kLogits;
+          Vec<SRC> v = w[0];   // that of the hit
+          int place = from[0];
+#pragma unroll
+          for (int o = 1; o < 4; ++o)
+            if (j == o) {
+              v = w[o];
+              place = from[o];
+            }
+          float l = v.at(0);
+#pragma unroll
+          for (int i = 1; i < kLogits; ++i)
+            if (bit % kLogits == i) l = v.at(i);
+          enter(to, l, p.head_all + (place + at) * kLogits + bit % kLogits);
+        }
+      }
+      if (few) break;
     }
   }
+#pragma unroll 1
+  for (int of = 0; of < 2; ++of) {
+    if (static_cast<int>(threadIdx.x) >= (of ? p.tail : p.head)) continue;
+    const int at = (of ? p.tail_at : 0) + static_cast<int>(threadIdx.x);
+    const float l = logit<SRC>(p.row, at);
+    if (!(l >= bound)) continue;
+    if (COUNT) ++finds;
+    else enter(atomicAdd(&s.found, 1), l, at);
+  }
+  return finds;
 }
 
-// The `count` entries ranked: out[i], i < k, with zeros where there are none.  (A barrier has to stand before and behind.)
-template <int B>
-__device__ __forceinline__ void rank(Search<B>& s, int count, int k, Entry* out) {
+// put(i, entry) for the k largest of the entries, or all of them, i their rank, by threads from .. of the CTA or, where they are few, by the
+// first warp alone.  (A barrier has to stand before, and behind unless they are few.)
+template <int B, class F>
+__device__ __forceinline__ void rank(Search<B>& s, int count, int k, F put) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (count > 2 * k + 64) {
     // first brought down to some more than k by one warp, by halving between the least and the largest of their keys
@@ -273,15 +304,17 @@ __device__ __forceinline__ void rank(Search<B>& s, int count, int k, Entry* out)
         kept += __popc(m);
         __syncwarp();
       }
-      if (lane == 0) s.found = kept;
+      if (lane == 0) s.kept = kept;
     }
     __syncthreads();
-    count = s.found;
+    count = s.kept;
   }
-  for (int i = threadIdx.x; i < k; i += B) out[i] = 0;
-  if (threadIdx.x == 0) s.entry[count] = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < count; i += B) {
+  const bool few = count <= kFewFound;
+  if (few && warp != 0) return;
+  if (threadIdx.x == 0) s.entry[count] = 0;   // (read with the last one where their number is odd)
+  if (few) __syncwarp();
+  else __syncthreads();
+  for (int i = threadIdx.x; i < count; i += few ? 32 : B) {
     const Entry e = s.entry[i];
     int above = 0;
 #pragma unroll 4
@@ -289,21 +322,27 @@ __device__ __forceinline__ void rank(Search<B>& s, int count, int k, Entry* out)
       const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(s.entry + j);
       above += (two.x > e) + (two.y > e);
     }
-    if (e != 0 && above < k) out[above] = e;
+    if (above < k) put(above, e);
   }
 }
 
-// Fills s.entry with logits of this CTA's part, in any order, the k first of them among these or all that there are; returns their number,
-// kFound at most.  m: the largest of this thread's.
-template <int SRC, int B>
-__device__ int search(Search<B>& s, const Part& p, float m, int k) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint32_t own = key_of(m);
+// The largest logits of groups of threads, for search (a barrier has to stand between).  m: the largest of this thread's.
+template <int B>
+__device__ __forceinline__ bool few_groups(const Part& p, int k) {   // (every group has logits then)
+  return k <= kFewAlternatives && p.end - p.first >= B;
+}
+template <int B>
+__device__ __forceinline__ void group(Search<B>& s, const Part& p, float m, int k) {
+  uint32_t most = key_of(m);
   if (threadIdx.x == 0) s.found = 0;
-  // A bound for the k-th largest: of disjoint groups of threads at least k have one as large, by halving until those are few enough (or down
-  // to kNoneKey + 1, the least that is not masked, where there are fewer than k).
+  if (few_groups<B>(p, k)) {
+    constexpr int kSize = B / kFewGroups;
+#pragma unroll
+    for (int o = 1; o < kSize; o *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    if (threadIdx.x % kSize == 0) s.group[threadIdx.x / kSize] = most;
+    return;
+  }
   int size = 1;
-  uint32_t most = own;
   if (B > kGroups) {
     most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
     size = 2;
@@ -315,55 +354,19 @@ __device__ int search(Search<B>& s, const Part& p, float m, int k) {
   for (int i = threadIdx.x; i < kGroups; i += B)
     if (i >= B / size) s.group[i] = 0;
   if (threadIdx.x % size == 0) s.group[threadIdx.x / size] = most;
-  __syncthreads();
-  if (warp == 0) {
-    uint32_t mine[kGroups / 32], lo = kNoneKey + 1, hi = 0;
-#pragma unroll
-    for (int i = 0; i < kGroups / 32; ++i) {
-      mine[i] = s.group[32 * i + lane];
-      hi = max(hi, mine[i]);
-    }
-    if (k <= 32) lo = max(lo, __reduce_min_sync(0xffffffffu, hi));   // (every lane has a group as large as that)
-    hi = __reduce_max_sync(0xffffffffu, hi);
-    int n = kGroups;
-    while (lo < hi && n > k + (k >> 2) + 2) {
-      const uint32_t mid = lo + (hi - lo + 1) / 2;
-      int c = 0;
-#pragma unroll
-      for (int i = 0; i < kGroups / 32; ++i) c += mine[i] >= mid;
-      c = __reduce_add_sync(0xffffffffu, c);
-      if (c >= k) {
-        lo = mid;
-        n = c;
-      } else {
-        hi = mid - 1;
-      }
-    }
-    if (lane == 0) s.least = lo;
-  }
-  __syncthreads();
-  uint32_t least = s.least;
-  // (the places of a warp's finds at once)
-  auto keep = [&](bool in, float l, int i) {
-    const uint32_t m = __ballot_sync(0xffffffffu, in);
-    if (!m) return;
-    int at = 0;
-    if (lane == 0) at = atomicAdd(&s.found, __popc(m));
-    at = __shfl_sync(0xffffffffu, at, 0) + __popc(m & ((1u << lane) - 1));
-    if (in && at < kFound) s.entry[at] = entry_of(l, i);
-  };
-  look_again<SRC, B>(p, own, least, keep);
-  __syncthreads();
-  if (s.found <= kFound) return s.found;
+}
 
-  // Too many.  The key of the k-th largest, by halving between that bound and the largest.
+// Where more logits than there is room for are not below the bound: fills s.entry with the k first of this CTA's part, in any order.
+template <int SRC, int B>
+__device__ __noinline__ int search_by_halves(Search<B>& s, const Part p, uint32_t own, uint32_t least, int k) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // The key of the k-th largest, by halving between that bound and the largest.
   uint32_t hi = 0;
-  for (int g = lane; g < kGroups; g += 32) hi = max(hi, s.group[g]);
+  for (int g = lane; g < (few_groups<B>(p, k) ? kFewGroups : kGroups); g += 32) hi = max(hi, s.group[g]);
   hi = __reduce_max_sync(0xffffffffu, hi);
   for (int turn = 0; least < hi; turn ^= 1) {   // (the same in all threads; at least k logits reach `least`)
     const uint32_t mid = least + (hi - least + 1) / 2;
-    int c = 0;
-    look_again<SRC, B>(p, own, mid, [&](bool in, float, int) { c += in; });
+    int c = look_again<SRC, B, true>(s, p, own, mid);
     c = __reduce_add_sync(0xffffffffu, c);
     if (lane == 0) s.run[turn][warp] = c;
     __syncthreads();
@@ -377,7 +380,7 @@ __device__ int search(Search<B>& s, const Part& p, float m, int k) {
   __syncthreads();
   if (threadIdx.x == 0) s.found = 0;
   __syncthreads();
-  look_again<SRC, B>(p, own, least + 1, keep);
+  look_again<SRC, B, false>(s, p, own, least + 1);
   __syncthreads();
   int have = s.found;
   constexpr int kLogits = Vec<SRC>::kLogits;
@@ -421,6 +424,59 @@ __device__ int search(Search<B>& s, const Part& p, float m, int k) {
   return have;
 }
 
+// Fills s.entry with logits of this CTA's part, in any order, the k first of them among these or all that there are; returns their number,
+// kFound at most.  m: the largest of this thread's.
+template <int SRC, int B>
+__device__ __forceinline__ int search(Search<B>& s, const Part& p, float m, int k) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t own = key_of(m);
+  // A bound for the k-th largest: of disjoint groups of threads at least k have one as large (or kNoneKey + 1, the least that is not masked,
+  // where there are fewer than k).  Of 32 groups that is the k-th largest, of more one not far below it, by halving.
+  if (warp == 0) {
+    uint32_t lo = kNoneKey + 1;
+    if (few_groups<B>(p, k)) {
+      const uint32_t mine = s.group[lane];
+      int above = 0;
+#pragma unroll
+      for (int i = 0; i < kFewGroups; i += 4) {
+        const uint4 four = *reinterpret_cast<const uint4*>(s.group + i);
+        above += (four.x > mine) + (four.y > mine) + (four.z > mine) + (four.w > mine);
+      }
+      lo = max(lo, __reduce_min_sync(0xffffffffu, above < k ? mine : ~0u));
+    } else {
+      uint32_t mine[kGroups / 32], hi = 0;
+#pragma unroll
+      for (int i = 0; i < kGroups / 32; ++i) {
+        mine[i] = s.group[32 * i + lane];
+        hi = max(hi, mine[i]);
+      }
+      if (k <= 32) lo = max(lo, __reduce_min_sync(0xffffffffu, hi));   // (every lane has a group as large as that)
+      hi = __reduce_max_sync(0xffffffffu, hi);
+      int n = kGroups;
+      while (lo < hi && n > k + (k >> 2) + 2) {
+        const uint32_t mid = lo + (hi - lo + 1) / 2;
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < kGroups / 32; ++i) c += mine[i] >= mid;
+        c = __reduce_add_sync(0xffffffffu, c);
+        if (c >= k) {
+          lo = mid;
+          n = c;
+        } else {
+          hi = mid - 1;
+        }
+      }
+    }
+    if (lane == 0) s.least = lo;
+  }
+  __syncthreads();
+  const uint32_t least = s.least;
+  look_again<SRC, B, false>(s, p, own, least);
+  __syncthreads();
+  const int found = s.found;
+  return found <= kFound ? found : search_by_halves<SRC, B>(s, p, own, least, k);
+}
+
 // B threads a CTA; a cluster of CTAs a row.  ENT: the entropy is wanted.
 template <int SRC, int B, bool ENT>
 __global__ void __launch_bounds__(B, kResident / B) logprobs_kernel(const Args a) {
@@ -428,22 +484,26 @@ __global__ void __launch_bounds__(B, kResident / B) logprobs_kernel(const Args a
   __shared__ Search<B> search_s;
   __shared__ Sums warp_s[B / 32];
   __shared__ Sums own_s;                     // this CTA's
+  __shared__ int count_s;
   __shared__ Entry top_s[PIPE_MAX_TOP];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int ctas = grp::cluster_ctas(), crank = grp::cluster_rank();
-  const int64_t t = blockIdx.x / ctas;
+  const int64_t t = blockIdx.x >> (31 - __clz(ctas));
   const Part p = part_of<SRC>(a, t, crank, ctas);
   const float c = a.scale * kLog2e;
   grid_wait();
   grid_release();
 
   // a given token and its logit, on their way while the row is read
-  int token = -1;
-  float given = 0.f;
-  if (crank == 0 && static_cast<int>(threadIdx.x) < a.n) {
-    token = __ldcg(a.tokens + t * a.n + threadIdx.x);
-    if (token >= 0 && token < a.V) given = logit<SRC>(p.row, token);
-  }
+  const int turn = static_cast<int>(threadIdx.x + 32) & (B - 1);   // (the last warp's first: the first one has the alternatives' bound to find)
+  auto given_of = [&](int64_t at) {   // its bits, or kOutside, which no number has
+    const int token = __ldcg(a.tokens + at);
+    if (token < 0 || token >= a.V) return kOutside;
+    const float l = logit<SRC>(p.row, token);
+    return __float_as_uint(l == l ? l : __int_as_float(0x7FC00000));
+  };
+  uint32_t given = kOutside;
+  if (crank == 0 && turn < a.n) given = given_of(t * a.n + turn);
   // The pass.  z is formed by one fused operation, c l - ref with ref = c m rounded: the same ref for all, so that what its rounding adds to
   // every z, one at most as long as c m is within kExact, cancels in the end.  Beyond that ref stays at kExact: the sums are then no use, but
   // nothing in them is infinite as long as m is negative, and they are made anew (below) should m stay there.
@@ -537,55 +597,87 @@ __global__ void __launch_bounds__(B, kResident / B) logprobs_kernel(const Args a
     if (static_cast<int>(threadIdx.x) < p.tail) add(logit<SRC>(p.row, p.tail_at + static_cast<int>(threadIdx.x)));
   }
   own = joined<32>(own, c);
+  if (a.k > 0) group(search_s, p, mine, a.k);
   if (lane == 0) warp_s[warp] = own;
   __syncthreads();
   own = joined<B / 32>(warp_s[lane & (B / 32 - 1)], c);   // (in every lane)
-  if (threadIdx.x == 0) own_s = own;
-  if (a.k > 0) {
-    // (a row that is no distribution has no alternatives, in whichever CTA that shows)
-    const int count = own.m <= 3.402823466e38f ? search<SRC, B>(search_s, p, mine, a.k) : 0;
-    __syncthreads();
-    rank<B>(search_s, count, a.k, top_s);
-  }
-  if (ctas > 1) {
-    grp::cluster_sync();
-    if (crank == 0) {
-      Sums others = {-INFINITY, 0.f, 0.f};
-      const int from = lane & (kCluster - 1);
-      if (from < ctas) others = Sums{grp::cluster_load(&own_s.m, from), grp::cluster_load(&own_s.s, from), grp::cluster_load(&own_s.h, from)};
-      own = joined<kCluster>(others, c);
-      for (int i = threadIdx.x; i < ctas * a.k; i += B) {
-        const int from = i / a.k;
-        asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(search_s.entry[i]) : "r"(grp::cluster_address(top_s + (i - from * a.k), from)) : "memory");
-      }
-    }
-    grp::cluster_sync();   // (no CTA leaves, and none ranks anew, while another one's memory is read)
-    if (crank != 0) return;
-    if (a.k > 0) rank<B>(search_s, ctas * a.k, a.k, top_s);
-  }
-  const bool bad = !(own.m <= 3.402823466e38f), none = own.m == -INFINITY;
-  const float logs = logf(own.s), nan = __int_as_float(0x7FC00000);
+  // What the row's first CTA writes, when `own` is the row's.
+  const float nan = __int_as_float(0x7FC00000);
   // (halves: the difference of two logits may be beyond the type's range where its product with the scale is not)
-  auto logprob = [&](float l) { return bad ? nan : (none || l == -INFINITY ? -INFINITY : (0.5f * l - 0.5f * own.m) * a.scale * 2.f - logs); };
-  if (threadIdx.x == 0) {
-    if (bad) raise_status(a.status, PIPE_ERR_NONFINITE);
-    if (ENT) a.entropy[t] = bad ? nan : (none ? 0.f : logs - kLn2 * own.h / own.s);
-  }
-  for (int j = threadIdx.x; j < a.n; j += B) {
-    if (j >= B) {
-      token = __ldcg(a.tokens + t * a.n + j);
-      if (token >= 0 && token < a.V) given = logit<SRC>(p.row, token);
+  auto is_bad = [&] { return !(own.m <= 3.402823466e38f); };
+  auto logprob = [&](float l, float logs) {
+    return is_bad() ? nan : (own.m == -INFINITY || l == -INFINITY ? -INFINITY : (0.5f * l - 0.5f * own.m) * a.scale * 2.f - logs);
+  };
+  auto write_sums = [&] {
+    if (turn >= max(a.n, 1)) return;
+    const float logs = logf(own.s);
+    if (turn == 0) {
+      if (is_bad()) raise_status(a.status, PIPE_ERR_NONFINITE);
+      if (ENT) a.entropy[t] = is_bad() ? nan : (own.m == -INFINITY ? 0.f : logs - kLn2 * own.h / own.s);
     }
-    a.logprobs[t * a.n + j] = token >= 0 && token < a.V ? logprob(given) : 0.f;
+    for (int j = turn; j < a.n; j += B) {
+      if (j >= B) given = given_of(t * a.n + j);
+      a.logprobs[t * a.n + j] = given != kOutside ? logprob(__uint_as_float(given), logs) : 0.f;
+    }
+  };
+  auto write_alternatives = [&](int count) {   // of the entries, and none behind them
+    for (int i = count + static_cast<int>(threadIdx.x); i < a.k; i += B) {
+      if (a.top) a.top[t * a.k + i] = -1;
+      if (a.top_logprobs) a.top_logprobs[t * a.k + i] = is_bad() ? nan : -INFINITY;
+    }
+    if (count <= 0) return;
+    const float logs = logf(own.s);
+    rank(search_s, count, a.k, [&](int i, Entry e) {
+      if (a.top) a.top[t * a.k + i] = place_in(e);
+      if (a.top_logprobs) a.top_logprobs[t * a.k + i] = logprob(number_of(key_in(e)), logs);
+    });
+  };
+  if (ctas == 1) write_sums();
+  if (ctas == 1 && a.k == 0) return;
+  // (a row that is no distribution has no alternatives, in whichever CTA that shows)
+  int count = a.k > 0 && own.m <= 3.402823466e38f ? search<SRC, B>(search_s, p, mine, a.k) : 0;
+  if (ctas == 1) {
+    write_alternatives(count);
+    return;
   }
-  if (a.k > 0) {
+  if (count > kFewFound) {
     __syncthreads();
-    for (int i = threadIdx.x; i < a.k; i += B) {
-      const Entry e = top_s[i];
-      if (a.top) a.top[t * a.k + i] = bad || e == 0 ? -1 : place_in(e);
-      if (a.top_logprobs) a.top_logprobs[t * a.k + i] = bad ? nan : (e == 0 ? -INFINITY : logprob(number_of(key_in(e))));
-    }
+    rank(search_s, count, a.k, [&](int i, Entry e) { top_s[i] = e; });
+    __syncthreads();
+    count = a.k;
+    for (int i = threadIdx.x; i < count; i += B) search_s.entry[i] = top_s[i];
   }
+  if (threadIdx.x == 0) {
+    own_s = own;
+    count_s = count;
+  }
+  grp::cluster_sync();
+  if (crank == 0) {
+    Sums others = {-INFINITY, 0.f, 0.f};
+    const int from = lane & (kCluster - 1);
+    int upto = 0;   // entries of the CTAs up to this lane's
+    if (from < ctas) {
+      others = Sums{grp::cluster_load(&own_s.m, from), grp::cluster_load(&own_s.s, from), grp::cluster_load(&own_s.h, from)};
+      upto = grp::cluster_load(&count_s, from);
+    }
+    own = joined<kCluster>(others, c);
+#pragma unroll
+    for (int d = 1; d < kCluster; d *= 2) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, d);
+      if (from >= d) upto += v;
+    }
+    // a warp for every other CTA's entries
+    for (int r = warp + 1; r < ctas; r += B / 32) {
+      const int at = __shfl_sync(0xffffffffu, upto, r - 1), n = __shfl_sync(0xffffffffu, upto, r) - at;
+      for (int i = lane; i < n; i += 32)
+        asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(search_s.entry[at + i]) : "r"(grp::cluster_address(search_s.entry + i, r)) : "memory");
+    }
+    count = __shfl_sync(0xffffffffu, upto, kCluster - 1);
+  }
+  grp::cluster_sync();   // (no CTA leaves while another reads its memory)
+  if (crank != 0) return;
+  write_sums();
+  write_alternatives(is_bad() ? 0 : count);
 }
 
 using Kernel = void (*)(Args);
