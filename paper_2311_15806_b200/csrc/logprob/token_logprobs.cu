@@ -18,7 +18,7 @@ constexpr float kExact = 16777216.f;   // numbers up to it are rounded by one at
 constexpr uint32_t kOutside = 0x7F800001u;   // a given token that is none (of NaNs there is one)
 constexpr int kFound = 544;        // most logits that are ranked: no less than a cluster's PIPE_MAX_TOP each
 constexpr int kCluster = 8;
-constexpr int kWide = 512, kMiddle = 256, kNarrow = 128, kResident = 1536;   // threads of a CTA, and of an SM
+constexpr int kWide = 512, kMiddle = 256, kNarrow = 128, kResident = 1536, kRoomy = 1024;   // threads of a CTA, and of an SM
 constexpr int kAhead = 4;                                      // vectors that a thread has in flight
 static_assert(kFound >= kCluster * PIPE_MAX_TOP && kFound % 2 == 0, "");
 
@@ -477,9 +477,9 @@ __device__ __forceinline__ int search(Search<B>& s, const Part& p, float m, int 
   return found <= kFound ? found : search_by_halves<SRC, B>(s, p, own, least, k);
 }
 
-// B threads a CTA; a cluster of CTAs a row.  ENT: the entropy is wanted.
-template <int SRC, int B, bool ENT>
-__global__ void __launch_bounds__(B, kResident / B) logprobs_kernel(const Args a) {
+// B threads a CTA, R an SM; a cluster of CTAs a row.  ENT: the entropy is wanted.
+template <int SRC, int B, int R, bool ENT>
+__global__ void __launch_bounds__(B, R / B) logprobs_kernel(const Args a) {
   constexpr int kLogits = Vec<SRC>::kLogits;
   __shared__ Search<B> search_s;
   __shared__ Sums warp_s[B / 32];
@@ -682,10 +682,11 @@ __global__ void __launch_bounds__(B, kResident / B) logprobs_kernel(const Args a
 
 using Kernel = void (*)(Args);
 template <int SRC>
-static Kernel logprobs_of(int threads, bool entropy) {
-  if (threads == kWide) return entropy ? logprobs_kernel<SRC, kWide, true> : logprobs_kernel<SRC, kWide, false>;
-  if (threads == kMiddle) return entropy ? logprobs_kernel<SRC, kMiddle, true> : logprobs_kernel<SRC, kMiddle, false>;
-  return entropy ? logprobs_kernel<SRC, kNarrow, true> : logprobs_kernel<SRC, kNarrow, false>;
+static Kernel logprobs_of(int threads, bool roomy, bool entropy) {
+  if (roomy) return entropy ? logprobs_kernel<SRC, kWide, kRoomy, true> : logprobs_kernel<SRC, kWide, kRoomy, false>;
+  if (threads == kWide) return entropy ? logprobs_kernel<SRC, kWide, kResident, true> : logprobs_kernel<SRC, kWide, kResident, false>;
+  if (threads == kMiddle) return entropy ? logprobs_kernel<SRC, kMiddle, kResident, true> : logprobs_kernel<SRC, kMiddle, kResident, false>;
+  return entropy ? logprobs_kernel<SRC, kNarrow, kResident, true> : logprobs_kernel<SRC, kNarrow, kResident, false>;
 }
 
 }  // namespace lpb
@@ -711,20 +712,23 @@ extern "C" pipe_status pipe_token_logprobs(const void* d_logits, int32_t dtype, 
   if (T == 0) return PIPE_OK;
   lpb::Args a = {d_logits, T, ldl, V, scale, d_tokens, n, d_logprobs, d_entropy, k, d_top, d_top_logprobs, device_status_word()};
   if (!a.status) return grp::runtime_failed();
-  // Threads of a row: a CTA's joins, search and ranking take some 5 us whatever its size, so that many rows want many small CTAs on an SM,
-  // a long row one that reads it fast, and rows that are all on the chip at once as many threads as there are.  With 10 alternatives and the
-  // entropy (us; 128, 256 and 512 threads): 4000 rows of 16 KB 40, 43, 69, of 64 KB 77, 78, 99, of 128 KB 142, 118, 127, of 256 KB 258, 214,
-  // 198; 300 rows of 16 KB 9.4, 7.2, 8.5, of 64 KB 16.1, 12.7, 13.8; 100 rows of 64 KB 12.0, 9.7, 9.1.
-  const int64_t bytes = static_cast<int64_t>(V) * (dtype == PIPE_DTYPE_FP32 ? 4 : 2);
-  int threads = bytes <= 32768 ? lpb::kNarrow : (bytes <= 163840 ? lpb::kMiddle : lpb::kWide);
+  // Threads of a row: behind the pass a CTA is some 3 us busy with joins, search and ranking whatever its size, so that many rows want many
+  // small CTAs on an SM, a long row one that reads it fast, and rows that are all on the chip at once as many threads as there are.  With 10
+  // alternatives and the entropy (us; 128, 256 and 512 threads): 4000 rows of 16 KB 27, 34, 58, of 40 KB 42, 49, 71, of 64 KB 61, 60, 79, of
+  // 128 KB 128, 102, 111, of 256 KB 255, 202, 186; 300 rows of 16 KB 7.3, 5.9, 7.9; 290 of 128 KB 256 threads 15.1, 512 12.9.
+  const int64_t bytes = static_cast<int64_t>(V) * (dtype == PIPE_DTYPE_FP32 ? 4 : 2), roomy_ctas = lpb::kRoomy / lpb::kWide * kPlanSMs;
+  int threads = bytes <= 49152 ? lpb::kNarrow : (bytes <= 163840 ? lpb::kMiddle : lpb::kWide);
   if (T <= 3 * kPlanSMs && bytes > 8192 && threads < lpb::kMiddle) threads = lpb::kMiddle;
-  if (T <= kPlanSMs && bytes > 16384) threads = lpb::kWide;
-  // and a few long rows several CTAs (1, 2, 4 and 8): a row of 256 KB 11.4, 10.4, 9.3, 8.6; 60 rows 15.3, 13.6, 15.4, 20.6
+  if (T <= roomy_ctas && bytes > 16384) threads = lpb::kWide;
+  // CTAs of 512 that are on the chip at once at 64 registers a thread have as many: 30 rows of 256 KB 9.6 us (at 40: 11.3).
+  const bool roomy = threads == lpb::kWide && T <= roomy_ctas;
+  // A few long rows have several CTAs (1, 2, 4 and 8): one row of 256 KB 9.6, 8.6, 8.2, 7.5, 60 rows 13.3, 11.2, 11.8, 18.0, one of 64 KB 5.9,
+  // 6.4, 6.8, 7.6.
   int ctas = 1;
-  while (threads == lpb::kWide && ctas < lpb::kCluster && bytes / ctas > 16384 && T * ctas * 2 <= lpb::kResident / lpb::kWide * kPlanSMs) ctas *= 2;
-  const lpb::Kernel kern = dtype == PIPE_DTYPE_FP32 ? lpb::logprobs_of<PIPE_DTYPE_FP32>(threads, d_entropy != nullptr)
-                                                    : (dtype == PIPE_DTYPE_BF16 ? lpb::logprobs_of<PIPE_DTYPE_BF16>(threads, d_entropy != nullptr)
-                                                                                : lpb::logprobs_of<PIPE_DTYPE_FP16>(threads, d_entropy != nullptr));
+  while (roomy && ctas < lpb::kCluster && bytes > 98304 && T * ctas * 2 <= kPlanSMs) ctas *= 2;
+  const lpb::Kernel kern = dtype == PIPE_DTYPE_FP32 ? lpb::logprobs_of<PIPE_DTYPE_FP32>(threads, roomy, d_entropy != nullptr)
+                                                    : (dtype == PIPE_DTYPE_BF16 ? lpb::logprobs_of<PIPE_DTYPE_BF16>(threads, roomy, d_entropy != nullptr)
+                                                                                : lpb::logprobs_of<PIPE_DTYPE_FP16>(threads, roomy, d_entropy != nullptr));
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (launch_overlapped(kern, dim3(static_cast<unsigned>(T * ctas)), threads, ctas, true, s, a) != cudaSuccess) return grp::runtime_failed();
   count_launch(1);
