@@ -60,7 +60,7 @@ inline bool lay_out(const TcShape& c, TcPlan* p) {
   const int stage = p->KS * (p->TM + p->TN / p->cg) * kBlock;
   const int room = kMaxSmem - 1024 - turn - sx - table;
   p->ring = room / stage < kMaxRing ? room / stage : kMaxRing;
-  p->ahead = 16;
+  p->ahead = 16;   // (4096 -> 11008 on one row: 10.2 us, with none 10.9, with 128 10.4)
   if (p->ring < 2 || p->columns > 512) return false;
   p->off_turn = static_cast<uint32_t>(p->ring * stage);
   p->off_sx = p->off_turn + turn;

@@ -4,7 +4,8 @@
 // neighbouring values W at a time, every load and store of a warp of whole neighbouring lines: eight of 16 bits, four where values are
 // written too (their 16-byte stores would leave half-written sectors otherwise).  The largest magnitude is found on the values' bits,
 // which order like the magnitudes, a NaN above all.  Rows beyond what the registers hold are read a second time.  Bound by HBM where
-// values are written, otherwise by the issue slots: some 7 instructions a value and 100 a thread and row.
+// values are written, otherwise by the issue slots: some 7 instructions a value and 100 a thread and row.  11008 rows of 4096 bf16: 29 us (4.6
+// TB/s, issue slots 71 % busy), with values 50 (6.3 TB/s).
 #include "int8_common.cuh"
 
 namespace pipe {
@@ -264,7 +265,8 @@ extern "C" pipe_status pipe_int8_quantize(const void* d_x, int32_t x_dtype, int6
   a.wide_v = !misaligned(d_values, 16) && ldv % 4 == 0;
   a.status = device_status_word();
   if (!a.status) return grp::runtime_failed();
-  // the fewest threads whose registers hold a row
+  // The fewest threads whose registers hold a row (32, 64, 128, 256 and 512 threads, us): 4096 rows of 4096 bf16 22, 19, 13, 16, 27; 20000 of 512
+  // 11, 15, 26, 44, 104; 4096 of 11008 with values 121, 109, 78, 62, 59.
   int P = 32;
   while (P < 512 && I > i8::kQHeld * P) P *= 2;
   const i8::QuantKernel k = x_dtype == PIPE_DTYPE_FP32 ? i8::quantize_kernel<PIPE_DTYPE_FP32>(P, d_values)
