@@ -442,3 +442,21 @@ def test_narrow_layers_on_many_rows(T, O, I):
 def test_narrow_experts_on_many_rows():
     _expert(3, 40, 96, "fp16", [700, 0, 2000], True, 2, 30)
     _expert(5, 8, 300, "fp32", [150, 151, 0, 149, 600], False, 0, 31)
+
+
+@pytest.mark.parametrize("T,O,I", [(2095, 479, 230), (300, 1003, 96), (37, 501, 700), (13, 77, 5000)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_outputs_are_the_same_wherever_rows_begin(T, O, I, dtype):
+    gen, h = _gen(T), R.TYPES[dtype]
+    w, sw, wd = _layer(gen, 1, O, I)
+    x = _pitched(torch.randint(-128, 128, (T, I), generator=gen, dtype=torch.int8), I + 15 & ~15)
+    sx, b = torch.rand((T,), generator=gen).cuda() * 0.02, torch.randn((O,), generator=gen).to(h).cuda()
+    got = []
+    for ldy in (O + 15 & ~15, (O + 15 & ~15) + 2, O, O + 9):
+        y = torch.full((T, ldy), -7.0, dtype=h, device="cuda")
+        B.pipe_int8_linear(B.make_int8_desc(O, I, dtype=h), wd, sw.cuda(), x, sx, y[:, :O], bias=b, activation=2)
+        _ok()
+        assert (y[:, O:] == -7).all()
+        got.append(y[:, :O].contiguous())
+    R.check_product(got[0], x.cpu(), sx.cpu(), w[0], sw[0], b.cpu(), 2, dtype)
+    assert all(torch.equal(g, got[0]) for g in got[1:])
