@@ -18,7 +18,8 @@ using grp::unit_ints;
 constexpr int kBlock = 128;                 // codes of a block of the reduction axis: bytes, a row of the 128-byte swizzle
 constexpr int kMaxRing = 16;
 constexpr int kMaxSmem = 226 * 1024;        // dynamic shared memory (the rest of 227 KiB: barriers)
-constexpr int kDrainWarps = 8;
+constexpr int kDrainWarps = 8, kMoreDrainWarps = 16;
+constexpr int kShort = 1408;
 constexpr int kTurnBytes = 32 * 32 * 2;     // a warp's 32 rows of y by 32 channels, 16-bit
 
 struct TcShape {
@@ -37,6 +38,7 @@ struct TcPlan {
   int ring;        // stages in flight
   int columns;     // of tensor memory that a CTA takes
   uint32_t off_turn, off_sx, off_table;   // shared memory behind the ring
+  int drain;       // warps that drain
   int smem;        // dynamic shared memory
   int ahead;       // blocks of the first tile's weights that are asked into L2 early
   int64_t tiles;   // the most there can be
@@ -56,7 +58,11 @@ inline bool lay_out(const TcShape& c, TcPlan* p) {
   const int wide = accumulator_columns(p->TN);
   p->columns = 32;
   while (p->columns < (p->split > 1 ? 1 : 2) * wide) p->columns *= 2;
-  const int turn = p->split > 1 ? 0 : kDrainWarps * kTurnBytes, sx = p->split > 1 ? 0 : kDrainWarps * wide * 4, table = unit_ints(c.E) * 4;
+  // Short sums on more than a round of tiles wait for the drain: 16 warps of it (4096 rows to 11008 channels, us, identity and SiLU: I = 256 39 and
+  // 60, by 16 warps 35 and 50, 1024 45 and 65, 42 and 55, 1408 51 and 67, 51 and 59; longer ones, which want the ring, 2048 64 and 75, 67 and 71,
+  // 4096 119 and 122, 126 and 125; in one round 300 rows of I = 1024 9.1, 11.0).
+  p->drain = p->split == 1 && c.I <= kShort && p->tiles > kChipSMs / p->cg ? kMoreDrainWarps : kDrainWarps;
+  const int turn = p->split > 1 ? 0 : p->drain * kTurnBytes, sx = p->split > 1 ? 0 : 4 * wide * 4, table = unit_ints(c.E) * 4;
   const int stage = p->KS * (p->TM + p->TN / p->cg) * kBlock;
   const int room = kMaxSmem - 1024 - turn - sx - table;
   p->ring = room / stage < kMaxRing ? room / stage : kMaxRing;

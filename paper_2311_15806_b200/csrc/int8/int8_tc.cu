@@ -6,7 +6,7 @@
 // read as zeros.  Sums are int32 in tensor memory, exact, in two accumulators, so that the drain of a tile overlaps the next one's
 // products.  The drain applies the channel's scale, the token's, bias and sigma; 16-bit outputs are turned in shared memory to rows of
 // y, 32-bit ones are stored as they come, 32 neighbouring channels at a time.
-//   warp 0 copies   warp 1 MMAs, tensor memory   warps 2-9 drain, two for every 32 lanes of tensor memory, which take 32 rows in turn
+//   warp 0 copies   warp 1 MMAs, tensor memory   warps 2 .. drain, two or four for every 32 lanes of tensor memory, which take 32 rows in turn
 // Few tiles: the CTAs of a cluster share a tile's reduction axis and add their sums through distributed shared memory (integers: in any
 // order the same).  Such a CTA gives its tensor memory back before it waits for the others: one that held it could wait for a CTA
 // that waits for tensor memory on another SM.
@@ -28,7 +28,7 @@ using grp::cluster_rank;
 using grp::cluster_sync;
 using grp::Unit;
 
-constexpr int kThreads = 64 + 32 * kDrainWarps;
+constexpr int kThreads = 64 + 32 * kMoreDrainWarps, kFewThreads = 64 + 32 * kDrainWarps;   // the most, and those that every launch has
 struct TcArgs : TcPlan {
   Call call;
   int wide_y;      // rows of y are 16-byte aligned
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(d_full + 8 * b, 1);
-      mbar_init(d_empty + 8 * b, kDrainWarps * CG);
+      mbar_init(d_empty + 8 * b, p.drain * CG);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&wmap)) : "memory");
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
   }
   grid_wait();
   grid_release();
-  if (c.offsets) grp::build_units<kThreads>(c, p.TN, table);   // (one expert needs no table: 0.7 us)
+  if (c.offsets) grp::build_units<kFewThreads>(c, p.TN, table);   // (one expert needs no table: 0.7 us)
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   if (CG == 2) cluster_sync();
@@ -259,11 +259,12 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
     __syncwarp();   // (one thread may have been alone)
   } else if (p.split == 1) {
     // ---- drain
-    const int q = warp & 3, half = (warp - 2) >> 2;   // this warp's 32 lanes of tensor memory, and its turn
+    const int q = warp & 3, part = (warp - 2) >> 2;   // this warp's 32 lanes of tensor memory, and its turn
     const uint32_t from = tmem + (static_cast<uint32_t>(q * 32) << 16);
     const uint32_t lead_e = (CG == 2 ? cluster_address(bars, 0) : bar0) + (d_empty - bar0);
-    float* sx = reinterpret_cast<float*>(gen + p.off_sx) + (4 * half + q) * acc_pitch;   // this warp's copy of the rows' scales
-    uint8_t* turn = gen + p.off_turn + (4 * half + q) * kTurnBytes;
+    float* sx = reinterpret_cast<float*>(gen + p.off_sx) + q * acc_pitch;   // the rows' scales: a warp copies those of its rows
+    uint8_t* turn = gen + p.off_turn + (4 * part + q) * kTurnBytes;
+    const int step = 8 * p.drain;   // four warps take 32 rows
     uint32_t n = 0;
     for (int64_t t = team; t < tiles; t += teams, ++n) {
       const Tile tl = tile_of<CG>(p, table, static_cast<int>(t), rank);
@@ -278,12 +279,12 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
         sw[h] = o < end ? __ldcg(p.call.sw + ch0 + o) : 0.f;
         bias[h] = c.bias && o < end ? H::load(c.bias, ch0 + o) : 0.f;
       }
-      for (int i = 32 * half + lane; i < acc_pitch; i += 64) sx[i] = i < count ? __ldcg(p.call.sx + tl.lo + i) : 0.f;
+      for (int i = 32 * part + lane; i < acc_pitch; i += step) sx[i] = i < count ? __ldcg(p.call.sx + tl.lo + i) : 0.f;
       __syncwarp();
       if (!__all_sync(0xffffffffu, mbar_wait<CG == 2, 64>(d_full + 8 * buf, use & 1, abort_flag, c.status))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t acc = from + buf * acc_pitch;
-      for (int n0 = 32 * half; n0 < count; n0 += 64) {   // rows of y, 32 at a time
+      for (int n0 = 32 * part; n0 < count; n0 += step) {   // rows of y, 32 at a time
         int v[2][16];
         if constexpr (H::kBytes == 4) {
           const int o = o0 + 32 * q + lane;
@@ -411,7 +412,7 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
       const int32_t* sums = reinterpret_cast<const int32_t*>(gen);
       const Tile tl = tile_of<CG>(p, table, team, rank);
       const int64_t ch0 = static_cast<int64_t>(tl.e) * c.O;
-      for (int i = crank * kThreads + threadIdx.x; i < (tl.hi - tl.lo) * 16; i += p.split * kThreads) {
+      for (int i = crank * kFewThreads + threadIdx.x; i < (tl.hi - tl.lo) * 16; i += p.split * kFewThreads) {
         const int r = i >> 4, col = tl.o0 + (i & 15) * 8;
         if (col >= min(c.O, tl.o0 + p.TM)) continue;
         int acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -494,7 +495,7 @@ pipe_status linear_tc(const Call& call, cudaStream_t stream) {
   attr[1].val.clusterDim.x = p.cg * p.split;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.gridDim = dim3(static_cast<unsigned>(p.teams * p.cg * p.split));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(64 + 32 * p.drain);
   cfg.dynamicSmemBytes = p.smem;
   cfg.stream = stream;
   cfg.attrs = attr;

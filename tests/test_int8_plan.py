@@ -36,8 +36,8 @@ static void look(const TcShape& c) {
   const int stage = p.KS * (p.TM + own) * 128;
   CHECK(p.ring >= 2 && p.ring <= kMaxRing);
   CHECK(static_cast<int>(p.off_turn) == p.ring * stage && p.off_turn % 1024 == 0);
-  CHECK(p.off_sx - p.off_turn == (p.split > 1 ? 0u : 8u * kTurnBytes) && p.off_sx % 16 == 0);
-  CHECK(p.off_table - p.off_sx == (p.split > 1 ? 0u : 8u * 4u * wide) && p.off_table % 4 == 0);
+  CHECK(p.off_sx - p.off_turn == (p.split > 1 ? 0u : p.drain * kTurnBytes) && p.off_sx % 16 == 0);
+  CHECK(p.off_table - p.off_sx == (p.split > 1 ? 0u : 4u * 4u * wide) && p.off_table % 4 == 0);
   CHECK(p.smem >= 1024 + static_cast<int>(p.off_table) + 4 * unit_ints(c.E) && p.smem <= kMaxSmem);
   // the last block's weights, read as 128 rows
   CHECK(p.smem >= 1024 + (p.ring - 1) * stage + (p.KS - 1) * p.TM * 128 + 128 * 128);
