@@ -607,7 +607,8 @@ pipe_status pipe_expert_combine(const void* d_y, int64_t N, int64_t ldy, const i
  * The other form in which checkpoints of large language models come: int8 codes, a float scale for every row of W, and activations
  * that are brought to int8 on the way, every token by a scale of its own.  (pipe_quantize_act has one scale for the whole tensor.)  A
  * layer of E experts [O, I] is two device arrays, which may come from elsewhere than pipe_int8_quantize:
- *   codes   int8, E*O rows of I at a pitch of ldw bytes, a multiple of 16, 16-byte aligned; expert e's rows follow expert e-1's
+ *   codes   int8, E*O rows of I at a pitch of ldw bytes, a multiple of 16 (of 128: up to a fifth faster), 16-byte aligned; expert e's rows
+ *           follow expert e-1's
  *   scales  float [E*O]
  * and stands for W_e[o, i] = scales[e*O + o] * codes[e*O + o, i]; activations likewise, row by row.  -128 is a code like any other.
  */

@@ -748,9 +748,10 @@ def pipe_int8_expert_linear(desc: Int8Desc, codes: torch.Tensor, scales: torch.T
 
 
 def alloc_int8(rows: int, I: int, device="cuda", experts: int | None = None):
-    """codes ([rows, I], or [experts, rows, I]) at the pitch that the products want, and scales; unset."""
+    """codes ([rows, I], or [experts, rows, I]) at the pitch that the products like best, and scales; unset."""
     lead = (rows,) if experts is None else (experts, rows)
-    codes = torch.empty((*lead, I + 15 & ~15), dtype=torch.int8, device=device)[..., :I]
+    # multiples of 16 bytes do; long rows that begin on a line of 128 are read faster (11008 x 1700, 4096 rows: 61 us for 75)
+    codes = torch.empty((*lead, I + 127 & ~127 if I > 512 else I + 15 & ~15), dtype=torch.int8, device=device)[..., :I]
     return codes, torch.empty(lead, dtype=torch.float32, device=device)
 
 

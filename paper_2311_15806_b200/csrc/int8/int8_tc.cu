@@ -14,7 +14,7 @@
 // wait.
 // Bound by HBM on few rows (4096 -> 11008 on one row: 10.2 us among launches that overlap, 4.4 TB/s; the start and the last drain are the
 // rest), by the tensor pipe on many (4096 rows: 119 us, 3.1 POP/s, pipe 87 % busy; under the power cap of a long run 141), by the drain, 3.7 us
-// of a tile of 256 x 256, on many rows of fewer than some 1000 values (32000 <- 128 on 2048 rows: 52 us).
+// of a tile of 256 x 256 with eight warps, on many rows of fewer than some 1000 values (11008 <- 256 on 4096 rows: 35 us with sixteen).
 #include "int8_common.cuh"
 #include "int8_plan.h"
 #include "pipe_tc_common.cuh"

@@ -162,3 +162,11 @@ def test_kernels_that_start_early_use_no_read_only_loads():
                 assert "__ldg(" not in text and "ld.global.nc" not in text and "__restrict__" not in text, name
                 assert "return PIPE_ERR_CUDA" not in text and "cudaFuncSetAttribute" not in text, name   # (runtime_failed, allow_dynamic_smem)
     assert seen >= 4
+
+
+def test_long_rows_are_given_whole_lines():
+    for I, pitch in ((512, 512), (513, 640), (700, 768), (4096, 4096)):
+        codes, _ = B.alloc_int8(3, I, device="cpu")
+        assert codes.stride() == (pitch, 1)
+        codes, _ = B.alloc_int8(3, I, device="cpu", experts=2)
+        assert codes.stride() == (3 * pitch, pitch, 1)
