@@ -640,9 +640,11 @@ pipe_status pipe_int8_quantize(const void* d_x, int32_t x_dtype, int64_t T, int3
 /*
  * y[t, o] = h(sigma((float(sum_i xq[t, i] * W[o, i]) * scales[o]) * sx[t] + bias[o])) for a layer of one expert: the sum is exact, what
  * follows is binary32 (the second product and the bias are one fused operation, sigma is one of PIPE_ACT_*), h() rounds to the layer's
- * type.  d_xq: int8 [T, I] pitch ldx bytes, a multiple of 16, 16-byte aligned; d_sx: float [T]; d_bias: [O] in the layer's type or
- * NULL; d_y: [T, O] pitch ldy.  T = 0 is a no-op, T is at most 2^30 (2^31 tiles of rows and channels or more: PIPE_ERR_UNSUPPORTED).  d_y must not overlap the inputs.  A row of y does not depend on
- * the other rows or on their number; equal calls give equal bits.
+ * type.  In PIPE_DTYPE_FP32 SiLU and sigmoid are off by less than 2^-20 of their value, GELU by 2^-19; before the rounding to 16 bits by
+ * |v| 2^-23 of it more (GELU v^2 2^-23); by 2^-139 where that is more.  d_xq: int8 [T, I] pitch ldx bytes, a multiple of 16, 16-byte
+ * aligned; d_sx: float [T]; d_bias: [O] in the layer's type or NULL; d_y: [T, O] pitch ldy.  T = 0 is a no-op, T is at most 2^30 (2^31 tiles
+ * of rows and channels or more: PIPE_ERR_UNSUPPORTED).  d_y must not overlap the inputs.  A row of y does not depend on the other rows or on
+ * their number; equal calls give equal bits.
  */
 pipe_status pipe_int8_linear(const pipe_int8_desc* desc, const int8_t* d_codes, int64_t ldw, const float* d_scales, const int8_t* d_xq,
                              int64_t T, int64_t ldx, const float* d_sx, const void* d_bias, int32_t activation, void* d_y, int64_t ldy,

@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
           }
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            activate(u[g], c.act);
+            activate<H>(u[g], c.act);
             if (o < end) {
 #pragma unroll
               for (int i = 0; i < 16; ++i, y += c.ldy)
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
             float u[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) u[i] = scaled(v[0][i], scale, sx[n0 + i0 + i], add);
-            activate(u, c.act);
+            activate<H>(u, c.act);
             if (o < end) {
 #pragma unroll
               for (int i = 0; i < 16; ++i, y += c.ldy)
@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
             float u[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) u[i] = scaled(v[h >> 1][4 * (i >> 1) + 2 * (h & 1) + (i & 1)], sw[h], sc[i], bias[h]);
-            activate(u, c.act);
+            activate<H>(u, c.act);
             turn_store(smem_u32(turn) + lane * 64 + ((h ^ ((lane >> 1) & 3)) * 16), H::pack(u[0], u[1]), H::pack(u[2], u[3]), H::pack(u[4], u[5]), H::pack(u[6], u[7]));
           }
           __syncwarp();
@@ -437,7 +437,7 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
           const bool real = col + k < c.O;
           v[k] = scaled(acc[k], real ? __ldcg(p.call.sw + ch0 + col + k) : 0.f, sx, real && c.bias ? H::load(c.bias, ch0 + col + k) : 0.f);
         }
-        activate(v, c.act);
+        activate<H>(v, c.act);
         store_y8<H>(c.y, (static_cast<int64_t>(tl.lo) + r) * c.ldy + col, v, p.wide_y, c.O - col);
       }
     }
