@@ -64,17 +64,16 @@ inline bool lay_out(const TcShape& c, TcPlan* p) {
   p->drain = p->split == 1 && c.I <= kShort && p->tiles > kChipSMs / p->cg ? kMoreDrainWarps : kDrainWarps;
   const int turn = p->split > 1 ? 0 : p->drain * kTurnBytes, sx = p->split > 1 ? 0 : 4 * wide * 4, table = unit_ints(c.E) * 4;
   const int stage = p->KS * (p->TM + p->TN / p->cg) * kBlock;
-  const int room = kMaxSmem - 1024 - turn - sx - table;
+  // (the MMA reads 128 rows of weights, also behind the last stage's, where the others lie)
+  const int read = (128 - p->TM) * kBlock, others = turn + sx + table;
+  const int room = kMaxSmem - 1024 - (read > others ? read : others);
   p->ring = room / stage < kMaxRing ? room / stage : kMaxRing;
   p->ahead = 16;   // (4096 -> 11008 on one row: 10.2 us, with none 10.9, with 128 10.4)
   if (p->ring < 2 || p->columns > 512) return false;
   p->off_turn = static_cast<uint32_t>(p->ring * stage);
   p->off_sx = p->off_turn + turn;
   p->off_table = p->off_sx + sx;
-  // the MMA reads 128 rows of weights, also behind the last stage's
-  const int read = p->ring * stage + (128 - p->TM) * kBlock, all = static_cast<int>(p->off_table) + table;
-  p->smem = 1024 + (read > all ? read : all);
-  if (p->smem > kMaxSmem) return false;
+  p->smem = 1024 + p->ring * stage + (read > others ? read : others);
   p->teams = p->split > 1 ? p->tiles : kChipSMs / p->cg;
   if (p->teams > p->tiles) p->teams = p->tiles;
   return true;
@@ -93,7 +92,18 @@ inline int stage_blocks(int TM, int TN, int cg) {
 // a form (the copies' bytes, the drain, the launch's latency) whose numbers are fitted to 6000 timings of 75 shapes; the choice takes 2 %
 // longer than the best that was timed, on average.  Either side (us): 11008 x 4096, one row: TM 80 10.1, TM 128 11.2; 128 rows: pairs of TM
 // 80 14.0, single CTAs of TM 80 14.9; 512 rows: pairs of 192 rows 24.0, of 256 27.4; 4096 x 11008, one row: TM 128 split four ways 12.0,
-// TM 32 not split 15.1; 4096 rows, 4096 -> 11008: pairs of 256 rows 123, single CTAs 150.
+// TM 32 not split 15.1; 3584 x 18944, one row: TM 112 split four ways 15.5, not split 26.8; 200 x 11008, 32 rows: four ways 8.6, not split 16.7;
+// 4096 rows, 4096 -> 11008: pairs of 256 rows 123, single CTAs 150.
+inline int64_t tile_cost(int64_t tiles, int64_t blocks, int TN, int TM, int cg, int split) {
+  const int64_t rounds = split > 1 ? 1 : div_up(tiles, kChipSMs / cg), load = (TM + TN / cg) * 23 / 10;
+  const int64_t work = div_up(blocks, split) * (load > 160 ? load : 160), floor = 7000 + 5 * TN;
+  const int64_t ctas = tiles * cg * split;
+  return rounds * (work > floor ? work : floor) + 47 * TN + 30 * (ctas < kChipSMs ? ctas : kChipSMs) + (cg == 2 ? 450 : 0) + (split > 1 ? 5000 : 0);
+}
+// Whether that many CTAs may share a tile's axis: their clusters stand on the chip at once, each has four blocks.
+inline bool may_split(int64_t tiles, int64_t blocks, int TN, int cg, int split) {
+  return cg == 1 && TN <= 64 && blocks >= 4 * split && tiles <= kClusters[split];
+}
 inline bool plan_tc(const TcShape& c, TcPlan* p) {
   const int64_t experts = c.ragged ? (c.N < c.E ? c.N : c.E) : 1;
   const int64_t mean = div_up(c.N, experts);   // rows of an expert
@@ -115,11 +125,8 @@ inline bool plan_tc(const TcShape& c, TcPlan* p) {
       for (int TM = cg == 1 ? 32 : 64; TM <= 128; TM += 16) {
         const int64_t tiles = units * div_up(c.O, TM * cg);
         for (int split = 1; split <= 8; ++split) {
-          if (split > 1 && (cg == 2 || TN > 64 || blocks < 4 * split || tiles > kClusters[split])) break;
-          const int64_t rounds = split > 1 ? 1 : div_up(tiles, kChipSMs / cg), load = (TM + TN / cg) * 23 / 10;
-          const int64_t work = div_up(blocks, split) * (load > 160 ? load : 160), floor = 7000 + 5 * TN;
-          const int64_t ctas = tiles * cg * split;
-          const int64_t cost = rounds * (work > floor ? work : floor) + 47 * TN + 30 * (ctas < kChipSMs ? ctas : kChipSMs) + (cg == 2 ? 450 : 0) + (split > 1 ? 5000 : 0);
+          if (split > 1 && !may_split(tiles, blocks, TN, cg, split)) break;
+          const int64_t cost = tile_cost(tiles, blocks, TN, TM, cg, split);
           if (best < 0 || cost < best) {
             best = cost;
             p->TN = TN; p->TM = TM; p->cg = cg; p->split = split;
@@ -129,9 +136,6 @@ inline bool plan_tc(const TcShape& c, TcPlan* p) {
     }
   }
   p->KS = stage_blocks(p->TM, p->TN, p->cg);
-  if (lay_out(c, p)) return true;
-  // (the bound on an expert call's units may be more than the clusters of a launch can be: those tiles are one CTA's)
-  p->split = 1;
   return lay_out(c, p);
 }
 
