@@ -668,6 +668,7 @@ pipe_status pipe_int8_expert_linear(const pipe_int8_desc* desc, const int8_t* d_
  *     entropy[t]         = - sum_v p log p,  p = exp(z[t, v] - norm_t)
  *     top[t, i]          = the token with the i-th largest logit, equal ones (-0 and 0 are) in ascending order, i < k
  *     top_logprobs[t, i] = its log probability
+ * No log probability is above 0, no entropy below.
  * A logit of -Inf is a masked token: its probability is 0, its log probability -Inf, and it is not among the top; where fewer than k
  * tokens are left, what is missing has token -1 and log probability -Inf.  A row of nothing but -Inf has log probabilities -Inf and
  * entropy 0.  A row with a NaN or +Inf sets PIPE_ERR_NONFINITE in the device status word; its floats are NaN (those of tokens outside

@@ -610,12 +610,15 @@ __global__ void __launch_bounds__(B, R / B) logprobs_kernel(const Args a) {
   auto logprob = [&](float l, float logs) {
     return is_bad() ? nan : (own.m == -INFINITY || l == -INFINITY ? -INFINITY : (0.5f * l - 0.5f * own.m) * a.scale * 2.f - logs);
   };
+  // (the largest logit's term is 1, so no sum is less; what two exponentials of opposite numbers lose may have left it 2^-24 below, and a log
+  // probability above 0)
+  auto log_sum = [&] { return logf(fmaxf(own.s, 1.f)); };
   auto write_sums = [&] {
     if (turn >= max(a.n, 1)) return;
-    const float logs = logf(own.s);
+    const float logs = log_sum();
     if (turn == 0) {
       if (is_bad()) raise_status(a.status, PIPE_ERR_NONFINITE);
-      if (ENT) a.entropy[t] = is_bad() ? nan : (own.m == -INFINITY ? 0.f : logs - kLn2 * own.h / own.s);
+      if (ENT) a.entropy[t] = is_bad() ? nan : (own.m == -INFINITY ? 0.f : fmaxf(logs - kLn2 * own.h / own.s, 0.f));
     }
     for (int j = turn; j < a.n; j += B) {
       if (j >= B) given = given_of(t * a.n + j);
@@ -628,7 +631,7 @@ __global__ void __launch_bounds__(B, R / B) logprobs_kernel(const Args a) {
       if (a.top_logprobs) a.top_logprobs[t * a.k + i] = is_bad() ? nan : -INFINITY;
     }
     if (count <= 0) return;
-    const float logs = logf(own.s);
+    const float logs = log_sum();
     rank(search_s, count, a.k, [&](int i, Entry e) {
       if (a.top) a.top[t * a.k + i] = place_in(e);
       if (a.top_logprobs) a.top_logprobs[t * a.k + i] = logprob(number_of(key_in(e)), logs);
