@@ -704,7 +704,7 @@ def _int8_product(where: str, desc: Int8Desc, codes, scales, xq, sx, bias, y) ->
         raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: int8 codes, float32 scales and outputs of the layer's type are needed")
     ldw, ldx, ldy = _pitch_of(where, codes, I), _pitch_of(where, xq, I), _pitch_of(where, y, O)
     w, N = codes.shape, y.shape[0]
-    if (w[0] if len(w) == 2 else w[0] * w[1]) != E * O or not _laid_out(scales, E, O):
+    if (w[0] if len(w) == 2 else w[0] * w[1]) != E * O or (len(w) == 3 and w[0] != E and 1 not in w[:2]) or not _laid_out(scales, E, O):
         raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: codes and scales are not the descriptor's arrays")
     if y.dim() != 2 or xq.dim() != 2 or xq.shape[0] != N or sx.numel() != N or not sx.is_contiguous():
         raise PipeError(PIPE_ERR_INVALID_ARG, f"{where}: xq, sx and y differ in rows")
