@@ -29,7 +29,7 @@ struct TcShape {
 };
 struct TcPlan {
   int TN;          // most rows of a tile
-  int TM;          // channels of a CTA's tile, a multiple of 8: 128 for a pair
+  int TM;          // channels of a CTA's tile, a multiple of 16 from 32 (a pair: 64) to 128
   int KS;          // blocks of the reduction axis in a stage
   int cg;          // CTAs of a tile: 1, or a pair of SMs
   int mtiles;      // ceil(O / (TM cg))
@@ -58,9 +58,14 @@ inline bool lay_out(const TcShape& c, TcPlan* p) {
   const int wide = accumulator_columns(p->TN);
   p->columns = 32;
   while (p->columns < (p->split > 1 ? 1 : 2) * wide) p->columns *= 2;
-  // Short sums on more than a round of tiles wait for the drain: 16 warps of it (4096 rows to 11008 channels, us, identity and SiLU: I = 256 39 and
-  // 60, by 16 warps 35 and 50, 1024 45 and 65, 42 and 55, 1408 51 and 67, 51 and 59; longer ones, which want the ring, 2048 64 and 75, 67 and 71,
-  // 4096 119 and 122, 126 and 125; in one round 300 rows of I = 1024 9.1, 11.0).
+  // Short sums on more than a round of tiles wait for the drain: 16 warps of it; longer ones want the ring.  By 8 and by 16 warps, us:
+  //   4096 rows to 11008 channels, 16-bit, identity     I = 256 39, 35; 1024 46, 43; 1408 52, 52; 2048 66, 69; 4096 119, 126
+  //                                SiLU                 60, 50; 65, 55; 67, 60; 78, 74; 122, 125
+  //                                32-bit, identity     46, 38; 53, 52; 63, 64; 80, 82
+  //                                SiLU                 68, 54; 72, 62; 77, 69; 88, 85
+  //   4096 channels, 16-bit, identity and SiLU          1024 21, 20 and 30, 26; 1408 22.7, 23.1 and 31, 27; 2048 28, 29 and 33, 31
+  //   1024 rows to 32000                                1024 35, 34 and 48, 42; 1408 42, 42 and 52, 47; 2048 55, 58 and 62, 61
+  // and in one round 300 rows of I = 1024 9.1, 11.0.  (With an activation 16 still win at 2048, which the rule, blind to it, gives away: 1 to 6 %.)
   p->drain = p->split == 1 && c.I <= kShort && p->tiles > kChipSMs / p->cg ? kMoreDrainWarps : kDrainWarps;
   const int turn = p->split > 1 ? 0 : p->drain * kTurnBytes, sx = p->split > 1 ? 0 : 4 * wide * 4, table = unit_ints(c.E) * 4;
   const int stage = p->KS * (p->TM + p->TN / p->cg) * kBlock;
@@ -93,7 +98,9 @@ inline int stage_blocks(int TM, int TN, int cg) {
 // longer than the best that was timed, on average.  Either side (us): 11008 x 4096, one row: TM 80 10.1, TM 128 11.2; 128 rows: pairs of TM
 // 80 14.0, single CTAs of TM 80 14.9; 512 rows: pairs of 192 rows 24.0, of 256 27.4; 4096 x 11008, one row: TM 128 split four ways 12.0,
 // TM 32 not split 15.1; 3584 x 18944, one row: TM 112 split four ways 15.5, not split 26.8; 200 x 11008, 32 rows: four ways 8.6, not split 16.7;
-// 4096 rows, 4096 -> 11008: pairs of 256 rows 123, single CTAs 150.
+// 4096 rows, 4096 -> 11008: pairs of 256 rows 123, single CTAs 150.  It is furthest off on small layers and few rows, whose tiles all stay
+// below the floor: one row, weights from HBM, 4096 x 4096 TM 80 8.3, TM 32 8.0, TM 128 split three ways 8.0; 2048 x 2048 TM 128 5.8, TM 64 5.3; 1024
+// x 4096 TM 80 7.3, TM 32 7.2, TM 64 split four ways 6.0.
 inline int64_t tile_cost(int64_t tiles, int64_t blocks, int TN, int TM, int cg, int split) {
   const int64_t rounds = split > 1 ? 1 : div_up(tiles, kChipSMs / cg), load = (TM + TN / cg) * 23 / 10;
   const int64_t work = div_up(blocks, split) * (load > 160 ? load : 160), floor = 7000 + 5 * TN;

@@ -4,8 +4,8 @@
 // neighbouring values W at a time, every load and store of a warp of whole neighbouring lines: eight of 16 bits, four where values are
 // written too (their 16-byte stores would leave half-written sectors otherwise).  The largest magnitude is found on the values' bits,
 // which order like the magnitudes, a NaN above all.  Rows beyond what the registers hold are read a second time.  Bound by HBM where
-// values are written, otherwise by the issue slots: some 7 instructions a value and 100 a thread and row.  11008 rows of 4096 bf16: 29 us (4.6
-// TB/s, issue slots 71 % busy), with values 50 (6.3 TB/s).
+// values are written; otherwise by nothing alone: some 7 instructions a value and 100 a thread and row, with the rows that the registers let stand
+// on an SM.  11008 rows of 4096 bf16: 29 us (4.6 TB/s, 71 % of the issue slots, 55 % of the warps), with values 50 (6.3 TB/s).
 #include "int8_common.cuh"
 
 namespace pipe {

@@ -1,7 +1,7 @@
 // Products of the 8-bit integer layers on the tensor cores (pipe_int8_linear, pipe_int8_expert_linear): tcgen05 kind::i8.
 //
-// The weights are the M operand, the tokens the N operand: a tile is 128 output channels per CTA (256 over a pair of SMs, cta_group::2) by
-// up to TN rows, so that one token costs an MMA of 16 columns and a prompt one of 256.  Both operands lie K-major as they are in memory:
+// The weights are the M operand, the tokens the N operand: a tile is TM output channels per CTA, 32 to 128 of the MMA's 128 (over a pair of SMs,
+// cta_group::2, twice that) by up to TN rows, so that one token costs an MMA of 16 columns and a prompt one of 256.  Both operands lie K-major as they are in memory:
 // tensor copies of 128 codes by the tile's rows in the 128-byte swizzle, on one ring, what lies behind the rows or the reduction axis
 // read as zeros.  Sums are int32 in tensor memory, exact, in two accumulators, so that the drain of a tile overlaps the next one's
 // products.  The drain applies the channel's scale, the token's, bias and sigma; 16-bit outputs are turned in shared memory to rows of
@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(kThreads) int8_tc_kernel(const __grid_constant
             }
           }
         } else if (!p.wide_y) {
-          // rows that begin anywhere: a channel a lane as well, 16 rows at a time (2095 rows of 4798 channels: 17 us; turned and stored
+          // rows that begin anywhere: a channel a lane as well, 16 rows at a time (2095 rows of 4798 channels: 15 us; turned and stored
           // a row at a time 29, eight neighbouring channels a lane 56)
           const int o = o0 + 32 * q + lane;
           const float scale = o < end ? __ldcg(p.call.sw + ch0 + o) : 0.f, add = c.bias && o < end ? H::load(c.bias, ch0 + o) : 0.f;

@@ -176,7 +176,10 @@ __device__ __forceinline__ uint32_t key_in(Entry e) { return static_cast<uint32_
 __device__ __forceinline__ int place_in(Entry e) { return static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(e)); }
 
 constexpr int kGroups = 256, kFewGroups = 32;
-constexpr int kFewAlternatives = 20;   // a bound from kFewGroups groups: 31 logits are found for the 20 largest, on average, 12 for 10
+// Up to so many alternatives the bound is that of kFewGroups groups: 31 logits are found for the 20 largest, on average, 12 for 10.  By few
+// groups and by more (us, bf16): 4000 x 16000 k = 10 35.3, 36.1, 16 39.1, 38.9, 20 43.4, 41.0, 21 44.7, 41.5, 28 56, 46; 2048 x 128000 10 99.1, 101.6, 16
+// 104.7, 106.9, 20 109.7, 108.6, 21 114, 107, 28 126, 115; one row of 32000 10 5.6, 5.9, 20 6.3, 6.2, 24 7.4, 6.9.
+constexpr int kFewAlternatives = 20;
 constexpr int kFewFound = 64;          // that one warp ranks, or a CTA hands to its cluster's first
 static_assert(kFewFound >= PIPE_MAX_TOP && kCluster * kFewFound <= kFound, "");
 
