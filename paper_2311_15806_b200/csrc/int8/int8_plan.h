@@ -65,7 +65,7 @@ inline bool lay_out(const TcShape& c, TcPlan* p) {
   //                                SiLU                 68, 54; 72, 62; 77, 69; 88, 85
   //   4096 channels, 16-bit, identity and SiLU          1024 21, 20 and 30, 26; 1408 22.7, 23.1 and 31, 27; 2048 28, 29 and 33, 31
   //   1024 rows to 32000                                1024 35, 34 and 48, 42; 1408 42, 42 and 52, 47; 2048 55, 58 and 62, 61
-  // and in one round 300 rows of I = 1024 9.1, 11.0.  (With an activation 16 still win at 2048, which the rule, blind to it, gives away: 1 to 6 %.)
+  // and in one round 300 rows of I = 1024 9.1, 11.0.  (With an activation 16 still win at 2048, which the rule, blind to it, gives away: 1 to 8 %.)
   p->drain = p->split == 1 && c.I <= kShort && p->tiles > kChipSMs / p->cg ? kMoreDrainWarps : kDrainWarps;
   const int turn = p->split > 1 ? 0 : p->drain * kTurnBytes, sx = p->split > 1 ? 0 : 4 * wide * 4, table = unit_ints(c.E) * 4;
   const int stage = p->KS * (p->TM + p->TN / p->cg) * kBlock;
